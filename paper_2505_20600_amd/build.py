@@ -18,8 +18,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmaskstep.so")
 
 SOURCES = ["compact.hip", "rows.hip", "gemm.hip", "attention.hip", "maskstep.hip", "noalloc.hip",
-           "copyplan.hip", "probes.hip"]
-HEADERS = ["common.h", "kernels.h", "step_internal.h"]
+           "copyplan.hip", "probes.hip", "kv8.hip", "kv8_attention.hip", "kv8_api.hip"]
+HEADERS = ["common.h", "kernels.h", "kv8.h", "step_internal.h"]
 
 ARCH = "gfx950"
 FLAGS = [

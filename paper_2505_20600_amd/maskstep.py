@@ -48,6 +48,23 @@ class KVSource(C.Structure):
 MS_KV_LOADS_AHEAD = 1
 
 
+class Kv8Cache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_caches", C.c_int32), ("tokens", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("block", C.c_int32), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class Kv8Select(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("ld_keys", C.c_int32), ("cache_of", C.c_void_p), ("keys", C.c_void_p),
+                ("n_keys", C.c_void_p)]
+
+
+class Kv8Attn(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("rows", C.c_int32), ("n_heads", C.c_int32),
+                ("n_seg", C.c_int32), ("seg_start", C.c_void_p), ("seg_req", C.c_void_p), ("fresh", C.c_void_p),
+                ("fresh_rows", C.c_int64), ("fresh_list", C.c_void_p), ("fresh_entries", C.c_int32),
+                ("fresh_start", C.c_void_p), ("scale", C.c_float)]
+
+
 class CostModel(C.Structure):
     """ms_cost_model: per-block Comp(F) = comp_ms0 + comp_ms_per_gflop * F / 1e9 and
     Load(B) = load_ms0 + load_ms_per_mb * B / 1e6 (Sec. 4.3)."""
@@ -100,6 +117,11 @@ def load() -> C.CDLL:
                                              C.POINTER(C.c_double)]),
             "mask_profiler_start": (i32, [C.c_uint32, i32]),
             "ms_linear": (i32, [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]),
+            "ms_kv8_keys": (i32, [vp, i32, i32, vp, i32, vp, vp]),
+            "ms_kv8_quantize": (i32, [C.POINTER(Kv8Cache), vp, C.c_int64, C.c_int64, vp, vp]),
+            "ms_kv8_dequantize": (i32, [C.POINTER(Kv8Cache), C.POINTER(Kv8Select), vp, C.c_int64, vp]),
+            "ms_kv8_attention_workspace_bytes": (sz, [C.POINTER(Kv8Cache), C.POINTER(Kv8Select), C.POINTER(Kv8Attn)]),
+            "ms_kv8_attention": (i32, [C.POINTER(Kv8Cache), C.POINTER(Kv8Select), C.POINTER(Kv8Attn), vp, sz, vp]),
             "mask_profiler_stop": (i32, [C.POINTER(C.c_double), C.POINTER(C.c_int64), C.POINTER(C.c_int64)]),
             "mask_profiler_intervals": (i32, [C.POINTER(C.c_int32), C.POINTER(C.c_double), C.POINTER(C.c_double),
                                               i32, C.POINTER(C.c_int32)]),
@@ -132,7 +154,9 @@ EXPORTED = ("mask_abi_version", "mask_last_error", "mask_workspace_bytes", "mask
             "mask_step_set_dense_prefix", "mask_plan_dense_prefix",
             "mask_profiler_start", "mask_profiler_stop", "mask_profiler_intervals", "ms_linear",
             "mask_fit_linear", "mask_batch_cost", "mask_route_request", "mask_plan_copies",
-            "mask_probe_mfma", "mask_probe_lds", "mask_probe_operand_stream")
+            "mask_probe_mfma", "mask_probe_lds", "mask_probe_operand_stream",
+            "ms_kv8_keys", "ms_kv8_quantize", "ms_kv8_dequantize", "ms_kv8_attention_workspace_bytes",
+            "ms_kv8_attention")
 
 MS_EPI_BIAS, MS_EPI_BIAS_RESID, MS_EPI_BIAS_GELU = 0, 1, 2
 
@@ -146,6 +170,190 @@ def ms_linear(A, W, bias, out, *, resid=None, epilogue=MS_EPI_BIAS, tile=(0, 0),
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(load().ms_linear(dt, M, N, K, _ptr(A), _ptr(W), _ptr(bias), _ptr(resid), _ptr(out), epilogue,
                             tile[0], tile[1], ksplit, _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# K/V cache in 8 bits. codes uint8 [caches][tokens][2][kv_heads][head_dim] and scales
+# uint8 [caches][ceil(tokens / block)][2][kv_heads], both contiguous; float32 or bf16 rows.
+# The tables (cache_of, keys, n_keys, src_row, seg_start, ...) are contiguous int32 tensors.
+# ---------------------------------------------------------------------------
+
+_KV8_DTYPES = {torch.bfloat16: MS_BF16, torch.float32: MS_FP32}
+
+
+def _kv8_bad(what):
+    return MaskStepError(MS_EINVAL, what)
+
+
+def _kv8_table(t, dev, shape, name):
+    if t is None:
+        return None
+    if not (t.dtype == torch.int32 and t.device == dev and t.shape == shape and t.is_contiguous()):
+        raise _kv8_bad(f"{name} must be a contiguous int32 tensor {tuple(shape)} on {dev}, not {t.dtype} {tuple(t.shape)} "
+                       f"on {t.device}")
+    return t.data_ptr()
+
+
+def _kv8_cache(codes, scales, block, like):
+    """ms_kv8_cache of the two tensors; ``like``: a K/V or query tensor of the element type."""
+    if codes.dim() != 5 or codes.shape[2] != 2 or codes.element_size() != 1 or not codes.is_contiguous():
+        raise _kv8_bad(f"codes must be contiguous bytes [caches][tokens][2][kv_heads][head_dim], not {codes.dtype} "
+                       f"{tuple(codes.shape)}")
+    S, T, _, H, hd = codes.shape
+    if block < 1 or scales.shape != (S, -(-T // block), 2, H) or scales.element_size() != 1 or not scales.is_contiguous():
+        raise _kv8_bad(f"scales must be contiguous bytes [caches][ceil(tokens / block)][2][kv_heads], not {scales.dtype} "
+                       f"{tuple(scales.shape)} (block {block})")
+    dt = _KV8_DTYPES.get(like.dtype)
+    if dt is None:
+        raise _kv8_bad(f"rows must be bfloat16 or float32, not {like.dtype}")
+    dev = like.device
+    if codes.device != dev or scales.device != dev or not like.is_cuda:
+        raise _kv8_bad("codes, scales and rows must be on one GPU")
+    return Kv8Cache(dt, S, T, H, hd, block, codes.data_ptr(), scales.data_ptr())
+
+
+def _kv8_select(dev, batch, cache_of, keys, n_keys):
+    ld = 0 if keys is None else keys.shape[-1]
+    return Kv8Select(batch, ld, _kv8_table(cache_of, dev, (batch,), "cache_of"), _kv8_table(keys, dev, (batch, ld), "keys"),
+                     _kv8_table(n_keys, dev, (batch,), "n_keys"))
+
+
+def _kv8_stride(kv, c):
+    """Rows between the requests of K/V rows [..][rows][2][kv_heads][head_dim] (contiguous but for the first axis)."""
+    H, hd = c.n_kv_heads, c.head_dim
+    row = 2 * H * hd
+    if kv.dim() != 5 or kv.shape[2:] != (2, H, hd) or kv.shape[1] < c.tokens:
+        raise _kv8_bad(f"kv must be [caches or requests][>= {c.tokens} rows][2][{H}][{hd}], not {tuple(kv.shape)}")
+    if kv.is_contiguous():
+        return kv.shape[1]
+    step = kv.stride(0)
+    if not kv[0].is_contiguous() or (kv.shape[0] > 1 and (step % row or step < c.tokens * row)):
+        raise _kv8_bad(f"kv must be contiguous within the first axis and its requests whole rows apart, not strided {kv.stride()}")
+    return kv.shape[1] if kv.shape[0] == 1 else step // row
+
+
+class _on_device_of:
+    """The tensor's device as the current one (a launch goes to the current device's stream)."""
+    __slots__ = ("dev", "was")
+
+    def __init__(self, t):
+        self.dev = t.device.index
+
+    def __enter__(self):
+        self.was = torch.cuda.current_device()
+        if self.was != self.dev:
+            torch.cuda.set_device(self.dev)
+
+    def __exit__(self, *exc):
+        if self.was != self.dev:
+            torch.cuda.set_device(self.was)
+
+
+def ms_kv8_keys(mask, keys, n_keys, *, stream=None):
+    """Ascending unmasked tokens of every request: mask uint8 or bool [batch][tokens] -> keys [batch][>= tokens],
+    n_keys [batch]."""
+    if not mask.is_cuda or mask.dim() != 2 or mask.element_size() != 1 or not mask.is_contiguous():
+        raise _kv8_bad("mask must be contiguous bytes [batch][tokens] on a GPU")
+    B, T = mask.shape
+    kp = _kv8_table(keys, mask.device, (B, keys.shape[-1]), "keys")
+    np_ = _kv8_table(n_keys, mask.device, (B,), "n_keys")
+    with _on_device_of(mask):
+        _check(load().ms_kv8_keys(mask.data_ptr(), B, T, kp, keys.shape[-1], np_, _stream(stream)))
+
+
+def ms_kv8_quantize(kv, codes, scales, *, block, src_row=None, stream=None):
+    """K/V rows into the caches. Without ``src_row``: kv [caches][>= tokens][2][kv_heads][head_dim], every token
+    written. With it (int32 [caches][tokens]): kv [rows][2][kv_heads][head_dim], token t of cache s becomes row
+    src_row[s][t], or keeps its value where that is no row of kv."""
+    c = _kv8_cache(codes, scales, block, kv)
+    if src_row is None:
+        stride = _kv8_stride(kv, c)
+        if kv.shape[0] != c.n_caches:
+            raise _kv8_bad(f"kv holds {kv.shape[0]} caches, codes {c.n_caches}")
+        rows, src = (c.n_caches - 1) * stride + max(stride, c.tokens), None
+    else:
+        if kv.dim() != 4 or kv.shape[1:] != (2, c.n_kv_heads, c.head_dim) or not kv.is_contiguous():
+            raise _kv8_bad(f"with src_row, kv must be contiguous [rows][2][kv_heads][head_dim], not {tuple(kv.shape)}")
+        src = _kv8_table(src_row, kv.device, (c.n_caches, c.tokens), "src_row")
+        rows, stride = kv.shape[0], 0
+        if rows == 0:
+            return
+    with _on_device_of(kv):
+        _check(load().ms_kv8_quantize(C.byref(c), kv.data_ptr(), rows, stride, src, _stream(stream)))
+
+
+def ms_kv8_dequantize(codes, scales, kv, *, block, cache_of=None, keys=None, n_keys=None, stream=None):
+    """The listed tokens' values into kv [batch][>= tokens][2][kv_heads][head_dim] at their token's row; the other rows
+    are left as they are."""
+    c = _kv8_cache(codes, scales, block, kv)
+    stride = _kv8_stride(kv, c)
+    sel = _kv8_select(kv.device, kv.shape[0], cache_of, keys, n_keys)
+    with _on_device_of(kv):
+        _check(load().ms_kv8_dequantize(C.byref(c), C.byref(sel), kv.data_ptr(), stride, _stream(stream)))
+
+
+def ms_kv8_attention_workspace_bytes(q, codes, seg_start, *, keys=None, fresh=None, fresh_list=None) -> int:
+    """Bytes of workspace with which ms_kv8_attention may split the keys as it sees fit, for tensors of these shapes."""
+    S, T, _, H, hd = codes.shape
+    n_seg = seg_start.shape[0] - 1
+    some = 16   # an address that is checked but not read
+    c = Kv8Cache(_KV8_DTYPES.get(q.dtype, -1), S, T, H, hd, 1, some, some)
+    sel = Kv8Select(n_seg, 0 if keys is None else keys.shape[-1], some, None if keys is None else some, None)
+    f_rows = 0 if fresh is None else fresh.shape[0]
+    a = Kv8Attn(some, some, q.shape[0], q.shape[1], n_seg, some, some, some if f_rows else None, f_rows,
+                None if fresh_list is None else some, 0 if fresh_list is None else fresh_list.numel(), some, 0.0)
+    n = load().ms_kv8_attention_workspace_bytes(C.byref(c), C.byref(sel), C.byref(a))
+    if n == 0 and load().mask_last_error():
+        raise MaskStepError(MS_EINVAL, load().mask_last_error().decode())
+    return n
+
+
+def ms_kv8_attention(q, codes, scales, out, seg_start, *, block, seg_req=None, cache_of=None, keys=None, n_keys=None,
+                     fresh=None, fresh_list=None, fresh_start=None, scale=None, workspace=None, stream=None):
+    """out[rows][heads][head_dim] = attention of the packed query rows q over the listed cached tokens of their request
+    and its fresh K/V rows ([rows][2][kv_heads][head_dim], by fresh_list and fresh_start [batch + 1])."""
+    c = _kv8_cache(codes, scales, block, q)
+    dev = q.device
+    if q.dim() != 3 or q.shape[2] != c.head_dim or not q.is_contiguous():
+        raise _kv8_bad(f"q must be contiguous [rows][heads][{c.head_dim}], not {tuple(q.shape)}")
+    if out.shape != q.shape or out.dtype != q.dtype or out.device != dev or not out.is_contiguous():
+        raise _kv8_bad("out must be like q")
+    n_seg = seg_start.shape[0] - 1
+    batch = n_seg if seg_req is None else c.n_caches
+    if cache_of is not None:
+        batch = cache_of.shape[0]
+    elif n_keys is not None:
+        batch = n_keys.shape[0]
+    elif keys is not None:
+        batch = keys.shape[0]
+    elif fresh is not None and fresh_start is not None:
+        batch = fresh_start.shape[0] - 1
+    sel = _kv8_select(dev, batch, cache_of, keys, n_keys)
+    fp, f_rows, fl, fe, fs = None, 0, None, 0, None
+    if fresh is not None:
+        if (fresh.dim() != 4 or fresh.shape[1:] != (2, c.n_kv_heads, c.head_dim) or fresh.dtype != q.dtype
+                or fresh.device != dev or not fresh.is_contiguous()):
+            raise _kv8_bad(f"fresh must be contiguous [rows][2][kv_heads][head_dim] like q, not {fresh.dtype} "
+                           f"{tuple(fresh.shape)}")
+        if fresh_start is None:
+            raise _kv8_bad("fresh rows need fresh_start")
+        f_rows = fresh.shape[0]
+        fp = fresh.data_ptr() if f_rows else None
+        if fresh_list is not None:
+            fe = fresh_list.numel()
+            fl = _kv8_table(fresh_list, dev, (fe,), "fresh_list")
+        fs = _kv8_table(fresh_start, dev, (batch + 1,), "fresh_start")
+    a = Kv8Attn(q.data_ptr(), out.data_ptr(), q.shape[0], q.shape[1], n_seg,
+                _kv8_table(seg_start, dev, (n_seg + 1,), "seg_start"), _kv8_table(seg_req, dev, (n_seg,), "seg_req"),
+                fp, f_rows, fl, fe, fs, 0.0 if scale is None else scale)
+    wp, wb = 0, 0
+    if workspace is not None:
+        if workspace.device != dev or not workspace.is_contiguous():
+            raise _kv8_bad("workspace must be a contiguous tensor on q's device")
+        wp, wb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    with _on_device_of(q):
+        _check(load().ms_kv8_attention(C.byref(c), C.byref(sel), C.byref(a), wp, wb, _stream(stream)))
+
 
 KERNEL_CLASSES = ("compact", "gather", "layernorm", "gemm_qkv", "attention", "gemm_out", "gemm_up",
                   "gemm_down", "scatter", "copy", "attn_combine", "gemm_reduce")
