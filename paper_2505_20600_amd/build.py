@@ -19,7 +19,7 @@ LIB = os.path.join(PKG, "libmaskstep.so")
 
 SOURCES = ["compact.hip", "rows.hip", "gemm.hip", "attention.hip", "maskstep.hip", "noalloc.hip",
            "copyplan.hip", "probes.hip", "kv8.hip", "kv8_attention.hip", "kv8_api.hip"]
-HEADERS = ["common.h", "kernels.h", "kv8.h", "step_internal.h"]
+HEADERS = ["attn_tiles.h", "common.h", "kernels.h", "kv8.h", "step_internal.h"]
 
 ARCH = "gfx950"
 FLAGS = [

@@ -26,8 +26,8 @@ ms_status check_cache(const ms_kv8_cache* c, ms::Kv8Cache* out) {
         return set_error(MS_ESHAPE, "head_dim %d must be a multiple of 8, at most 128 (bf16) or 64 (fp32)", c->head_dim);
     if (c->block < 1 || c->block > 128 || (c->block & (c->block - 1)))
         return set_error(MS_ESHAPE, "block %d must be a power of two, 1..128", c->block);
-    if (2ll * c->tokens * c->n_kv_heads * c->head_dim >= (1ll << 32))
-        return set_error(MS_ESHAPE, "one cache's codes (tokens x 2 x n_kv_heads x head_dim bytes) must stay below 4 GiB");
+    if (2ll * c->tokens * c->n_kv_heads * c->head_dim >= (1ll << 32) - (1 << 20))
+        return set_error(MS_ESHAPE, "one cache's codes (tokens x 2 x n_kv_heads x head_dim bytes) must stay below 4095 MiB");
     if (!c->codes || !c->scales) return set_error(MS_EINVAL, "codes or scales is NULL");
     if (!aligned(c->codes, 16)) return set_error(MS_EALIGN, "codes not 16-byte aligned");
     out->codes = static_cast<uint8_t*>(c->codes);
@@ -71,6 +71,7 @@ ms_status check_attn(const ms_kv8_cache* c, const ms_kv8_select* sel, const ms_k
     if (a->rows < 0 || a->rows > (1 << 26)) return set_error(MS_ESHAPE, "rows %d outside 0..2^26", a->rows);
     if (a->n_heads < 1 || a->n_heads % c->n_kv_heads || a->n_heads > 1024)
         return set_error(MS_ESHAPE, "n_heads %d must be a multiple of n_kv_heads %d, at most 1024", a->n_heads, c->n_kv_heads);
+    if ((int64_t)a->rows * a->n_heads > (1 << 28)) return set_error(MS_ESHAPE, "rows x n_heads above 2^28");
     if (a->n_seg < 1 || a->n_seg > ms::kKv8MaxSegments)
         return set_error(MS_ESHAPE, "n_seg %d outside 1..%d", a->n_seg, ms::kKv8MaxSegments);
     if (!a->seg_req && a->n_seg > sel->batch) return set_error(MS_ESHAPE, "n_seg %d above batch %d needs seg_req", a->n_seg, sel->batch);
@@ -94,7 +95,7 @@ ms_status check_attn(const ms_kv8_cache* c, const ms_kv8_select* sel, const ms_k
     d->nseg = a->n_seg;
     d->M = a->rows;
     d->group = a->n_heads / c->n_kv_heads;
-    d->kv = a->fresh;
+    d->kv = a->fresh && a->fresh_rows > 0 ? a->fresh : nullptr;
     d->f_rows = a->fresh_list;
     d->f_start = a->fresh_start;
     d->kv_rows = a->fresh ? a->fresh_rows : 0;

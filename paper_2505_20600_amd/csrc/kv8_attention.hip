@@ -1,13 +1,573 @@
 // Attention over an 8-bit K/V cache: packed query rows of a batch over the
 // listed cached tokens of their request (codes and scales) and its fresh K/V
 // rows (the model's type), one softmax over both. A row without any key is 0.
+//
+// A query slot is a (packed row, query head of one K/V head's group) pair, so
+// query heads that share a K/V head share its tiles. A request's keys form
+// tiles: the listed cached tokens first, then the fresh rows. Tiles are staged
+// through registers: lane l of a wave holds tile key l's token number (read one
+// tile ahead), the row's offset and its two scales; the threads fetch the rows'
+// chunks by those offsets, convert codes to bf16 with their scales (exact: a
+// scale is a power of two) on the way to LDS, and the products run on bf16
+// matrix instructions in the layout of attention.hip: S^T = K Q^T leaves the
+// weights in the operand layout of O^T = V^T P^T, V is read transposed by
+// ds_read_b64_tr_b16, rows of ones in V^T give the denominator. Absent keys
+// (past a list's end, numbers out of range) are zero rows with score -inf.
 #include <algorithm>
 
+#include "attn_tiles.h"
 #include "kernels.h"
 #include "kv8.h"
 
 namespace ms {
 namespace {
+
+constexpr int kThreads = 256;
+
+// LDS operations of the wave done (vector-memory loads may stay in flight).
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }
+
+// Which query slots and key tiles a workgroup has.
+struct Work {
+    int row0;       // first packed row of the segment
+    int slots;      // query slots of the segment
+    int q0;         // first slot of this tile
+    int kvh;        // K/V head
+    int split;
+    int t0, t1;     // key tiles
+    int ntc;        // cached tiles of the request
+    Kv8Req r;
+};
+
+// Slot tile `tile` of all segments, K/V head and key range; false: past the last tile.
+template <int QT, int KT>
+__device__ __forceinline__ bool find_work(const Kv8AttnDesc& a, int tile, int kvh, int split, Work& w) {
+    int seg = 0, r0 = 0, r1 = 0;
+    for (; seg < a.nseg; ++seg) {
+        r0 = min(max(a.seg_start[seg], 0), a.M);
+        r1 = min(max(a.seg_start[seg + 1], r0), a.M);
+        const int nt = ((r1 - r0) * a.group + QT - 1) / QT;
+        if (tile < nt) break;
+        tile -= nt;
+    }
+    if (seg >= a.nseg) return false;
+    w.row0 = r0;
+    w.slots = (r1 - r0) * a.group;
+    w.q0 = tile * QT;
+    w.kvh = kvh;
+    w.split = split;
+    const int b = a.seg_req ? a.seg_req[seg] : seg;
+    w.r = Kv8Req{nullptr, nullptr, nullptr, 0, 0, 0};
+    if (b >= 0 && b < a.sel.batch) {
+        w.r = kv8_request(a.c, a.sel, b);
+        kv8_fresh(a, b, w.r);
+    }
+    w.ntc = (w.r.nk + KT - 1) / KT;
+    const long nt = w.ntc + (w.r.nf + KT - 1) / KT;
+    w.t0 = (int)(nt * split / a.nsplit);
+    w.t1 = (int)(nt * (split + 1) / a.nsplit);
+    return true;
+}
+
+// Row index of a query slot's (row, query head) in [M][n_heads].
+__device__ __forceinline__ long slot_row(const Kv8AttnDesc& a, const Work& w, int slot) {
+    const int HG = a.c.heads * a.group;
+    if (a.group == 1) return (long)(w.row0 + slot) * HG + w.kvh;
+    const int r = slot / a.group;
+    return (long)(w.row0 + r) * HG + w.kvh * a.group + (slot - r * a.group);
+}
+
+// Staging of KT-key tiles by NT threads, each 1/NT of the chunks of CW elements.
+template <int HD, int KT, int NT>
+struct Stager {
+    static constexpr int CW = HD % 16 == 0 ? 16 : 8;
+    static constexpr int CR = HD / CW;                  // chunks per row
+    static constexpr int NCHUNK = KT * 2 * CR;
+    static constexpr int NCH = (NCHUNK + NT - 1) / NT;
+    static constexpr int ROWB = HD * 2;
+    static constexpr int TILEB = KT * ROWB;
+    static constexpr int KPAD = 16;                     // zeros past the K tile, read by padding slots of the last QK step
+    static constexpr int STAGEB = 2 * TILEB + KPAD;
+    static constexpr uint32_t kAbsent = 0xfff00000u;    // row offset past every cache's end
+
+    __amdgpu_buffer_rsrc_t rsrc;
+    int tid, lane;
+    uint32_t row_bytes;     // of a token's codes
+    int rl[NCH];            // tile key of each chunk
+    uint32_t coloff[NCH];   // its first element within a token's row
+    uint32_t dst[NCH];      // LDS offset of its first 16 bytes in a stage; the second 16 at ^ 16 unless swizzled
+    uint32_t dst2[CW == 16 ? NCH : 1];
+    vec16 raw[NCH][CW / 8];
+    uint32_t sb = 0;        // this lane's key: scale bytes, K in bits 0-7, V in 8-15
+    uint32_t sk = 0, sv = 0;
+    int idx = -1;           // token number (row of the fresh K/V) of this lane's key in the next tile to issue
+    uint64_t valid = 0;     // present keys of the tile in raw
+
+    __device__ __forceinline__ void init(const Kv8AttnDesc& a, const Work& w, int tid_) {
+        tid = tid_;
+        lane = threadIdx.x % kWave;
+        const int dkv = a.c.heads * HD;
+        row_bytes = 2 * dkv;
+        rsrc = make_rsrc(w.r.codes, w.r.codes ? (uint32_t)a.c.T * row_bytes : 0u);
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            const int q = min(i * NT + tid, NCHUNK - 1);
+            const bool isv = q >= KT * CR;
+            const int r = (q / CR) % KT, c = (q % CR) * (CW / 8);
+            rl[i] = r;
+            coloff[i] = (isv ? dkv : 0) + w.kvh * HD + c * 8;
+            const int sw = isv ? v_swz<ROWB>(r) : k_swz<ROWB>(r);
+            const uint32_t base = (isv ? TILEB + KPAD : 0) + r * ROWB;
+            dst[i] = base + (c ^ sw) * 16;
+            if constexpr (CW == 16) dst2[i] = base + ((c + 1) ^ sw) * 16;
+        }
+    }
+    // number of this lane's key of tile t
+    __device__ __forceinline__ void fetch_index(const Kv8AttnDesc& a, const Work& w, int t) {
+        idx = -1;
+        if (t >= w.t1 || lane >= KT) return;
+        if (t < w.ntc) {
+            const int i = t * KT + lane;
+            if (i < w.r.nk) {
+                idx = w.r.keys ? w.r.keys[i] : i;
+                if (idx >= a.c.T) idx = -1;
+            }
+        } else {
+            const int i = (t - w.ntc) * KT + lane;
+            if (i < w.r.nf) {
+                idx = a.f_rows ? a.f_rows[w.r.f0 + i] : w.r.f0 + i;
+                if (idx >= a.kv_rows) idx = -1;
+            }
+        }
+    }
+    // starts the loads of tile t, whose numbers fetch_index has read
+    __device__ __forceinline__ void issue(const Kv8AttnDesc& a, const Work& w, int t) {
+        valid = __ballot(idx >= 0);
+        if (t < w.ntc) {
+            const uint32_t off = idx >= 0 ? (uint32_t)idx * row_bytes : kAbsent;
+            sk = sv = 0;
+            if (idx >= 0) {
+                const uint8_t* sp = w.r.scales + (long)(idx >> a.c.lblock) * 2 * a.c.heads + w.kvh;
+                sk = sp[0];
+                sv = sp[a.c.heads];
+            }
+#pragma unroll
+            for (int i = 0; i < NCH; ++i) {
+                const uint32_t o = (uint32_t)__shfl((int)off, rl[i], kWave) + coloff[i];
+                if constexpr (CW == 16) {
+                    raw[i][0] = buf_ld16(rsrc, o, 0);
+                } else {
+                    const auto v = __builtin_amdgcn_raw_buffer_load_b64(rsrc, (int)o, 0, 0);
+                    raw[i][0].w[0] = v[0];
+                    raw[i][0].w[1] = v[1];
+                }
+            }
+        } else {
+            const int safe = max(idx, 0);
+#pragma unroll
+            for (int i = 0; i < NCH; ++i) {
+                const long row = __shfl(safe, rl[i], kWave);
+                const bf16_t* p = static_cast<const bf16_t*>(a.kv) + row * row_bytes + coloff[i];
+#pragma unroll
+                for (int j = 0; j < CW / 8; ++j) raw[i][j] = ld16(p + 8 * j);
+            }
+        }
+    }
+    // the tile in raw, as bf16, to the stage at smem
+    __device__ __forceinline__ void store(const Work& w, int t, uint8_t* smem) {
+        if (t < w.ntc) {
+            // the two scales as the upper halves of their float32 values
+            const uint32_t both = (__float_as_uint(kv8_scale(sk)) >> 16) | __float_as_uint(kv8_scale(sv));
+#pragma unroll
+            for (int i = 0; i < NCH; ++i) {
+                const uint32_t pr = (uint32_t)__shfl((int)both, rl[i], kWave);
+                const float s = __uint_as_float(i * NT + tid >= KT * CR ? pr & 0xffff0000u : pr << 16);
+                vec16 o[CW / 8];
+#pragma unroll
+                for (int j = 0; j < CW / 8; ++j) {
+                    o[j].w[0] = kv8_to_bf16x2<false>(raw[i][0].w[2 * j], s);
+                    o[j].w[1] = kv8_to_bf16x2<true>(raw[i][0].w[2 * j], s);
+                    o[j].w[2] = kv8_to_bf16x2<false>(raw[i][0].w[2 * j + 1], s);
+                    o[j].w[3] = kv8_to_bf16x2<true>(raw[i][0].w[2 * j + 1], s);
+                }
+                put(i, o, smem);
+            }
+        } else {
+            const uint64_t all = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
+#pragma unroll
+            for (int i = 0; i < NCH; ++i) {
+                vec16 o[CW / 8];
+#pragma unroll
+                for (int j = 0; j < CW / 8; ++j) o[j] = raw[i][j];
+                if (valid != all && !((valid >> rl[i]) & 1)) {
+#pragma unroll
+                    for (int j = 0; j < CW / 8; ++j) o[j] = vec16{{0u, 0u, 0u, 0u}};
+                }
+                put(i, o, smem);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(int i, const vec16 (&o)[CW / 8], uint8_t* smem) {
+        if (NCHUNK % NT == 0 || i * NT + tid < NCHUNK) {
+            st16(smem + dst[i], o[0]);
+            if constexpr (CW == 16) st16(smem + dst2[i], o[1]);
+        }
+    }
+};
+
+// bf16. SHARED: 128 query slots, 32 per wave, the four waves share 64-key tiles
+// in two stages. Not SHARED: 16 slots, every wave has key tiles of its own (32
+// keys, tile t0 + wave + 4 i) and the four partial results are joined at the end.
+template <int HD, bool SHARED>
+struct Bf16Cfg {
+    static constexpr int KT = SHARED ? 64 : 32;
+    static constexpr int NQB = SHARED ? 2 : 1;          // 16-slot blocks per wave
+    static constexpr int QT = SHARED ? 128 : 16;
+    static constexpr int NT = SHARED ? kThreads : kWave;
+    static constexpr int STAGES = SHARED ? 2 : 1;
+    using S = Stager<HD, KT, NT>;
+    static constexpr int NKS = KT / 16;
+    static constexpr int NK32 = (HD + 31) / 32;
+    static constexpr bool KTAIL = HD % 32 != 0;
+    static constexpr bool SUM_IN_PAD = HD % 16 != 0;
+    static constexpr int NREAL = (HD + 15) / 16;
+    static constexpr int NHS = NREAL + (SUM_IN_PAD ? 0 : 1);
+    static constexpr int LDSB = (SHARED ? STAGES : 4) * S::STAGEB;
+};
+
+template <int HD, bool SHARED>
+__global__ __launch_bounds__(kThreads, SHARED ? (HD <= 48 ? 4 : HD <= 64 ? 3 : 2) : 2) void attend_bf16_kernel(Kv8AttnDesc a, int qtiles) {
+    using C = Bf16Cfg<HD, SHARED>;
+    using S = typename C::S;
+    constexpr int NQB = C::NQB, NKS = C::NKS;
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDSB + 16];
+    const uint32_t lds0 = lds_addr(smem);
+    const uint32_t ones_rel = C::LDSB;                  // 8 bytes of bf16 ones (SUM_IN_PAD)
+
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const int grp = lane / 16, l16 = lane % 16;
+    // SHARED: a head's slot tiles side by side, so that an XCD's L2 serves a head's codes to
+    // all of them; else a tile's heads side by side, which read neighbouring parts of the rows
+    const int total = qtiles * a.nsplit * a.c.heads;
+    const int lb = xcd_logical_block(blockIdx.x, total);
+    Work w;
+    if constexpr (SHARED) {
+        if (!find_work<C::QT, C::KT>(a, lb % qtiles, lb / (qtiles * a.nsplit), lb / qtiles % a.nsplit, w)) return;
+    } else {
+        if (!find_work<C::QT, C::KT>(a, lb / (a.nsplit * a.c.heads), lb % a.c.heads, lb / a.c.heads % a.nsplit, w)) return;
+    }
+    const int first = SHARED ? w.t0 : w.t0 + wave, step = SHARED ? 1 : 4;
+
+    // constant LDS: the K pads' zeros and the ones block
+    constexpr int NSTG = SHARED ? C::STAGES : 4;
+    if (tid < NSTG) *reinterpret_cast<uint4*>(smem + tid * S::STAGEB + S::TILEB) = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == NSTG) *reinterpret_cast<uint2*>(smem + C::LDSB) = make_uint2(0x3f803f80u, 0x3f803f80u);
+
+    S st;
+    st.init(a, w, SHARED ? tid : lane);
+    st.fetch_index(a, w, first);
+
+    // Q^T fragments (B operand), their sign that of the score scale
+    bf16x8_t qf[NQB][C::NK32];
+    const bf16_t* __restrict__ q = static_cast<const bf16_t*>(a.q);
+    const int wq0 = w.q0 + (SHARED ? wave * 32 : 0);
+    const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+        const int slot = wq0 + qb * 16 + l16;
+        const bf16_t* qp = q + slot_row(a, w, slot) * HD;
+#pragma unroll
+        for (int kc = 0; kc < C::NK32; ++kc) {
+            vec16 v = {{0u, 0u, 0u, 0u}};
+            if (slot < w.slots && kc * 32 + grp * 8 < HD) v = ld16(qp + kc * 32 + grp * 8);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v.w[j] ^= flip;
+            qf[qb][kc] = __builtin_bit_cast(bf16x8_t, v);
+        }
+    }
+
+    // fragment read offsets inside a stage (bytes)
+    const int fK = k_swz<S::ROWB>(l16);
+    uint32_t koff[C::NK32];
+#pragma unroll
+    for (int kc = 0; kc < C::NK32; ++kc) koff[kc] = l16 * S::ROWB + (((4 * kc + grp) ^ fK) * 16);
+    uint32_t kofft[C::KTAIL ? NKS : 1];
+    if constexpr (C::KTAIL) {
+        const int col = (C::NK32 - 1) * 64 + grp * 16;   // bytes
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks)
+            kofft[ks] = col < S::ROWB ? (ks * 16 + l16) * S::ROWB + ((col / 16) ^ fK) * 16 : S::TILEB;
+    }
+    const int rowA = 4 * grp + (l16 >> 2);
+    const int fV = v_swz<S::ROWB>(rowA);
+    uint32_t voffh[C::NREAL];
+#pragma unroll
+    for (int h = 0; h < C::NREAL; ++h) {
+        const int hd = 16 * h + 4 * (l16 & 3);
+        voffh[h] = S::TILEB + S::KPAD + rowA * S::ROWB + (((hd / 8) ^ fV) * 16) + (hd % 8) * 2;
+    }
+    const bool ones_lane = C::SUM_IN_PAD && (16 * (C::NREAL - 1) + 4 * (l16 & 3)) >= HD;
+
+    f32x4_t oacc[NQB][C::NHS];
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+        for (int h = 0; h < C::NHS; ++h) oacc[qb][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const float cs = fabsf(a.scale_log2), rescale_at = kRescaleLog2 / cs;
+    float m_run[NQB];
+    f32x4_t negm[NQB];
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+        m_run[qb] = -INFINITY;
+        negm[qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    bool beyond = true;
+    const bf16x8_t onesf = __builtin_bit_cast(bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
+    constexpr uint64_t kAll = C::KT == 64 ? ~0ull : (1ull << (C::KT % 64)) - 1;
+
+    auto qk = [&](uint32_t sbase, uint64_t present, f32x4_t (&sacc)[NQB][NKS]) {
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) sacc[qb][ks] = negm[qb];
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+#pragma unroll
+            for (int kc = 0; kc < C::NK32; ++kc) {
+                const bool pad = C::KTAIL && kc == C::NK32 - 1;
+                const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(
+                    smem + sbase + (pad ? kofft[C::KTAIL ? ks : 0] : koff[kc] + ks * 16 * S::ROWB));
+#pragma unroll
+                for (int qb = 0; qb < NQB; ++qb) sacc[qb][ks] = mfma32(kf, qf[qb][kc], sacc[qb][ks]);
+            }
+        }
+        if (present != kAll) {
+            const uint64_t mine = present >> (grp * 4);
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (!((mine >> (ks * 16 + r)) & 1)) {
+#pragma unroll
+                        for (int qb = 0; qb < NQB; ++qb) sacc[qb][ks][r] = -INFINITY;
+                    }
+        }
+    };
+    // online softmax in place: sacc becomes the weights; running maxima and accumulators
+    // updated, a rescale only where a score exceeds its slot's maximum by more than 2^8
+    auto softmax = [&](f32x4_t (&sacc)[NQB][NKS], bool first_tile) {
+        float mx[NQB];
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+            mx[qb] = sacc[qb][0][0];
+#pragma unroll
+            for (int i = 1; i < 4 * NKS; ++i) mx[qb] = fmaxf(mx[qb], sacc[qb][i / 4][i % 4]);
+        }
+        float most = mx[0];
+#pragma unroll
+        for (int qb = 1; qb < NQB; ++qb) most = fmaxf(most, mx[qb]);
+        if (beyond || __any(most > rescale_at)) {
+            bool far = false;
+#pragma unroll
+            for (int qb = 0; qb < NQB; ++qb) {
+                const float rm = rows_max(mx[qb]);
+                const bool none = m_run[qb] == -INFINITY;
+                const float was = none ? -INFINITY : m_run[qb] + negm[qb][0];
+                const float up = fmaxf(rm, was);
+                const bool still = up == -INFINITY;
+                if (!first_tile) {
+                    const float corr = none ? 0.f : fast_exp2((was - up) * cs);
+#pragma unroll
+                    for (int h = 0; h < C::NHS; ++h) oacc[qb][h] *= corr;
+                }
+                m_run[qb] = fmaxf(m_run[qb], rm - negm[qb][0]);
+                const float n = m_run[qb] == -INFINITY ? 0.f : -fminf(fmaxf(m_run[qb], -kStartMax), kStartMax);
+                negm[qb] = f32x4_t{n, n, n, n};
+                far |= fabsf(m_run[qb]) > kStartMax;
+                const float off = still ? 0.f : up;
+#pragma unroll
+                for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sacc[qb][ks][r] -= off;
+            }
+            beyond = __any(far);
+        }
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sacc[qb][ks][r] = fast_exp2(sacc[qb][ks][r] * cs);
+    };
+    auto pv = [&](uint32_t sbase, f32x4_t (&sacc)[NQB][NKS]) {
+        uint32_t vbase[C::NREAL];
+#pragma unroll
+        for (int h = 0; h < C::NREAL; ++h) {
+            vbase[h] = lds0 + sbase + voffh[h];
+            asm volatile("" : "+v"(vbase[h]));   // keep the sum: offsets are added per read
+        }
+#pragma unroll
+        for (int c = 0; c < C::KT / 32; ++c) {
+            bf16x8_t vf[C::NHS];
+#pragma unroll
+            for (int h = 0; h < C::NHS; ++h) {
+                if (h >= C::NREAL) {
+                    vf[h] = onesf;
+                } else {
+                    lds_cptr p0 = (lds_cptr)(uintptr_t)vbase[h] + (32 * c) * S::ROWB;
+                    lds_cptr p1 = (lds_cptr)(uintptr_t)vbase[h] + (32 * c + 16) * S::ROWB;
+                    if (h == C::NREAL - 1 && ones_lane) { p0 = (lds_cptr)(uintptr_t)(lds0 + ones_rel); p1 = p0; }
+                    const bf16x4_t lo = ld_tr16(p0), hi = ld_tr16(p1);
+                    vf[h] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+            }
+            bf16x8_t pf[NQB];
+#pragma unroll
+            for (int qb = 0; qb < NQB; ++qb) {
+                uint4 p;
+                p.x = pack_bf16x2(sacc[qb][2 * c][0], sacc[qb][2 * c][1]);
+                p.y = pack_bf16x2(sacc[qb][2 * c][2], sacc[qb][2 * c][3]);
+                p.z = pack_bf16x2(sacc[qb][2 * c + 1][0], sacc[qb][2 * c + 1][1]);
+                p.w = pack_bf16x2(sacc[qb][2 * c + 1][2], sacc[qb][2 * c + 1][3]);
+                pf[qb] = __builtin_bit_cast(bf16x8_t, p);
+            }
+#pragma unroll
+            for (int h = 0; h < C::NHS; ++h)
+#pragma unroll
+                for (int qb = 0; qb < NQB; ++qb) oacc[qb][h] = mfma32(vf[h], pf[qb], oacc[qb][h]);
+        }
+    };
+
+    f32x4_t sa[NQB][NKS];
+    const bool active = wq0 < w.slots;
+    __syncthreads();   // constant LDS
+    if (first < w.t1) {
+        st.issue(a, w, first);
+        st.fetch_index(a, w, first + step);
+    }
+    int n = 0;
+    for (int t = first; t < w.t1; t += step, ++n) {
+        const uint32_t sbase = SHARED ? (n & 1) * S::STAGEB : wave * S::STAGEB;
+        const uint64_t present = st.valid;
+        st.store(w, t, smem + sbase);
+        if (t + step < w.t1) {
+            st.issue(a, w, t + step);
+            st.fetch_index(a, w, t + 2 * step);
+        }
+        wait_lds();
+        if constexpr (SHARED) barrier_only();
+        else __builtin_amdgcn_wave_barrier();
+        if (!active) continue;
+        qk(sbase, present, sa);
+        softmax(sa, n == 0);
+        pv(sbase, sa);
+        if constexpr (!SHARED) asm volatile("" ::: "memory");
+    }
+
+    float l[NQB];
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+        if constexpr (C::SUM_IN_PAD) {
+            // the last 8 rows of the last subtile are the ones rows: lane groups 2-3 hold them
+            const float t0 = grp >= 2 ? oacc[qb][C::NHS - 1][0] : 0.f;
+            auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(t0), __float_as_uint(t0), false, false);
+            l[qb] = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+        } else {
+            l[qb] = oacc[qb][C::NHS - 1][0];
+        }
+    }
+    const long range = (long)w.split * a.M * a.c.heads * a.group;
+    __syncthreads();   // every wave is past its last read of the stages
+    if constexpr (SHARED) {
+        // through LDS: rows of a slot in 16-byte vectors, chunks swizzled by the slot where rows are a power of two
+        constexpr int CH = HD / 8, CF = HD / 4;
+        constexpr int SWM = (CH & (CH - 1)) == 0 ? (CH >= 16 ? 15 : CH - 1) : 0;
+        constexpr int SWF = (CF & (CF - 1)) == 0 ? (CF >= 16 ? 15 : CF - 1) : 0;
+        uint8_t* const so = smem + wave * 32 * S::ROWB * (a.nsplit == 1 ? 1 : 2);
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+            const float inv_l = l[qb] == 0.f ? 0.f : 1.0f / l[qb];
+            const int rl = qb * 16 + l16;
+#pragma unroll
+            for (int h = 0; h < C::NHS; ++h) {
+                const int cidx = h * 16 + grp * 4;
+                if (cidx < HD) {
+                    float v[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = oacc[qb][h][r] * inv_l;
+                    if (a.nsplit == 1)
+                        store4<bf16_t>(reinterpret_cast<bf16_t*>(so + rl * S::ROWB + (((cidx / 8) ^ (rl & SWM)) * 16) + (cidx % 8) * 2), v);
+                    else
+                        store4<float>(reinterpret_cast<float*>(so + rl * 2 * S::ROWB) + ((cidx / 4) ^ (rl & SWF)) * 4, v);
+                }
+            }
+            const int slot = wq0 + rl;
+            if (a.nsplit > 1 && grp == 0 && slot < w.slots)
+                *reinterpret_cast<float2*>(a.part_ml + 2 * (range + slot_row(a, w, slot))) = make_float2(m_run[qb] * cs, l[qb]);
+        }
+        __syncthreads();
+        if (a.nsplit == 1) {
+            for (int k = lane; k < 32 * CH; k += kWave) {
+                const int rl = k / CH, c = k % CH;
+                if (wq0 + rl < w.slots)
+                    st16(static_cast<bf16_t*>(a.o) + slot_row(a, w, wq0 + rl) * HD + c * 8,
+                         ld16(so + rl * S::ROWB + ((c ^ (rl & SWM)) * 16)));
+            }
+        } else {
+            for (int k = lane; k < 32 * CF; k += kWave) {
+                const int rl = k / CF, c = k % CF;
+                if (wq0 + rl < w.slots)
+                    st16(a.part_o + (range + slot_row(a, w, wq0 + rl)) * HD + c * 4,
+                         ld16(so + rl * 2 * S::ROWB + ((c ^ (rl & SWF)) * 16)));
+            }
+        }
+    } else {
+        // the four waves' sums, each relative to its own maximum, joined through LDS
+        constexpr int OLD = HD + 4;
+        float* const so = reinterpret_cast<float*>(smem);
+        float2* const sml = reinterpret_cast<float2*>(so + 4 * 16 * OLD);
+        static_assert((4 * 16 * OLD + 4 * 16 * 2) * 4 <= C::LDSB, "join fits the stages");
+#pragma unroll
+        for (int h = 0; h < C::NREAL; ++h) {
+            const int cidx = h * 16 + grp * 4;
+            if (cidx < HD) {
+                float v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = oacc[0][h][r];
+                store4<float>(so + (wave * 16 + l16) * OLD + cidx, v);
+            }
+        }
+        if (grp == 0) sml[wave * 16 + l16] = make_float2(m_run[0] * cs, l[0]);
+        __syncthreads();
+        const int s = tid / 16, slot = w.q0 + s;
+        if (slot >= w.slots) return;
+        float m = -INFINITY, f[4], sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) m = fmaxf(m, sml[v * 16 + s].x);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const float2 ml = sml[v * 16 + s];
+            f[v] = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
+            sum += f[v] * ml.y;
+        }
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        const long row = slot_row(a, w, slot);
+        for (int c = (tid % 16) * 4; c < HD; c += 64) {
+            float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float4 x = *reinterpret_cast<const float4*>(so + (v * 16 + s) * OLD + c);
+                o[0] += f[v] * x.x; o[1] += f[v] * x.y; o[2] += f[v] * x.z; o[3] += f[v] * x.w;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] *= inv;
+            if (a.nsplit == 1) store4<bf16_t>(static_cast<bf16_t*>(a.o) + row * HD + c, o);
+            else store4<float>(a.part_o + (range + row) * HD + c, o);
+        }
+        if (a.nsplit > 1 && tid % 16 == 0)
+            *reinterpret_cast<float2*>(a.part_ml + 2 * (range + row)) = make_float2(m, sum);
+    }
+}
 
 // One wave per (row, query head): lane = key of a 64-key tile for the scores,
 // lane = column for the weighted sum.
@@ -95,15 +655,75 @@ __global__ __launch_bounds__(kWave) void attend_row_kernel(Kv8AttnDesc a) {
     }
 }
 
+// Join of the key ranges, in range order: range s has the weight
+// l_s 2^(m_s - m); rows of no segment are left alone, rows of no key get 0. One
+// thread per four columns.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void join_kernel(Kv8AttnDesc a) {
+    const int HG = a.c.heads * a.group, per_row = HG * a.c.hd / 4;
+    const int lo = min(max(a.seg_start[0], 0), a.M), hi = min(max(a.seg_start[a.nseg], 0), a.M);
+    const long i = (long)blockIdx.x * kThreads + threadIdx.x + (long)lo * per_row;
+    const long plane = (long)a.M * HG;
+    if (i >= (long)hi * per_row) return;
+    const long sr = i * 4 / a.c.hd;            // (row, head)
+    float m = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, a.part_ml[2 * (s * plane + sr)]);
+    for (int s = 0; s < a.nsplit; ++s) {
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (s * plane + sr));
+        const float4 po = *reinterpret_cast<const float4*>(a.part_o + s * plane * a.c.hd + i * 4);
+        const float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m) * ml.y;
+        L += f;
+        acc[0] += f * po.x; acc[1] += f * po.y; acc[2] += f * po.z; acc[3] += f * po.w;
+    }
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[r] *= inv;
+    store4<T>(static_cast<T*>(a.o) + i * 4, acc);
+}
+
+// Few query slots per segment: the form whose waves have key tiles of their own.
+bool few_slots(int M, int nseg, int group) { return (long)M * group <= 32l * nseg; }
+
+template <bool SHARED>
+void launch_bf16(const Kv8AttnDesc& a, hipStream_t s) {
+    const int QT = SHARED ? 128 : 16;
+    const int qtiles = (int)std::min<long>((long)a.M * a.group / QT + a.nseg, (long)a.M * a.group);
+    const dim3 grid((unsigned)qtiles * a.nsplit * a.c.heads), block(kThreads);
+    switch (a.c.hd) {
+#define MS_HD(n) case n: hipLaunchKernelGGL((attend_bf16_kernel<n, SHARED>), grid, block, 0, s, a, qtiles); break;
+        MS_HD(8) MS_HD(16) MS_HD(24) MS_HD(32) MS_HD(40) MS_HD(48) MS_HD(56) MS_HD(64)
+        MS_HD(72) MS_HD(80) MS_HD(88) MS_HD(96) MS_HD(104) MS_HD(112) MS_HD(120) MS_HD(128)
+#undef MS_HD
+    }
+}
+
 }  // namespace
 
-int plan_kv8_attention(int dtype, int M, int nseg, int heads, int group, int hd, long keys) { return 1; }
+int plan_kv8_attention(int dtype, int M, int nseg, int heads, int group, int hd, long keys) {
+    if (dtype != kBF16 || M == 0) return 1;
+    const bool few = few_slots(M, nseg, group);
+    const int QT = few ? 16 : 128, KT = few ? 128 : 64;
+    const long base = ((long)M * group + QT - 1) / QT * heads;
+    const long tiles = (keys + KT - 1) / KT;
+    const long want = few ? (512 + base - 1) / base : (512 + base - 1) / base;
+    return (int)std::max<long>(1, std::min<long>({want, tiles, 64}));
+}
 
 hipError_t launch_kv8_attention(int dtype, const Kv8AttnDesc& a, hipStream_t s) {
     if (a.M == 0) return hipSuccess;
-    const dim3 grid(a.M, a.c.heads * a.group), block(kWave);
-    if (dtype == kBF16) hipLaunchKernelGGL(attend_row_kernel<bf16_t>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(attend_row_kernel<float>, grid, block, 0, s, a);
+    if (dtype == kBF16) {
+        if (few_slots(a.M, a.nseg, a.group)) launch_bf16<false>(a, s);
+        else launch_bf16<true>(a, s);
+    } else {
+        const dim3 grid(a.M, a.c.heads * a.group), block(kWave);
+        hipLaunchKernelGGL(attend_row_kernel<float>, grid, block, 0, s, a);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.nsplit == 1) return e;
+    const long n4 = (long)a.M * a.c.heads * a.group * a.c.hd / 4;
+    const dim3 grid((unsigned)((n4 + kThreads - 1) / kThreads)), block(kThreads);
+    if (dtype == kBF16) hipLaunchKernelGGL(join_kernel<bf16_t>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(join_kernel<float>, grid, block, 0, s, a);
     return hipGetLastError();
 }
 

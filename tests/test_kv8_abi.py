@@ -39,6 +39,7 @@ BAD_CACHE = [
     (dict(dtype=MS.MS_FP32, head_dim=72), MS.MS_ESHAPE),
     (dict(block=0), MS.MS_ESHAPE), (dict(block=24), MS.MS_ESHAPE), (dict(block=256), MS.MS_ESHAPE), (dict(block=-16), MS.MS_ESHAPE),
     (dict(tokens=1 << 20, n_kv_heads=32), MS.MS_ESHAPE),          # 2^20 x 2 x 32 x 64 = 2^32 bytes
+    (dict(tokens=4095 << 7, n_kv_heads=32, head_dim=128), MS.MS_ESHAPE),   # 4095 MiB
     (dict(codes=None), MS.MS_EINVAL), (dict(scales=None), MS.MS_EINVAL), (dict(codes=P + 8), MS.MS_EALIGN),
 ]
 BAD_SELECT = [
@@ -48,6 +49,7 @@ BAD_SELECT = [
 ]
 BAD_ATTN = [
     (dict(rows=-1), MS.MS_ESHAPE), (dict(rows=(1 << 26) + 1), MS.MS_ESHAPE),
+    (dict(rows=(1 << 25) + 1), MS.MS_ESHAPE),                        # x 8 heads above 2^28
     (dict(n_heads=0), MS.MS_ESHAPE), (dict(n_heads=6), MS.MS_ESHAPE), (dict(n_heads=2048), MS.MS_ESHAPE),
     (dict(n_seg=0), MS.MS_ESHAPE), (dict(n_seg=129, seg_req=P), MS.MS_ESHAPE), (dict(n_seg=3), MS.MS_ESHAPE),
     (dict(q=None), MS.MS_EINVAL), (dict(out=None), MS.MS_EINVAL), (dict(seg_start=None), MS.MS_EINVAL),
