@@ -86,7 +86,7 @@ ms_status check_attn(const ms_kv8_cache* c, const ms_kv8_select* sel, const ms_k
         if (!a->fresh_start) return set_error(MS_EINVAL, "fresh rows need fresh_start");
         if (a->fresh_rows < 0 || a->fresh_rows > (1 << 30)) return set_error(MS_ESHAPE, "fresh_rows outside 0..2^30");
         entries = a->fresh_list ? a->fresh_entries : a->fresh_rows;
-        if (entries < 0 || entries > (1 << 30)) return set_error(MS_ESHAPE, "fresh_entries outside 0..2^30");
+        if (entries < 0 || entries > (1 << 28)) return set_error(MS_ESHAPE, "fresh rows or entries outside 0..2^28");
     }
     d->q = a->q;
     d->o = a->out;

@@ -42,15 +42,32 @@ struct Work {
 // Slot tile `tile` of all segments, K/V head and key range; false: past the last tile.
 template <int QT, int KT>
 __device__ __forceinline__ bool find_work(const Kv8AttnDesc& a, int tile, int kvh, int split, Work& w) {
-    int seg = 0, r0 = 0, r1 = 0;
-    for (; seg < a.nseg; ++seg) {
-        r0 = min(max(a.seg_start[seg], 0), a.M);
-        r1 = min(max(a.seg_start[seg + 1], r0), a.M);
-        const int nt = ((r1 - r0) * a.group + QT - 1) / QT;
-        if (tile < nt) break;
-        tile -= nt;
+    // lane l looks at segments l and l + 64 at once
+    const int lane = threadIdx.x % kWave;
+    int seg = -1, r0 = 0, r1 = 0;
+    for (int s0 = 0; s0 < a.nseg && seg < 0; s0 += kWave) {
+        const int s = min(s0 + lane, a.nseg - 1);
+        const int b0 = min(max(a.seg_start[s], 0), a.M);
+        const int b1 = min(max(a.seg_start[s + 1], b0), a.M);
+        const int own = s0 + lane < a.nseg ? ((b1 - b0) * a.group + QT - 1) / QT : 0;
+        int upto = own;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int v = __shfl_up(upto, o, kWave);
+            if (lane >= o) upto += v;
+        }
+        const uint64_t past = __ballot(upto > tile);
+        if (past) {
+            const int at = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
+            seg = s0 + at;
+            r0 = __builtin_amdgcn_readlane(b0, at);
+            r1 = __builtin_amdgcn_readlane(b1, at);
+            tile -= __builtin_amdgcn_readlane(upto - own, at);
+        } else {
+            tile -= __builtin_amdgcn_readlane(upto, kWave - 1);
+        }
     }
-    if (seg >= a.nseg) return false;
+    if (seg < 0) return false;
     w.row0 = r0;
     w.slots = (r1 - r0) * a.group;
     w.q0 = tile * QT;
@@ -63,7 +80,7 @@ __device__ __forceinline__ bool find_work(const Kv8AttnDesc& a, int tile, int kv
         kv8_fresh(a, b, w.r);
     }
     w.ntc = (w.r.nk + KT - 1) / KT;
-    const long nt = w.ntc + (w.r.nf + KT - 1) / KT;
+    const uint32_t nt = w.ntc + (w.r.nf + KT - 1) / KT;   // at most 2^25 + 2^15; times 64 ranges below 2^32
     w.t0 = (int)(nt * split / a.nsplit);
     w.t1 = (int)(nt * (split + 1) / a.nsplit);
     return true;
@@ -77,83 +94,95 @@ __device__ __forceinline__ long slot_row(const Kv8AttnDesc& a, const Work& w, in
     return (long)(w.row0 + r) * HG + w.kvh * a.group + (slot - r * a.group);
 }
 
-// Staging of KT-key tiles by NT threads, each 1/NT of the chunks of CW elements.
-template <int HD, int KT, int NT>
+// Staging of KT-key tiles by NT threads, of the listed cached tokens or (FRESH)
+// of the fresh rows. A thread keeps one chunk column of CW elements and takes the
+// rows r0, r0 + RS, ... of the K rows followed by the V rows, so that its
+// addresses differ by constants. Loads are unconditional (absent keys load
+// nothing or a row that is then zeroed) and their results untouched until the
+// next step, so that no branch or use makes a wave wait for what it has just
+// issued.
+template <int HD, int KT, int NT, bool FRESH>
 struct Stager {
     static constexpr int CW = HD % 16 == 0 ? 16 : 8;
     static constexpr int CR = HD / CW;                  // chunks per row
-    static constexpr int NCHUNK = KT * 2 * CR;
-    static constexpr int NCH = (NCHUNK + NT - 1) / NT;
+    static constexpr int RS = NT / CR;                  // rows per pass
+    static constexpr int NCH = (2 * KT + RS - 1) / RS;  // passes
+    static constexpr int NV = FRESH ? CW / 8 : 1;       // 16-byte loads per chunk
     static constexpr int ROWB = HD * 2;
     static constexpr int TILEB = KT * ROWB;
-    static constexpr int KPAD = 16;                     // zeros past the K tile, read by padding slots of the last QK step
+    static constexpr int KPAD = 32;                     // zeros past the K tile, read by padding slots of the last QK step
     static constexpr int STAGEB = 2 * TILEB + KPAD;
+    static constexpr bool SWZ = ROWB == 128 || ROWB == 256 || ROWB % 128 == 64;
+    static constexpr int gcd16(int x) { return x % 16 == 0 ? 16 : x % 8 == 0 ? 8 : x % 4 == 0 ? 4 : x % 2 == 0 ? 2 : 1; }
+    static constexpr int PER = SWZ ? 16 / gcd16(RS) : 1;    // the swizzles repeat every 16 rows
+    static constexpr int ND = PER < NCH ? PER : NCH;
     static constexpr uint32_t kAbsent = 0xfff00000u;    // row offset past every cache's end
 
-    __amdgpu_buffer_rsrc_t rsrc;
-    int tid, lane;
+    __amdgpu_buffer_rsrc_t rsrc, rscale, rlist;
+    int lane, r0;
+    int count;              // keys of this kind
+    bool listed;            // whether rlist holds their numbers
     uint32_t row_bytes;     // of a token's codes
-    int rl[NCH];            // tile key of each chunk
-    uint32_t coloff[NCH];   // its first element within a token's row
-    uint32_t dst[NCH];      // LDS offset of its first 16 bytes in a stage; the second 16 at ^ 16 unless swizzled
-    uint32_t dst2[CW == 16 ? NCH : 1];
-    vec16 raw[NCH][CW / 8];
-    uint32_t sb = 0;        // this lane's key: scale bytes, K in bits 0-7, V in 8-15
-    uint32_t sk = 0, sv = 0;
-    int idx = -1;           // token number (row of the fresh K/V) of this lane's key in the next tile to issue
-    uint64_t valid = 0;     // present keys of the tile in raw
+    uint32_t kcol, vcol;    // first element of this thread's K and V chunks within a token's row
+    uint32_t dk[ND], dv[ND];// LDS offsets of the chunk of row r0 + i RS within a stage, less i RS rows
+    vec16 raw[NCH][NV];
+    uint32_t sk, sv;        // this lane's key: its scales' exponent bytes
+    int num;                // list entry of this lane's key in the next tile to issue
+    uint64_t valid;         // present keys of the tile in raw
 
-    __device__ __forceinline__ void init(const Kv8AttnDesc& a, const Work& w, int tid_) {
-        tid = tid_;
+    // pass i's row among the V rows: compile-time where no pass straddles the border
+    __device__ __forceinline__ bool in_v(int i) const {
+        if (i * RS >= KT) return true;
+        if ((i + 1) * RS <= KT) return false;
+        return r0 + i * RS >= KT;
+    }
+    __device__ __forceinline__ bool in_tile(int i) const { return (NT % CR == 0 && (i + 1) * RS <= 2 * KT) || r0 + i * RS < 2 * KT; }
+    // tile key of pass i (any lane number past the tile's end)
+    __device__ __forceinline__ int key(int i) const { return r0 + i * RS - (in_v(i) ? KT : 0); }
+
+    __device__ __forceinline__ void init(const Kv8AttnDesc& a, const Work& w, int tid) {
         lane = threadIdx.x % kWave;
         const int dkv = a.c.heads * HD;
         row_bytes = 2 * dkv;
-        rsrc = make_rsrc(w.r.codes, w.r.codes ? (uint32_t)a.c.T * row_bytes : 0u);
+        count = FRESH ? w.r.nf : w.r.nk;
+        const int32_t* const l = FRESH ? (a.f_rows ? a.f_rows + w.r.f0 : nullptr) : w.r.keys;
+        listed = l != nullptr;
+        rlist = make_rsrc(l, listed ? (uint32_t)count * 4u : 0u);
+        if constexpr (!FRESH) {
+            rsrc = make_rsrc(w.r.codes, (uint32_t)a.c.T * row_bytes);
+            rscale = make_rsrc(w.r.scales, (uint32_t)a.c.blocks * 2u * a.c.heads);
+        }
+        r0 = tid / CR;
+        const int col = tid % CR;
+        if (r0 >= RS) r0 = 2 * KT;      // NT % CR threads have no chunk
+        kcol = w.kvh * HD + col * CW;
+        vcol = kcol + dkv;
 #pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            const int q = min(i * NT + tid, NCHUNK - 1);
-            const bool isv = q >= KT * CR;
-            const int r = (q / CR) % KT, c = (q % CR) * (CW / 8);
-            rl[i] = r;
-            coloff[i] = (isv ? dkv : 0) + w.kvh * HD + c * 8;
-            const int sw = isv ? v_swz<ROWB>(r) : k_swz<ROWB>(r);
-            const uint32_t base = (isv ? TILEB + KPAD : 0) + r * ROWB;
-            dst[i] = base + (c ^ sw) * 16;
-            if constexpr (CW == 16) dst2[i] = base + ((c + 1) ^ sw) * 16;
+        for (int i = 0; i < ND; ++i) {
+            const int r = r0 + i * RS;
+            dk[i] = r0 * ROWB + (((col * (CW / 8)) ^ k_swz<ROWB>(r % 16)) * 16);
+            dv[i] = r0 * ROWB + (((col * (CW / 8)) ^ v_swz<ROWB>((r + 2 * KT - KT) % 16)) * 16) + KPAD;
         }
     }
-    // number of this lane's key of tile t
-    __device__ __forceinline__ void fetch_index(const Kv8AttnDesc& a, const Work& w, int t) {
-        idx = -1;
-        if (t >= w.t1 || lane >= KT) return;
-        if (t < w.ntc) {
-            const int i = t * KT + lane;
-            if (i < w.r.nk) {
-                idx = w.r.keys ? w.r.keys[i] : i;
-                if (idx >= a.c.T) idx = -1;
-            }
-        } else {
-            const int i = (t - w.ntc) * KT + lane;
-            if (i < w.r.nf) {
-                idx = a.f_rows ? a.f_rows[w.r.f0 + i] : w.r.f0 + i;
-                if (idx >= a.kv_rows) idx = -1;
-            }
-        }
+    // reads the list entry of this lane's key of tile t
+    __device__ __forceinline__ void fetch_index(int t) {
+        num = (int)__builtin_amdgcn_raw_buffer_load_b32(rlist, (t * KT + lane) * 4, 0, 0);   // past the end: 0
     }
-    // starts the loads of tile t, whose numbers fetch_index has read
-    __device__ __forceinline__ void issue(const Kv8AttnDesc& a, const Work& w, int t) {
-        valid = __ballot(idx >= 0);
-        if (t < w.ntc) {
-            const uint32_t off = idx >= 0 ? (uint32_t)idx * row_bytes : kAbsent;
-            sk = sv = 0;
-            if (idx >= 0) {
-                const uint8_t* sp = w.r.scales + (long)(idx >> a.c.lblock) * 2 * a.c.heads + w.kvh;
-                sk = sp[0];
-                sv = sp[a.c.heads];
-            }
+    // starts the loads of tile t, whose numbers fetch_index has read; past the last tile of the range (`end`) every key is absent
+    __device__ __forceinline__ void issue(const Kv8AttnDesc& a, const Work& w, int t, int end) {
+        const int i = t * KT + lane;
+        const int v = listed ? num : (FRESH ? w.r.f0 : 0) + i;
+        const bool there = t < end && lane < KT && i < count && v >= 0 && (FRESH ? v < a.kv_rows : v < a.c.T);
+        valid = __ballot(there);
+        const int row = there ? v : 0;
+        if constexpr (!FRESH) {
+            const uint32_t off = there ? (uint32_t)v * row_bytes : kAbsent;
+            const int so = (row >> a.c.lblock) * (2 * a.c.heads) + w.kvh;
+            sk = __builtin_amdgcn_raw_buffer_load_b8(rscale, so, 0, 0);
+            sv = __builtin_amdgcn_raw_buffer_load_b8(rscale, so, a.c.heads, 0);
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
-                const uint32_t o = (uint32_t)__shfl((int)off, rl[i], kWave) + coloff[i];
+                const uint32_t o = (uint32_t)__shfl((int)off, key(i), kWave) + (in_v(i) ? vcol : kcol);
                 if constexpr (CW == 16) {
                     raw[i][0] = buf_ld16(rsrc, o, 0);
                 } else {
@@ -163,25 +192,24 @@ struct Stager {
                 }
             }
         } else {
-            const int safe = max(idx, 0);
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
-                const long row = __shfl(safe, rl[i], kWave);
-                const bf16_t* p = static_cast<const bf16_t*>(a.kv) + row * row_bytes + coloff[i];
+                const long from = __shfl(row, key(i), kWave);
+                const bf16_t* p = static_cast<const bf16_t*>(a.kv) + from * row_bytes + (in_v(i) ? vcol : kcol);
 #pragma unroll
-                for (int j = 0; j < CW / 8; ++j) raw[i][j] = ld16(p + 8 * j);
+                for (int j = 0; j < NV; ++j) raw[i][j] = ld16(p + 8 * j);
             }
         }
     }
     // the tile in raw, as bf16, to the stage at smem
-    __device__ __forceinline__ void store(const Work& w, int t, uint8_t* smem) {
-        if (t < w.ntc) {
+    __device__ __forceinline__ void store(uint8_t* smem) {
+        if constexpr (!FRESH) {
             // the two scales as the upper halves of their float32 values
             const uint32_t both = (__float_as_uint(kv8_scale(sk)) >> 16) | __float_as_uint(kv8_scale(sv));
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
-                const uint32_t pr = (uint32_t)__shfl((int)both, rl[i], kWave);
-                const float s = __uint_as_float(i * NT + tid >= KT * CR ? pr & 0xffff0000u : pr << 16);
+                const uint32_t pr = (uint32_t)__shfl((int)both, key(i), kWave);
+                const float s = __uint_as_float(in_v(i) ? pr & 0xffff0000u : pr << 16);
                 vec16 o[CW / 8];
 #pragma unroll
                 for (int j = 0; j < CW / 8; ++j) {
@@ -193,25 +221,23 @@ struct Stager {
                 put(i, o, smem);
             }
         } else {
-            const uint64_t all = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
+                const bool there = (valid >> (key(i) & 63)) & 1;
                 vec16 o[CW / 8];
 #pragma unroll
-                for (int j = 0; j < CW / 8; ++j) o[j] = raw[i][j];
-                if (valid != all && !((valid >> rl[i]) & 1)) {
+                for (int j = 0; j < CW / 8; ++j)
 #pragma unroll
-                    for (int j = 0; j < CW / 8; ++j) o[j] = vec16{{0u, 0u, 0u, 0u}};
-                }
+                    for (int k = 0; k < 4; ++k) o[j].w[k] = there ? raw[i][j].w[k] : 0u;
                 put(i, o, smem);
             }
         }
     }
     __device__ __forceinline__ void put(int i, const vec16 (&o)[CW / 8], uint8_t* smem) {
-        if (NCHUNK % NT == 0 || i * NT + tid < NCHUNK) {
-            st16(smem + dst[i], o[0]);
-            if constexpr (CW == 16) st16(smem + dst2[i], o[1]);
-        }
+        if (!in_tile(i)) return;
+        const uint32_t at = in_v(i) ? dv[i % ND] : dk[i % ND];
+        st16(smem + at + i * RS * ROWB, o[0]);
+        if constexpr (CW == 16) st16(smem + (at ^ 16) + i * RS * ROWB, o[1]);
     }
 };
 
@@ -225,7 +251,8 @@ struct Bf16Cfg {
     static constexpr int QT = SHARED ? 128 : 16;
     static constexpr int NT = SHARED ? kThreads : kWave;
     static constexpr int STAGES = SHARED ? 2 : 1;
-    using S = Stager<HD, KT, NT>;
+    using S = Stager<HD, KT, NT, false>;
+    using F = Stager<HD, KT, NT, true>;
     static constexpr int NKS = KT / 16;
     static constexpr int NK32 = (HD + 31) / 32;
     static constexpr bool KTAIL = HD % 32 != 0;
@@ -236,7 +263,7 @@ struct Bf16Cfg {
 };
 
 template <int HD, bool SHARED>
-__global__ __launch_bounds__(kThreads, SHARED ? (HD <= 48 ? 4 : HD <= 64 ? 3 : 2) : 2) void attend_bf16_kernel(Kv8AttnDesc a, int qtiles) {
+__global__ __launch_bounds__(kThreads, SHARED ? (HD <= 24 ? 4 : HD <= 64 ? 3 : 2) : HD <= 64 ? 4 : 2) void attend_bf16_kernel(Kv8AttnDesc a, int qtiles) {
     using C = Bf16Cfg<HD, SHARED>;
     using S = typename C::S;
     constexpr int NQB = C::NQB, NKS = C::NKS;
@@ -244,7 +271,7 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 48 ? 4 : HD <= 64 ? 3 : 2
     const uint32_t lds0 = lds_addr(smem);
     const uint32_t ones_rel = C::LDSB;                  // 8 bytes of bf16 ones (SUM_IN_PAD)
 
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int grp = lane / 16, l16 = lane % 16;
     // SHARED: a head's slot tiles side by side, so that an XCD's L2 serves a head's codes to
     // all of them; else a tile's heads side by side, which read neighbouring parts of the rows
@@ -256,16 +283,12 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 48 ? 4 : HD <= 64 ? 3 : 2
     } else {
         if (!find_work<C::QT, C::KT>(a, lb / (a.nsplit * a.c.heads), lb % a.c.heads, lb / a.c.heads % a.nsplit, w)) return;
     }
-    const int first = SHARED ? w.t0 : w.t0 + wave, step = SHARED ? 1 : 4;
+    constexpr int step = SHARED ? 1 : 4;
 
     // constant LDS: the K pads' zeros and the ones block
     constexpr int NSTG = SHARED ? C::STAGES : 4;
-    if (tid < NSTG) *reinterpret_cast<uint4*>(smem + tid * S::STAGEB + S::TILEB) = make_uint4(0u, 0u, 0u, 0u);
-    if (tid == NSTG) *reinterpret_cast<uint2*>(smem + C::LDSB) = make_uint2(0x3f803f80u, 0x3f803f80u);
-
-    S st;
-    st.init(a, w, SHARED ? tid : lane);
-    st.fetch_index(a, w, first);
+    if (tid < 2 * NSTG) *reinterpret_cast<uint4*>(smem + (tid / 2) * S::STAGEB + S::TILEB + (tid % 2) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == 2 * NSTG) *reinterpret_cast<uint2*>(smem + C::LDSB) = make_uint2(0x3f803f80u, 0x3f803f80u);
 
     // Q^T fragments (B operand), their sign that of the score scale
     bf16x8_t qf[NQB][C::NK32];
@@ -355,7 +378,7 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 48 ? 4 : HD <= 64 ? 3 : 2
     };
     // online softmax in place: sacc becomes the weights; running maxima and accumulators
     // updated, a rescale only where a score exceeds its slot's maximum by more than 2^8
-    auto softmax = [&](f32x4_t (&sacc)[NQB][NKS], bool first_tile) {
+    auto softmax = [&](f32x4_t (&sacc)[NQB][NKS]) {
         float mx[NQB];
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb) {
@@ -375,11 +398,9 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 48 ? 4 : HD <= 64 ? 3 : 2
                 const float was = none ? -INFINITY : m_run[qb] + negm[qb][0];
                 const float up = fmaxf(rm, was);
                 const bool still = up == -INFINITY;
-                if (!first_tile) {
-                    const float corr = none ? 0.f : fast_exp2((was - up) * cs);
+                const float corr = none ? 0.f : fast_exp2((was - up) * cs);
 #pragma unroll
-                    for (int h = 0; h < C::NHS; ++h) oacc[qb][h] *= corr;
-                }
+                for (int h = 0; h < C::NHS; ++h) oacc[qb][h] *= corr;
                 m_run[qb] = fmaxf(m_run[qb], rm - negm[qb][0]);
                 const float n = m_run[qb] == -INFINITY ? 0.f : -fminf(fmaxf(m_run[qb], -kStartMax), kStartMax);
                 negm[qb] = f32x4_t{n, n, n, n};
@@ -440,29 +461,56 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 48 ? 4 : HD <= 64 ? 3 : 2
 
     f32x4_t sa[NQB][NKS];
     const bool active = wq0 < w.slots;
-    __syncthreads();   // constant LDS
-    if (first < w.t1) {
-        st.issue(a, w, first);
-        st.fetch_index(a, w, first + step);
-    }
-    int n = 0;
-    for (int t = first; t < w.t1; t += step, ++n) {
-        const uint32_t sbase = SHARED ? (n & 1) * S::STAGEB : wave * S::STAGEB;
-        const uint64_t present = st.valid;
-        st.store(w, t, smem + sbase);
-        if (t + step < w.t1) {
-            st.issue(a, w, t + step);
-            st.fetch_index(a, w, t + 2 * step);
+    // Tiles [from, to) of one kind: tile t is in LDS, tile t + step in registers or on its way
+    // there while t is multiplied; its conversion stands between the two products, under the
+    // matrix instructions.
+    auto run = [&](auto st, int from, int to) {
+        if constexpr (!SHARED) from += wave;
+        if (from >= to) return;   // the whole workgroup, or a wave that waits for no other
+        st.init(a, w, SHARED ? tid : lane);
+        auto stage = [&](int n) { return (uint32_t)(SHARED ? (n & 1) * S::STAGEB : wave * S::STAGEB); };
+        st.fetch_index(from);
+        st.issue(a, w, from, to);
+        st.fetch_index(from + step);
+        uint64_t present = st.valid;
+        st.store(smem + stage(0));
+        st.issue(a, w, from + step, to);
+        st.fetch_index(from + 2 * step);
+        int n = 0;
+        for (int t = from; t < to; t += step, ++n) {
+            wait_lds();
+            if constexpr (SHARED) barrier_only();
+            else __builtin_amdgcn_wave_barrier();
+            const uint64_t now = present;
+            auto next = [&]() {
+                present = st.valid;
+                st.store(smem + stage(n + 1));
+                st.issue(a, w, t + 2 * step, to);
+                st.fetch_index(t + 3 * step);
+            };
+            if constexpr (SHARED) {
+                if (active) qk(stage(n), now, sa);
+                next();
+                if (active) {
+                    softmax(sa);
+                    pv(stage(n), sa);
+                }
+            } else {
+                qk(stage(n), now, sa);
+                softmax(sa);
+                pv(stage(n), sa);
+                asm volatile("" ::: "memory");
+                next();
+            }
         }
-        wait_lds();
-        if constexpr (SHARED) barrier_only();
-        else __builtin_amdgcn_wave_barrier();
-        if (!active) continue;
-        qk(sbase, present, sa);
-        softmax(sa, n == 0);
-        pv(sbase, sa);
-        if constexpr (!SHARED) asm volatile("" ::: "memory");
-    }
+        if constexpr (SHARED) {
+            wait_lds();
+            barrier_only();   // the stages may be written again
+        }
+    };
+    __syncthreads();   // constant LDS
+    run(typename C::S{}, min(w.t0, w.ntc), min(w.t1, w.ntc));
+    if (w.r.nf > 0) run(typename C::F{}, max(w.t0 - w.ntc, 0), max(w.t1 - w.ntc, 0));
 
     float l[NQB];
 #pragma unroll
@@ -655,30 +703,44 @@ __global__ __launch_bounds__(kWave) void attend_row_kernel(Kv8AttnDesc a) {
     }
 }
 
-// Join of the key ranges, in range order: range s has the weight
-// l_s 2^(m_s - m); rows of no segment are left alone, rows of no key get 0. One
-// thread per four columns.
+// Join of the key ranges: range s has the weight l_s 2^(m_s - m); rows of no
+// segment are left alone, rows of no key get 0. One wave per (row, head): lane s
+// holds range s's maximum and sum, then hd / 4 lanes take four columns each and as
+// many groups of them as the wave holds take the ranges in turn, so that a row
+// costs two rounds of loads however many ranges there are.
+constexpr int kMaxRanges = 64;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void join_kernel(Kv8AttnDesc a) {
-    const int HG = a.c.heads * a.group, per_row = HG * a.c.hd / 4;
+    const int HG = a.c.heads * a.group, hd = a.c.hd, lane = threadIdx.x % kWave;
     const int lo = min(max(a.seg_start[0], 0), a.M), hi = min(max(a.seg_start[a.nseg], 0), a.M);
-    const long i = (long)blockIdx.x * kThreads + threadIdx.x + (long)lo * per_row;
     const long plane = (long)a.M * HG;
-    if (i >= (long)hi * per_row) return;
-    const long sr = i * 4 / a.c.hd;            // (row, head)
-    float m = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, a.part_ml[2 * (s * plane + sr)]);
-    for (int s = 0; s < a.nsplit; ++s) {
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (s * plane + sr));
-        const float4 po = *reinterpret_cast<const float4*>(a.part_o + s * plane * a.c.hd + i * 4);
-        const float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m) * ml.y;
-        L += f;
-        acc[0] += f * po.x; acc[1] += f * po.y; acc[2] += f * po.z; acc[3] += f * po.w;
-    }
+    const long sr = (long)lo * HG + (long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;   // (row, head)
+    if (sr >= (long)hi * HG) return;
+    const int CL = hd / 4, groups = kWave / CL, grp = lane / CL, col = lane % CL;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < a.nsplit) ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (lane * plane + sr));
+    const float m = wave_max(ml.x);
+    const float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m) * ml.y;
+    const float L = wave_sum(f);
     const float inv = L == 0.f ? 0.f : 1.0f / L;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    const float* const po = a.part_o + sr * hd + col * 4;
+#pragma unroll 8
+    for (int s0 = 0; s0 < a.nsplit; s0 += groups) {
+        const int s = s0 + grp;
+        const float fs = __shfl(f, s, kWave);
+        if (grp < groups && s < a.nsplit) {
+            const float4 p = *reinterpret_cast<const float4*>(po + s * plane * hd);
+            acc[0] += fs * p.x; acc[1] += fs * p.y; acc[2] += fs * p.z; acc[3] += fs * p.w;
+        }
+    }
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < groups; ++g)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) acc[r] *= inv;
-    store4<T>(static_cast<T*>(a.o) + i * 4, acc);
+        for (int r = 0; r < 4; ++r) o[r] += __shfl(acc[r], (g * CL + col) % kWave, kWave);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] *= inv;
+    if (lane < CL) store4<T>(static_cast<T*>(a.o) + sr * hd + col * 4, o);
 }
 
 // Few query slots per segment: the form whose waves have key tiles of their own.
@@ -701,12 +763,13 @@ void launch_bf16(const Kv8AttnDesc& a, hipStream_t s) {
 
 int plan_kv8_attention(int dtype, int M, int nseg, int heads, int group, int hd, long keys) {
     if (dtype != kBF16 || M == 0) return 1;
+    if (getenv("KV8_NS")) return atoi(getenv("KV8_NS"));
     const bool few = few_slots(M, nseg, group);
     const int QT = few ? 16 : 128, KT = few ? 128 : 64;
     const long base = ((long)M * group + QT - 1) / QT * heads;
     const long tiles = (keys + KT - 1) / KT;
     const long want = few ? (512 + base - 1) / base : (512 + base - 1) / base;
-    return (int)std::max<long>(1, std::min<long>({want, tiles, 64}));
+    return (int)std::max<long>(1, std::min<long>({want, tiles, kMaxRanges}));
 }
 
 hipError_t launch_kv8_attention(int dtype, const Kv8AttnDesc& a, hipStream_t s) {
@@ -720,8 +783,8 @@ hipError_t launch_kv8_attention(int dtype, const Kv8AttnDesc& a, hipStream_t s) 
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.nsplit == 1) return e;
-    const long n4 = (long)a.M * a.c.heads * a.group * a.c.hd / 4;
-    const dim3 grid((unsigned)((n4 + kThreads - 1) / kThreads)), block(kThreads);
+    const long n = (long)a.M * a.c.heads * a.group;
+    const dim3 grid((unsigned)((n + kThreads / kWave - 1) / (kThreads / kWave))), block(kThreads);
     if (dtype == kBF16) hipLaunchKernelGGL(join_kernel<bf16_t>, grid, block, 0, s, a);
     else hipLaunchKernelGGL(join_kernel<float>, grid, block, 0, s, a);
     return hipGetLastError();
