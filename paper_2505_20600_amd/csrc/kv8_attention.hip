@@ -103,11 +103,11 @@ __device__ __forceinline__ long slot_row(const Kv8AttnDesc& a, const Work& w, in
 // issued.
 template <int HD, int KT, int NT, bool FRESH>
 struct Stager {
-    static constexpr int CW = HD % 16 == 0 ? 16 : 8;
+    static constexpr int CW = HD % 16 == 0 ? 16 : HD % 24 == 0 ? 24 : 8;
     static constexpr int CR = HD / CW;                  // chunks per row
     static constexpr int RS = NT / CR;                  // rows per pass
     static constexpr int NCH = (2 * KT + RS - 1) / RS;  // passes
-    static constexpr int NV = FRESH ? CW / 8 : 1;       // 16-byte loads per chunk
+    static constexpr int NV = FRESH ? CW / 8 : (CW + 15) / 16;   // 16-byte loads per chunk (the last of 24 codes: 8 bytes)
     static constexpr int ROWB = HD * 2;
     static constexpr int TILEB = KT * ROWB;
     static constexpr int KPAD = 32;                     // zeros past the K tile, read by padding slots of the last QK step
@@ -183,12 +183,11 @@ struct Stager {
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
                 const uint32_t o = (uint32_t)__shfl((int)off, key(i), kWave) + (in_v(i) ? vcol : kcol);
-                if constexpr (CW == 16) {
-                    raw[i][0] = buf_ld16(rsrc, o, 0);
-                } else {
-                    const auto v = __builtin_amdgcn_raw_buffer_load_b64(rsrc, (int)o, 0, 0);
-                    raw[i][0].w[0] = v[0];
-                    raw[i][0].w[1] = v[1];
+                if constexpr (CW >= 16) raw[i][0] = buf_ld16(rsrc, o, 0);
+                if constexpr (CW % 16 == 8) {
+                    const auto v = __builtin_amdgcn_raw_buffer_load_b64(rsrc, (int)(o + CW - 8), 0, 0);
+                    raw[i][NV - 1].w[0] = v[0];
+                    raw[i][NV - 1].w[1] = v[1];
                 }
             }
         } else {
@@ -213,10 +212,11 @@ struct Stager {
                 vec16 o[CW / 8];
 #pragma unroll
                 for (int j = 0; j < CW / 8; ++j) {
-                    o[j].w[0] = kv8_to_bf16x2<false>(raw[i][0].w[2 * j], s);
-                    o[j].w[1] = kv8_to_bf16x2<true>(raw[i][0].w[2 * j], s);
-                    o[j].w[2] = kv8_to_bf16x2<false>(raw[i][0].w[2 * j + 1], s);
-                    o[j].w[3] = kv8_to_bf16x2<true>(raw[i][0].w[2 * j + 1], s);
+                    const uint32_t c0 = raw[i][j / 2].w[2 * (j % 2)], c1 = raw[i][j / 2].w[2 * (j % 2) + 1];
+                    o[j].w[0] = kv8_to_bf16x2<false>(c0, s);
+                    o[j].w[1] = kv8_to_bf16x2<true>(c0, s);
+                    o[j].w[2] = kv8_to_bf16x2<false>(c1, s);
+                    o[j].w[3] = kv8_to_bf16x2<true>(c1, s);
                 }
                 put(i, o, smem);
             }
@@ -238,6 +238,10 @@ struct Stager {
         const uint32_t at = in_v(i) ? dv[i % ND] : dk[i % ND];
         st16(smem + at + i * RS * ROWB, o[0]);
         if constexpr (CW == 16) st16(smem + (at ^ 16) + i * RS * ROWB, o[1]);
+        if constexpr (CW == 24) {   // rows without a swizzle
+            st16(smem + at + i * RS * ROWB + 16, o[1]);
+            st16(smem + at + i * RS * ROWB + 32, o[2]);
+        }
     }
 };
 
@@ -274,14 +278,16 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 24 ? 4 : HD <= 64 ? 3 : 2
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int grp = lane / 16, l16 = lane % 16;
     // SHARED: a head's slot tiles side by side, so that an XCD's L2 serves a head's codes to
-    // all of them; else a tile's heads side by side, which read neighbouring parts of the rows
-    const int total = qtiles * a.nsplit * a.c.heads;
-    const int lb = xcd_logical_block(blockIdx.x, total);
+    // all of them. Else the heads of a (tile, range) pair side by side, which read neighbouring
+    // parts of the same rows, and the pairs dealt out to the XCDs in turn: the tiles that no
+    // segment fills come last and would leave whole XCDs idle in a contiguous split.
     Work w;
     if constexpr (SHARED) {
+        const int lb = xcd_logical_block(blockIdx.x, qtiles * a.nsplit * a.c.heads);
         if (!find_work<C::QT, C::KT>(a, lb % qtiles, lb / (qtiles * a.nsplit), lb / qtiles % a.nsplit, w)) return;
     } else {
-        if (!find_work<C::QT, C::KT>(a, lb / (a.nsplit * a.c.heads), lb % a.c.heads, lb / a.c.heads % a.nsplit, w)) return;
+        const int i = blockIdx.x / kXcds, pair = i / a.c.heads * kXcds + blockIdx.x % kXcds;
+        if (!find_work<C::QT, C::KT>(a, pair / a.nsplit, i % a.c.heads, pair % a.nsplit, w)) return;
     }
     constexpr int step = SHARED ? 1 : 4;
 
@@ -464,8 +470,8 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 24 ? 4 : HD <= 64 ? 3 : 2
     // Tiles [from, to) of one kind: tile t is in LDS, tile t + step in registers or on its way
     // there while t is multiplied; its conversion stands between the two products, under the
     // matrix instructions.
-    auto run = [&](auto st, int from, int to) {
-        if constexpr (!SHARED) from += wave;
+    auto run = [&](auto st, int from, int to, int skip) {
+        if constexpr (!SHARED) from += (wave - skip) & 3;   // the waves go on in turn from one kind to the next
         if (from >= to) return;   // the whole workgroup, or a wave that waits for no other
         st.init(a, w, SHARED ? tid : lane);
         auto stage = [&](int n) { return (uint32_t)(SHARED ? (n & 1) * S::STAGEB : wave * S::STAGEB); };
@@ -509,8 +515,9 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 24 ? 4 : HD <= 64 ? 3 : 2
         }
     };
     __syncthreads();   // constant LDS
-    run(typename C::S{}, min(w.t0, w.ntc), min(w.t1, w.ntc));
-    if (w.r.nf > 0) run(typename C::F{}, max(w.t0 - w.ntc, 0), max(w.t1 - w.ntc, 0));
+    const int c0 = min(w.t0, w.ntc), c1 = min(w.t1, w.ntc);
+    run(typename C::S{}, c0, c1, 0);
+    if (w.r.nf > 0) run(typename C::F{}, max(w.t0 - w.ntc, 0), max(w.t1 - w.ntc, 0), c1 - c0);
 
     float l[NQB];
 #pragma unroll
@@ -750,7 +757,8 @@ template <bool SHARED>
 void launch_bf16(const Kv8AttnDesc& a, hipStream_t s) {
     const int QT = SHARED ? 128 : 16;
     const int qtiles = (int)std::min<long>((long)a.M * a.group / QT + a.nseg, (long)a.M * a.group);
-    const dim3 grid((unsigned)qtiles * a.nsplit * a.c.heads), block(kThreads);
+    const int pairs = qtiles * a.nsplit;
+    const dim3 grid((unsigned)(SHARED ? pairs : (pairs + kXcds - 1) / kXcds * kXcds) * a.c.heads), block(kThreads);
     switch (a.c.hd) {
 #define MS_HD(n) case n: hipLaunchKernelGGL((attend_bf16_kernel<n, SHARED>), grid, block, 0, s, a, qtiles); break;
         MS_HD(8) MS_HD(16) MS_HD(24) MS_HD(32) MS_HD(40) MS_HD(48) MS_HD(56) MS_HD(64)
