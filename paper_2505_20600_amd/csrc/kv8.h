@@ -104,16 +104,24 @@ struct Kv8Req {
     int f0, nf;     // fresh list entries [f0, f0 + nf)
 };
 
-__device__ __forceinline__ Kv8Req kv8_request(const Kv8Cache& c, const Kv8Select& sel, int b) {
+// `codes`, `scales`: the request's cache numbers (0 where it has none).
+__device__ __forceinline__ Kv8Req kv8_request(const Kv8Cache& c, const Kv8Select& sel, int b, int& codes, int& scales) {
     Kv8Req r{nullptr, nullptr, nullptr, 0, 0, 0};
     const int cc = sel.codes_of ? sel.codes_of[b] : b;
     const int sc = sel.scales_of ? sel.scales_of[b] : b;
-    if (cc < 0 || cc >= c.n_caches || sc < 0 || sc >= c.n_scales) return r;
-    r.codes = c.codes + (long)cc * c.T * 2 * c.heads * c.hd;
-    r.scales = c.scales + (long)sc * c.blocks * 2 * c.heads;
+    const int n = sel.n_keys ? min(max(sel.n_keys[b], 0), sel.ld_keys) : sel.ld_keys;
+    const bool known = cc >= 0 && cc < c.n_caches && sc >= 0 && sc < c.n_scales;
+    codes = known ? cc : 0;
+    scales = known ? sc : 0;
+    r.codes = c.codes + (long)codes * c.T * 2 * c.heads * c.hd;
+    r.scales = c.scales + (long)scales * c.blocks * 2 * c.heads;
     r.keys = sel.keys ? sel.keys + (long)b * sel.ld_keys : nullptr;
-    r.nk = sel.n_keys ? min(max(sel.n_keys[b], 0), sel.ld_keys) : sel.ld_keys;
+    r.nk = known ? n : 0;
     return r;
+}
+__device__ __forceinline__ Kv8Req kv8_request(const Kv8Cache& c, const Kv8Select& sel, int b) {
+    int cc, sc;
+    return kv8_request(c, sel, b, cc, sc);
 }
 
 __device__ __forceinline__ void kv8_fresh(const Kv8AttnDesc& a, int b, Kv8Req& r) {

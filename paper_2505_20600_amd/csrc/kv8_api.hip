@@ -84,7 +84,9 @@ ms_status check_attn(const ms_kv8_cache* c, const ms_kv8_select* sel, const ms_k
     long entries = 0;
     if (a->fresh) {
         if (!a->fresh_start) return set_error(MS_EINVAL, "fresh rows need fresh_start");
-        if (a->fresh_rows < 0 || a->fresh_rows > (1 << 30)) return set_error(MS_ESHAPE, "fresh_rows outside 0..2^30");
+        const int64_t row = 2ll * c->n_kv_heads * c->head_dim * (c->dtype == MS_BF16 ? 2 : 4);
+        if (a->fresh_rows < 0 || a->fresh_rows > (1 << 28) || a->fresh_rows * row >= (1ll << 32) - (1 << 20))
+            return set_error(MS_ESHAPE, "fresh_rows %lld: the rows must stay below 4095 MiB", (long long)a->fresh_rows);
         entries = a->fresh_list ? a->fresh_entries : a->fresh_rows;
         if (entries < 0 || entries > (1 << 28)) return set_error(MS_ESHAPE, "fresh rows or entries outside 0..2^28");
     }

@@ -27,6 +27,8 @@ constexpr int kThreads = 256;
 // LDS operations of the wave done (vector-memory loads may stay in flight).
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }
 
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // Which query slots and key tiles a workgroup has.
 struct Work {
     int row0;       // first packed row of the segment
@@ -42,14 +44,24 @@ struct Work {
 // Slot tile `tile` of all segments, K/V head and key range; false: past the last tile.
 template <int QT, int KT>
 __device__ __forceinline__ bool find_work(const Kv8AttnDesc& a, int tile, int kvh, int split, Work& w) {
-    // lane l looks at segments l and l + 64 at once
+    // lane l reads what belongs to segment l (then l + 64), all at once
     const int lane = threadIdx.x % kWave;
-    int seg = -1, r0 = 0, r1 = 0;
-    for (int s0 = 0; s0 < a.nseg && seg < 0; s0 += kWave) {
+    for (int s0 = 0; s0 < a.nseg; s0 += kWave) {
         const int s = min(s0 + lane, a.nseg - 1);
-        const int b0 = min(max(a.seg_start[s], 0), a.M);
-        const int b1 = min(max(a.seg_start[s + 1], b0), a.M);
-        const int own = s0 + lane < a.nseg ? ((b1 - b0) * a.group + QT - 1) / QT : 0;
+        const int b = a.seg_req ? a.seg_req[s] : s;
+        const bool known = b >= 0 && b < a.sel.batch;
+        const int bs = known ? b : 0;
+        const int r0 = min(max(a.seg_start[s], 0), a.M), r1 = min(max(a.seg_start[s + 1], r0), a.M);
+        int cc, sc, f0 = 0, nf = 0;
+        int nk = kv8_request(a.c, a.sel, bs, cc, sc).nk;
+        if (a.kv) {
+            Kv8Req f{};
+            kv8_fresh(a, bs, f);
+            f0 = f.f0;
+            nf = f.nf;
+        }
+        if (!known) nk = nf = 0;
+        const int own = s0 + lane < a.nseg ? ((r1 - r0) * a.group + QT - 1) / QT : 0;
         int upto = own;
 #pragma unroll
         for (int o = 1; o < kWave; o <<= 1) {
@@ -57,33 +69,30 @@ __device__ __forceinline__ bool find_work(const Kv8AttnDesc& a, int tile, int kv
             if (lane >= o) upto += v;
         }
         const uint64_t past = __ballot(upto > tile);
-        if (past) {
-            const int at = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
-            seg = s0 + at;
-            r0 = __builtin_amdgcn_readlane(b0, at);
-            r1 = __builtin_amdgcn_readlane(b1, at);
-            tile -= __builtin_amdgcn_readlane(upto - own, at);
-        } else {
+        if (!past) {
             tile -= __builtin_amdgcn_readlane(upto, kWave - 1);
+            continue;
         }
+        const int at = uniform(__ffsll((unsigned long long)past) - 1);
+        auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+        w.row0 = of(r0);
+        w.slots = (of(r1) - w.row0) * a.group;
+        w.q0 = (tile - of(upto - own)) * QT;
+        w.kvh = kvh;
+        w.split = split;
+        w.r.nk = of(nk);
+        w.r.f0 = of(f0);
+        w.r.nf = of(nf);
+        w.r.codes = a.c.codes + (long)of(cc) * a.c.T * 2 * a.c.heads * a.c.hd;
+        w.r.scales = a.c.scales + (long)of(sc) * a.c.blocks * 2 * a.c.heads;
+        w.r.keys = a.sel.keys ? a.sel.keys + (long)of(bs) * a.sel.ld_keys : nullptr;
+        w.ntc = (w.r.nk + KT - 1) / KT;
+        const uint32_t nt = w.ntc + (w.r.nf + KT - 1) / KT;   // below 2^24; times 64 ranges below 2^32
+        w.t0 = (int)(nt * split / a.nsplit);
+        w.t1 = (int)(nt * (split + 1) / a.nsplit);
+        return true;
     }
-    if (seg < 0) return false;
-    w.row0 = r0;
-    w.slots = (r1 - r0) * a.group;
-    w.q0 = tile * QT;
-    w.kvh = kvh;
-    w.split = split;
-    const int b = a.seg_req ? a.seg_req[seg] : seg;
-    w.r = Kv8Req{nullptr, nullptr, nullptr, 0, 0, 0};
-    if (b >= 0 && b < a.sel.batch) {
-        w.r = kv8_request(a.c, a.sel, b);
-        kv8_fresh(a, b, w.r);
-    }
-    w.ntc = (w.r.nk + KT - 1) / KT;
-    const uint32_t nt = w.ntc + (w.r.nf + KT - 1) / KT;   // at most 2^25 + 2^15; times 64 ranges below 2^32
-    w.t0 = (int)(nt * split / a.nsplit);
-    w.t1 = (int)(nt * (split + 1) / a.nsplit);
-    return true;
+    return false;
 }
 
 // Row index of a query slot's (row, query head) in [M][n_heads].
@@ -111,7 +120,8 @@ struct Stager {
     static constexpr int ROWB = HD * 2;
     static constexpr int TILEB = KT * ROWB;
     static constexpr int KPAD = 32;                     // zeros past the K tile, read by padding slots of the last QK step
-    static constexpr int STAGEB = 2 * TILEB + KPAD;
+    static constexpr int TRASH = 2 * TILEB + KPAD;      // 64 bytes past the tiles, never read
+    static constexpr int STAGEB = TRASH + 64;
     static constexpr bool SWZ = ROWB == 128 || ROWB == 256 || ROWB % 128 == 64;
     static constexpr int gcd16(int x) { return x % 16 == 0 ? 16 : x % 8 == 0 ? 8 : x % 4 == 0 ? 4 : x % 2 == 0 ? 2 : 1; }
     static constexpr int PER = SWZ ? 16 / gcd16(RS) : 1;    // the swizzles repeat every 16 rows
@@ -233,14 +243,71 @@ struct Stager {
             }
         }
     }
+    // a thread without a row in this pass writes past the stage's tiles instead of branching
     __device__ __forceinline__ void put(int i, const vec16 (&o)[CW / 8], uint8_t* smem) {
-        if (!in_tile(i)) return;
-        const uint32_t at = in_v(i) ? dv[i % ND] : dk[i % ND];
-        st16(smem + at + i * RS * ROWB, o[0]);
-        if constexpr (CW == 16) st16(smem + (at ^ 16) + i * RS * ROWB, o[1]);
+        const uint32_t d = in_v(i) ? dv[i % ND] : dk[i % ND], there = in_tile(i);
+        const uint32_t at = there ? d + i * RS * ROWB : TRASH;
+        st16(smem + at, o[0]);
+        if constexpr (CW == 16) st16(smem + (at ^ 16), o[1]);
         if constexpr (CW == 24) {   // rows without a swizzle
-            st16(smem + at + i * RS * ROWB + 16, o[1]);
-            st16(smem + at + i * RS * ROWB + 32, o[2]);
+            st16(smem + at + 16, o[1]);
+            st16(smem + at + 32, o[2]);
+        }
+    }
+};
+
+// Staging of the fresh rows' 64-key tiles by the four waves of a workgroup with
+// direct-to-LDS loads: they need no conversion. Absent keys' rows read as zeros.
+template <int HD, int KT, typename S>
+struct FreshDma {
+    static constexpr int ROWB = HD * 2, TILEB = KT * ROWB;
+    static constexpr int INSTR = TILEB / 1024;          // 1 KB copies per tile
+    static constexpr int NQ = 2 * INSTR;                // K then V
+    static constexpr int IPW = (NQ + 3) / 4;            // copies per wave (most)
+    static_assert(TILEB % 1024 == 0, "tile copies");
+    u32x4_t rsrc;
+    __amdgpu_buffer_rsrc_t rlist;
+    int lane, wave, count, f0;
+    bool listed;
+    uint32_t row_bytes;
+    int rl[IPW];
+    uint32_t col[IPW], dst[IPW];
+    int num;
+    uint64_t valid;
+
+    __device__ __forceinline__ void init(const Kv8AttnDesc& a, const Work& w, int wave_, int lane_) {
+        lane = lane_;
+        wave = wave_;
+        count = w.r.nf;
+        f0 = w.r.f0;
+        const int32_t* const l = a.f_rows ? a.f_rows + f0 : nullptr;
+        listed = l != nullptr;
+        rlist = make_rsrc(l, listed ? (uint32_t)count * 4u : 0u);
+        row_bytes = 4u * a.c.heads * HD;
+        rsrc = raw_rsrc(a.kv, (uint32_t)a.kv_rows * row_bytes);
+#pragma unroll
+        for (int i = 0; i < IPW; ++i) {
+            const int q = min(i * 4 + wave, NQ - 1);
+            const bool isv = q >= INSTR;
+            const int pos = (q % INSTR) * 1024 + lane * 16, r = pos / ROWB;
+            rl[i] = r;
+            col[i] = (isv ? row_bytes / 2 : 0u) + w.kvh * ROWB + (((pos % ROWB) / 16) ^ (isv ? v_swz<ROWB>(r) : k_swz<ROWB>(r))) * 16;
+            dst[i] = uniform((isv ? TILEB + S::KPAD : 0) + (q % INSTR) * 1024);
+        }
+    }
+    __device__ __forceinline__ void fetch_index(int t) {
+        num = (int)__builtin_amdgcn_raw_buffer_load_b32(rlist, (t * KT + lane) * 4, 0, 0);   // past the end: 0
+    }
+    // tile t into the stage at LDS address `lds`
+    __device__ __forceinline__ void issue(const Kv8AttnDesc& a, int t, int end, uint32_t lds) {
+        const int i = t * KT + lane, v = listed ? num : f0 + i;
+        const bool there = t < end && i < count && v >= 0 && v < a.kv_rows;
+        valid = __ballot(there);
+        const uint32_t off = there ? (uint32_t)v * row_bytes : S::kAbsent;
+#pragma unroll
+        for (int i = 0; i < IPW; ++i) {
+            const uint32_t o = (uint32_t)__shfl((int)off, rl[i], kWave) + col[i];
+            if (i * 4 + wave < NQ) dma_buf16(rsrc, o, 0, lds + dst[i]);
         }
     }
 };
@@ -267,7 +334,7 @@ struct Bf16Cfg {
 };
 
 template <int HD, bool SHARED>
-__global__ __launch_bounds__(kThreads, SHARED ? (HD <= 24 ? 4 : HD <= 64 ? 3 : 2) : HD <= 64 ? 4 : 2) void attend_bf16_kernel(Kv8AttnDesc a, int qtiles) {
+__global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2) : HD <= 48 || HD == 64 ? 4 : HD <= 80 ? 3 : 2) void attend_bf16_kernel(Kv8AttnDesc a, int qtiles) {
     using C = Bf16Cfg<HD, SHARED>;
     using S = typename C::S;
     constexpr int NQB = C::NQB, NKS = C::NKS;
@@ -275,7 +342,7 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 24 ? 4 : HD <= 64 ? 3 : 2
     const uint32_t lds0 = lds_addr(smem);
     const uint32_t ones_rel = C::LDSB;                  // 8 bytes of bf16 ones (SUM_IN_PAD)
 
-    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave);
     const int grp = lane / 16, l16 = lane % 16;
     // SHARED: a head's slot tiles side by side, so that an XCD's L2 serves a head's codes to
     // all of them. Else the heads of a (tile, range) pair side by side, which read neighbouring
@@ -514,10 +581,36 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 24 ? 4 : HD <= 64 ? 3 : 2
             barrier_only();   // the stages may be written again
         }
     };
+    // the same of the fresh rows in the SHARED form: their loads land in LDS
+    auto run_dma = [&](int from, int to) {
+        if (from >= to) return;
+        FreshDma<HD, 64, S> st;
+        st.init(a, w, wave, lane);
+        st.fetch_index(from);
+        st.issue(a, from, to, lds0);
+        st.fetch_index(from + 1);
+        for (int t = from, n = 0; t < to; ++t, ++n) {
+            const uint64_t now = st.valid;
+            wait_all();   // tile t has landed, and this wave's reads of the stage refilled below are done
+            barrier_only();
+            if (t + 1 < to) {
+                st.issue(a, t + 1, to, lds0 + ((n + 1) & 1) * S::STAGEB);
+                st.fetch_index(t + 2);
+            }
+            if (!active) continue;
+            qk((n & 1) * S::STAGEB, now, sa);
+            softmax(sa);
+            pv((n & 1) * S::STAGEB, sa);
+        }
+    };
     __syncthreads();   // constant LDS
     const int c0 = min(w.t0, w.ntc), c1 = min(w.t1, w.ntc);
     run(typename C::S{}, c0, c1, 0);
-    if (w.r.nf > 0) run(typename C::F{}, max(w.t0 - w.ntc, 0), max(w.t1 - w.ntc, 0), c1 - c0);
+    if (w.r.nf > 0) {
+        const int f0 = max(w.t0 - w.ntc, 0), f1 = max(w.t1 - w.ntc, 0);
+        if constexpr (SHARED) run_dma(f0, f1);
+        else run(typename C::F{}, f0, f1, c1 - c0);
+    }
 
     float l[NQB];
 #pragma unroll
