@@ -141,8 +141,8 @@ hipError_t launch_kv8_quantize(int dtype, const Kv8Cache& c, const void* kv, lon
 // kv[b * row_stride + t] = the listed tokens' values.
 hipError_t launch_kv8_dequantize(int dtype, const Kv8Cache& c, const Kv8Select& sel, void* kv, long row_stride,
                                  hipStream_t s);
-// Key ranges of an attention call of M rows in nseg segments over at most `keys` keys per request.
-int plan_kv8_attention(int dtype, int M, int nseg, int heads, int group, int hd, long keys);
+// Key ranges that an attention call is best divided into (from its sizes; its tables are not read).
+int plan_kv8_attention(int dtype, const Kv8AttnDesc& a);
 hipError_t launch_kv8_attention(int dtype, const Kv8AttnDesc& a, hipStream_t s);
 
 }  // namespace ms

@@ -113,12 +113,6 @@ size_t range_floats(const ms::Kv8AttnDesc& d) {
     return (size_t)d.M * d.c.heads * d.group * (d.c.hd + 2);
 }
 
-int wanted_ranges(int dtype, const ms::Kv8AttnDesc& d) {
-    // the fresh rows of a batch are about as many per request
-    const long keys = d.sel.ld_keys + (d.f_list + d.sel.batch - 1) / d.sel.batch;
-    return ms::plan_kv8_attention(dtype, d.M, d.nseg, d.c.heads, d.group, d.c.hd, keys);
-}
-
 }  // namespace
 
 extern "C" {
@@ -176,7 +170,7 @@ size_t ms_kv8_attention_workspace_bytes(const ms_kv8_cache* c, const ms_kv8_sele
     ms::Kv8AttnDesc d;
     if (check_attn(c, sel, a, &d) != MS_OK) return 0;
     ms::clear_error();
-    const int n = wanted_ranges(c->dtype, d);
+    const int n = ms::plan_kv8_attention(c->dtype, d);
     return n > 1 ? n * range_floats(d) * sizeof(float) : 0;
 }
 
@@ -189,7 +183,7 @@ ms_status ms_kv8_attention(const ms_kv8_cache* c, const ms_kv8_select* sel, cons
     if (!aligned(d_ws, 16)) return set_error(MS_EALIGN, "workspace not 16-byte aligned");
     if (d.M == 0) return ms::clear_error();
     const size_t one = range_floats(d) * sizeof(float);
-    d.nsplit = std::max(1, std::min<int>(wanted_ranges(c->dtype, d), d_ws ? (int)std::min<size_t>(ws_bytes / one, 1024) : 1));
+    d.nsplit = std::max(1, std::min<int>(ms::plan_kv8_attention(c->dtype, d), d_ws ? (int)std::min<size_t>(ws_bytes / one, 1024) : 1));
     if (d.nsplit > 1) {
         d.part_o = static_cast<float*>(d_ws);
         d.part_ml = d.part_o + (size_t)d.nsplit * d.M * d.c.heads * d.group * d.c.hd;

@@ -312,6 +312,38 @@ struct FreshDma {
     }
 };
 
+// The four waves' sums of 16 slots, each relative to its own maximum (so [wave][slot][OLD]
+// and sml [wave][slot]), to the output or the key range's part.
+template <typename T, int HD, int OLD>
+__device__ __forceinline__ void join_waves(const Kv8AttnDesc& a, const Work& w, const float* so, const float2* sml, int tid) {
+    const int s = tid / 16, slot = w.q0 + s;
+    if (slot >= w.slots) return;
+    float m = -INFINITY, f[4], sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) m = fmaxf(m, sml[v * 16 + s].x);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const float2 ml = sml[v * 16 + s];
+        f[v] = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
+        sum += f[v] * ml.y;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    const long row = slot_row(a, w, slot), part = (long)w.split * a.M * a.c.heads * a.group + row;
+    for (int c = (tid % 16) * 4; c < HD; c += 64) {
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const float4 x = *reinterpret_cast<const float4*>(so + (v * 16 + s) * OLD + c);
+            o[0] += f[v] * x.x; o[1] += f[v] * x.y; o[2] += f[v] * x.z; o[3] += f[v] * x.w;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] *= inv;
+        if (a.nsplit == 1) store4<T>(static_cast<T*>(a.o) + row * HD + c, o);
+        else store4<float>(a.part_o + part * HD + c, o);
+    }
+    if (a.nsplit > 1 && tid % 16 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * part) = make_float2(m, sum);
+}
+
 // bf16. SHARED: 128 query slots, 32 per wave, the four waves share 64-key tiles
 // in two stages. Not SHARED: 16 slots, every wave has key tiles of its own (32
 // keys, tile t0 + wave + 4 i) and the four partial results are joined at the end.
@@ -421,7 +453,7 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
     const bf16x8_t onesf = __builtin_bit_cast(bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
     constexpr uint64_t kAll = C::KT == 64 ? ~0ull : (1ull << (C::KT % 64)) - 1;
 
-    auto qk = [&](uint32_t sbase, uint64_t present, f32x4_t (&sacc)[NQB][NKS]) {
+    auto qk = [&](uint32_t sbase, f32x4_t (&sacc)[NQB][NKS]) {
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb)
 #pragma unroll
@@ -437,6 +469,8 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
                 for (int qb = 0; qb < NQB; ++qb) sacc[qb][ks] = mfma32(kf, qf[qb][kc], sacc[qb][ks]);
             }
         }
+    };
+    auto drop_absent = [&](uint64_t present, f32x4_t (&sacc)[NQB][NKS]) {
         if (present != kAll) {
             const uint64_t mine = present >> (grp * 4);
 #pragma unroll
@@ -537,7 +571,7 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
     // Tiles [from, to) of one kind: tile t is in LDS, tile t + step in registers or on its way
     // there while t is multiplied; its conversion stands between the two products, under the
     // matrix instructions.
-    auto run = [&](auto st, int from, int to, int skip) {
+    auto run = [&](auto st, int from, int to, int skip) __attribute__((always_inline)) {
         if constexpr (!SHARED) from += (wave - skip) & 3;   // the waves go on in turn from one kind to the next
         if (from >= to) return;   // the whole workgroup, or a wave that waits for no other
         st.init(a, w, SHARED ? tid : lane);
@@ -562,14 +596,18 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
                 st.fetch_index(t + 3 * step);
             };
             if constexpr (SHARED) {
-                if (active) qk(stage(n), now, sa);
-                next();
-                if (active) {
-                    softmax(sa);
-                    pv(stage(n), sa);
+                if (!active) {
+                    next();
+                    continue;
                 }
+                qk(stage(n), sa);
+                next();
+                drop_absent(now, sa);
+                softmax(sa);
+                pv(stage(n), sa);
             } else {
-                qk(stage(n), now, sa);
+                qk(stage(n), sa);
+                drop_absent(now, sa);
                 softmax(sa);
                 pv(stage(n), sa);
                 asm volatile("" ::: "memory");
@@ -598,7 +636,8 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
                 st.fetch_index(t + 2);
             }
             if (!active) continue;
-            qk((n & 1) * S::STAGEB, now, sa);
+            qk((n & 1) * S::STAGEB, sa);
+            drop_absent(now, sa);
             softmax(sa);
             pv((n & 1) * S::STAGEB, sa);
         }
@@ -687,120 +726,220 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
         }
         if (grp == 0) sml[wave * 16 + l16] = make_float2(m_run[0] * cs, l[0]);
         __syncthreads();
-        const int s = tid / 16, slot = w.q0 + s;
-        if (slot >= w.slots) return;
-        float m = -INFINITY, f[4], sum = 0.f;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) m = fmaxf(m, sml[v * 16 + s].x);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const float2 ml = sml[v * 16 + s];
-            f[v] = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
-            sum += f[v] * ml.y;
-        }
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        const long row = slot_row(a, w, slot);
-        for (int c = (tid % 16) * 4; c < HD; c += 64) {
-            float o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const float4 x = *reinterpret_cast<const float4*>(so + (v * 16 + s) * OLD + c);
-                o[0] += f[v] * x.x; o[1] += f[v] * x.y; o[2] += f[v] * x.z; o[3] += f[v] * x.w;
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] *= inv;
-            if (a.nsplit == 1) store4<bf16_t>(static_cast<bf16_t*>(a.o) + row * HD + c, o);
-            else store4<float>(a.part_o + (range + row) * HD + c, o);
-        }
-        if (a.nsplit > 1 && tid % 16 == 0)
-            *reinterpret_cast<float2*>(a.part_ml + 2 * (range + row)) = make_float2(m, sum);
+        join_waves<bf16_t, HD, OLD>(a, w, so, sml, tid);
     }
 }
 
-// One wave per (row, query head): lane = key of a 64-key tile for the scores,
-// lane = column for the weighted sum.
-template <typename T>
-__global__ __launch_bounds__(kWave) void attend_row_kernel(Kv8AttnDesc a) {
-    __shared__ float s_q[128], s_p[kWave], s_sc[kWave];
-    __shared__ int s_row[kWave];
-    const int lane = threadIdx.x, row = blockIdx.x, head = blockIdx.y;
-    const int hd = a.c.hd, H = a.c.heads, dkv = H * hd, d = dkv * a.group, g = head / a.group;
-    int seg = 0;
-    while (seg < a.nseg && !(row >= a.seg_start[seg] && row < a.seg_start[seg + 1])) ++seg;
-    if (seg == a.nseg) return;
-    const int b = a.seg_req ? a.seg_req[seg] : seg;
-    Kv8Req r{nullptr, nullptr, nullptr, 0, 0, 0};
-    if (b >= 0 && b < a.sel.batch) {
-        r = kv8_request(a.c, a.sel, b);
-        kv8_fresh(a, b, r);
-    }
-    for (int i = lane; i < hd; i += kWave) s_q[i] = Elt<T>::to_f32(static_cast<const T*>(a.q)[(long)row * d + head * hd + i]);
-    __syncthreads();
-    const T* const fresh = static_cast<const T*>(a.kv);
-    float m = -INFINITY, l = 0.f, o[2] = {0.f, 0.f};
-    const int total = r.nk + r.nf;
-    for (int k0 = 0; k0 < total; k0 += kWave) {
-        const int i = k0 + lane;
-        const bool cached = i < r.nk;
-        int t = -1;
-        float sv = 0.f, z = -INFINITY;
-        if (cached) {
-            t = r.keys ? r.keys[i] : i;
-            if (t < 0 || t >= a.c.T) t = -1;
-        } else if (i < total) {
-            t = a.f_rows ? a.f_rows[r.f0 + i - r.nk] : r.f0 + i - r.nk;
-            if (t < 0 || t >= a.kv_rows) t = -1;
+// float32: 16 query slots, every wave has 32-key tiles of its own, joined at the end, as in
+// the bf16 form for few slots. Bound by the float32 matrix instructions (HD of them per tile
+// and wave, 32 cycles each, against ~300 cycles of staging), so the same form serves many slots.
+template <int HD, bool FRESH>
+struct StagerF32 {
+    static constexpr int KT = 32;
+    static constexpr int CW = HD % 16 == 0 ? 16 : 8;
+    static constexpr int CR = HD / CW, RS = kWave / CR, NCH = (2 * KT + RS - 1) / RS;
+    static constexpr int NV = FRESH ? CW / 4 : 1;       // 16-byte loads per chunk
+    // words per row: 4 P = 16 or 48 mod 64 keeps the four rows that a transposed V read takes in different banks
+    static constexpr int P = HD + 4;
+    static constexpr int TRASH = 2 * KT * P;            // words past the K and V rows: spare chunks, reads past the last row
+    static constexpr int WORDS = TRASH + 16;
+    static constexpr uint32_t kAbsent = 0xfff00000u;
+
+    __amdgpu_buffer_rsrc_t rsrc, rscale, rlist;
+    int lane, r0, col, count;
+    bool listed;
+    uint32_t row_elts, kcol;    // elements of a token's K and V rows; first K element of this lane's chunk
+    vec16 raw[NCH][NV];
+    uint32_t sk, sv;
+    int num;
+    uint64_t valid;
+
+    __device__ __forceinline__ bool in_v(int i) const { return r0 + i * RS >= KT; }
+    __device__ __forceinline__ int key(int i) const { return r0 + i * RS - (in_v(i) ? KT : 0); }
+
+    __device__ __forceinline__ void init(const Kv8AttnDesc& a, const Work& w, int lane_) {
+        lane = lane_;
+        row_elts = 2 * a.c.heads * HD;
+        count = FRESH ? w.r.nf : w.r.nk;
+        const int32_t* const l = FRESH ? (a.f_rows ? a.f_rows + w.r.f0 : nullptr) : w.r.keys;
+        listed = l != nullptr;
+        rlist = make_rsrc(l, listed ? (uint32_t)count * 4u : 0u);
+        if constexpr (FRESH) {
+            rsrc = make_rsrc(a.kv, (uint32_t)a.kv_rows * row_elts * 4u);
+        } else {
+            rsrc = make_rsrc(w.r.codes, (uint32_t)a.c.T * row_elts);
+            rscale = make_rsrc(w.r.scales, (uint32_t)a.c.blocks * 2u * a.c.heads);
         }
-        if (t >= 0) {
-            float dot = 0.f;
-            if (cached) {
-                const uint8_t* sp = r.scales + (long)(t >> a.c.lblock) * 2 * H + g;
-                sv = kv8_scale(sp[H]);
-                const uint8_t* p = r.codes + (long)t * 2 * dkv + g * hd;
-                const float sk = kv8_scale(sp[0]);
-                for (int j = 0; j < hd; j += 2) {
-                    const float2 v = kv8_to_f32x2<false>(*reinterpret_cast<const uint16_t*>(p + j), sk);
-                    dot += s_q[j] * v.x + s_q[j + 1] * v.y;
-                }
+        r0 = lane / CR;
+        col = lane % CR;
+        if (r0 >= RS) r0 = 2 * KT;      // kWave % CR lanes have no chunk
+        kcol = w.kvh * HD + col * CW;
+    }
+    __device__ __forceinline__ void fetch_index(int t) {
+        num = (int)__builtin_amdgcn_raw_buffer_load_b32(rlist, (t * KT + lane) * 4, 0, 0);   // past the end: 0
+    }
+    __device__ __forceinline__ void issue(const Kv8AttnDesc& a, const Work& w, int t, int end) {
+        const int i = t * KT + lane;
+        const int v = listed ? num : (FRESH ? w.r.f0 : 0) + i;
+        const bool there = t < end && lane < KT && i < count && v >= 0 && (FRESH ? v < a.kv_rows : v < a.c.T);
+        valid = __ballot(there);
+        const uint32_t off = there ? (uint32_t)v * row_elts * (FRESH ? 4u : 1u) : kAbsent;   // absent rows read as zeros
+        if constexpr (!FRESH) {
+            const int so = ((there ? v : 0) >> a.c.lblock) * (2 * a.c.heads) + w.kvh;
+            sk = __builtin_amdgcn_raw_buffer_load_b8(rscale, so, 0, 0);
+            sv = __builtin_amdgcn_raw_buffer_load_b8(rscale, so, a.c.heads, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            const uint32_t e = kcol + (in_v(i) ? row_elts / 2 : 0u);
+            const uint32_t o = (uint32_t)__shfl((int)off, key(i), kWave) + e * (FRESH ? 4u : 1u);
+            if constexpr (FRESH) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j) raw[i][j] = buf_ld16(rsrc, o + 16 * j, 0);
+            } else if constexpr (CW == 16) {
+                raw[i][0] = buf_ld16(rsrc, o, 0);
             } else {
-                const T* p = fresh + (long)t * 2 * dkv + g * hd;
-                for (int j = 0; j < hd; ++j) dot += s_q[j] * Elt<T>::to_f32(p[j]);
+                const auto v = __builtin_amdgcn_raw_buffer_load_b64(rsrc, (int)o, 0, 0);
+                raw[i][0].w[0] = v[0];
+                raw[i][0].w[1] = v[1];
             }
-            z = dot * a.scale_log2;
         }
-        const float m_new = fmaxf(m, wave_max(z));
-        const float ref = m_new == -INFINITY ? 0.f : m_new;
-        const float corr = m == -INFINITY ? 0.f : fast_exp2(m - ref);
-        const float p = t >= 0 ? fast_exp2(z - ref) : 0.f;
-        l = l * corr + wave_sum(p);
-        m = m_new;
-        __syncthreads();
-        s_p[lane] = p;
-        s_sc[lane] = sv;
-        s_row[lane] = t;
-        __syncthreads();
-        for (int x = 0; x < 2; ++x) {
-            const int col = lane + x * kWave;
-            if (col >= hd) continue;
-            float acc = o[x] * corr;
-            for (int k = 0; k < kWave; ++k) {
-                if (s_row[k] < 0) continue;
-                float v;
-                if (k0 + k < r.nk) {
-                    v = kv8_to_f32x2<false>(r.codes[((long)s_row[k] * 2 + 1) * dkv + g * hd + col], s_sc[k]).x;
-                } else {
-                    v = Elt<T>::to_f32(fresh[((long)s_row[k] * 2 + 1) * dkv + g * hd + col]);
+    }
+    __device__ __forceinline__ void store(float* smem) {
+        uint32_t both = 0;
+        if constexpr (!FRESH) both = (__float_as_uint(kv8_scale(sk)) >> 16) | __float_as_uint(kv8_scale(sv));
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            const int r = r0 + i * RS;
+            float* const p = smem + (r < 2 * KT ? r * P + col * CW : TRASH);
+            if constexpr (FRESH) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j) st16(p + 4 * j, raw[i][j]);
+            } else {
+                const uint32_t pr = (uint32_t)__shfl((int)both, key(i), kWave);
+                const float s = __uint_as_float(in_v(i) ? pr & 0xffff0000u : pr << 16);
+#pragma unroll
+                for (int j = 0; j < CW / 4; ++j) {
+                    const float2 x = kv8_to_f32x2<false>(raw[i][0].w[j], s), y = kv8_to_f32x2<true>(raw[i][0].w[j], s);
+                    const float v[4] = {x.x, x.y, y.x, y.y};
+                    store4<float>(p + 4 * j, v);
                 }
-                acc += s_p[k] * v;
             }
-            o[x] = acc;
         }
     }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    for (int x = 0; x < 2; ++x) {
-        const int col = lane + x * kWave;
-        if (col < hd) static_cast<T*>(a.o)[(long)row * d + head * hd + col] = Elt<T>::from_f32(o[x] * inv);
+};
+
+template <int HD>
+__global__ __launch_bounds__(kThreads, 2) void attend_f32_kernel(Kv8AttnDesc a) {
+    using S = StagerF32<HD, false>;
+    constexpr int KT = S::KT, P = S::P, NJ = (HD + 15) / 16;
+    constexpr int OLD = NJ * 16 + 4;
+    constexpr int JOIN = 4 * 16 * OLD + 4 * 16 * 2;     // words of the waves' sums
+    __shared__ __attribute__((aligned(16))) float smem[4 * S::WORDS > JOIN ? 4 * S::WORDS : JOIN];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), grp = lane / 16, l16 = lane % 16;
+    const int i = blockIdx.x / kXcds, pair = i / a.c.heads * kXcds + blockIdx.x % kXcds;
+    Work w;
+    if (!find_work<16, KT>(a, pair / a.nsplit, i % a.c.heads, pair % a.nsplit, w)) return;
+    float* const sw = smem + wave * S::WORDS;
+
+    // Q^T operand: slot l16, head_dim 16 j + 4 grp + e for the instruction (j, e)
+    float qf[NJ][4];
+    const int slot = w.q0 + l16;
+    const float* const q = static_cast<const float*>(a.q) + slot_row(a, w, slot) * HD;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (slot < w.slots && j * 16 + grp * 4 < HD) load4<float>(q + j * 16 + grp * 4, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) qf[j][e] = v[e];
     }
+    f32x4_t oacc[NJ];
+#pragma unroll
+    for (int h = 0; h < NJ; ++h) oacc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, l_run = 0.f;
+
+    auto multiply = [&](uint64_t present) __attribute__((always_inline)) {
+        // S^T: keys 16 ks + 4 grp + r of slot l16, in the log2 domain
+        float sc[2][4];
+        float mx = -INFINITY;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                float k[4] = {0.f, 0.f, 0.f, 0.f};
+                if (HD % 16 == 0 || j + 1 < NJ || j * 16 + grp * 4 < HD) load4<float>(sw + (ks * 16 + l16) * P + j * 16 + grp * 4, k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc = Elt<float>::mma(k[e], qf[j][e], acc);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool there = (present >> (ks * 16 + grp * 4 + r)) & 1;
+                sc[ks][r] = there ? acc[r] * a.scale_log2 : -INFINITY;
+                mx = fmaxf(mx, sc[ks][r]);
+            }
+        }
+        const float m_new = fmaxf(m_run, rows_max(mx));
+        const float ref = m_new == -INFINITY ? 0.f : m_new;
+        const float corr = m_run == -INFINITY ? 0.f : fast_exp2(m_run - ref);
+        m_run = m_new;
+        l_run *= corr;
+#pragma unroll
+        for (int h = 0; h < NJ; ++h) oacc[h] *= corr;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                sc[ks][r] = fast_exp2(sc[ks][r] - ref);
+                l_run += sc[ks][r];
+            }
+        // O^T += V^T P^T; a last block of eight columns multiplies what lies behind the row too, into rows that are not used
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int h = 0; h < NJ; ++h)
+                    oacc[h] = Elt<float>::mma(sw[(KT + ks * 16 + grp * 4 + r) * P + h * 16 + l16], sc[ks][r], oacc[h]);
+    };
+    auto run = [&](auto st, int from, int to, int skip) __attribute__((always_inline)) {
+        from += (wave - skip) & 3;   // the waves go on in turn from one kind to the next
+        if (from >= to) return;
+        st.init(a, w, lane);
+        st.fetch_index(from);
+        st.issue(a, w, from, to);
+        st.fetch_index(from + 4);
+        uint64_t present = st.valid;
+        st.store(sw);
+        st.issue(a, w, from + 4, to);
+        st.fetch_index(from + 8);
+        for (int t = from; t < to; t += 4) {
+            wait_lds();
+            __builtin_amdgcn_wave_barrier();
+            multiply(present);
+            asm volatile("" ::: "memory");
+            present = st.valid;
+            st.store(sw);
+            st.issue(a, w, t + 8, to);
+            st.fetch_index(t + 12);
+        }
+    };
+    const int c0 = min(w.t0, w.ntc), c1 = min(w.t1, w.ntc);
+    run(S{}, c0, c1, 0);
+    if (w.r.nf > 0) run(StagerF32<HD, true>{}, max(w.t0 - w.ntc, 0), max(w.t1 - w.ntc, 0), c1 - c0);
+
+    const float l = rows_sum(l_run);
+    __syncthreads();
+    float* const so = smem;
+    float2* const sml = reinterpret_cast<float2*>(so + 4 * 16 * OLD);
+#pragma unroll
+    for (int h = 0; h < NJ; ++h) {
+        const float v[4] = {oacc[h][0], oacc[h][1], oacc[h][2], oacc[h][3]};
+        store4<float>(so + (wave * 16 + l16) * OLD + h * 16 + grp * 4, v);
+    }
+    if (grp == 0) sml[wave * 16 + l16] = make_float2(m_run, l);
+    __syncthreads();
+    join_waves<float, HD, OLD>(a, w, so, sml, tid);
 }
 
 // Join of the key ranges: range s has the weight l_s 2^(m_s - m); rows of no
@@ -843,8 +982,19 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Kv8AttnDesc a) {
     if (lane < CL) store4<T>(static_cast<T*>(a.o) + sr * hd + col * 4, o);
 }
 
-// Few query slots per segment: the form whose waves have key tiles of their own.
-bool few_slots(int M, int nseg, int group) { return (long)M * group <= 32l * nseg; }
+// Whether a bf16 call takes the form for few query slots, whose waves have key tiles of
+// their own: up to 16 slots per segment, up to 32 at short rows, or where all of it is one
+// or two rounds of workgroups. Few / many, 4096 keys: 8 requests of 16, 32, 48 rows of 16 heads
+// of 64 23 / 29, 33 / 33, 48 / 38 us; 4 x 32 rows of 24 heads of 128 47 / 37; 1 x 48, 64 rows
+// of 24 heads of 128 27 / 29, 32 / 28; 128 rows of 12 heads of 64 over 1024 keys 12 / 15.
+bool few_slots(const Kv8AttnDesc& a) {
+    const long rows = (long)a.M * a.group, segs = std::min(a.nseg, a.M), per = (rows + segs - 1) / segs;
+    const long keys = a.sel.ld_keys + a.f_list / a.sel.batch;
+    return per <= (a.c.hd < 96 ? 32 : 16) || segs * ((per + 15) / 16) * a.c.heads * keys <= 1l << 18;
+}
+
+// Workgroups of the SHARED form that the registers let a CU hold.
+constexpr int shared_per_cu(int hd) { return hd <= 16 ? 4 : hd <= 64 ? 3 : 2; }
 
 template <bool SHARED>
 void launch_bf16(const Kv8AttnDesc& a, hipStream_t s) {
@@ -860,27 +1010,63 @@ void launch_bf16(const Kv8AttnDesc& a, hipStream_t s) {
     }
 }
 
+void launch_f32(const Kv8AttnDesc& a, hipStream_t s) {
+    const int qtiles = (int)std::min<long>((long)a.M * a.group / 16 + a.nseg, (long)a.M * a.group);
+    const int pairs = qtiles * a.nsplit;
+    const dim3 grid((unsigned)(pairs + kXcds - 1) / kXcds * kXcds * a.c.heads), block(kThreads);
+    switch (a.c.hd) {
+#define MS_HD(n) case n: hipLaunchKernelGGL(attend_f32_kernel<n>, grid, block, 0, s, a); break;
+        MS_HD(8) MS_HD(16) MS_HD(24) MS_HD(32) MS_HD(40) MS_HD(48) MS_HD(56) MS_HD(64)
+#undef MS_HD
+    }
+}
+
 }  // namespace
 
-int plan_kv8_attention(int dtype, int M, int nseg, int heads, int group, int hd, long keys) {
-    if (dtype != kBF16 || M == 0) return 1;
-    if (getenv("KV8_NS")) return atoi(getenv("KV8_NS"));
-    const bool few = few_slots(M, nseg, group);
-    const int QT = few ? 16 : 128, KT = few ? 128 : 64;
-    const long base = ((long)M * group + QT - 1) / QT * heads;
-    const long tiles = (keys + KT - 1) / KT;
-    const long want = few ? (512 + base - 1) / base : (512 + base - 1) / base;
-    return (int)std::max<long>(1, std::min<long>({want, tiles, kMaxRanges}));
+// Key ranges. Few slots and float32: as many as give every CU two workgroups (one where rows
+// are long and a workgroup alone keeps its CU's loads in flight), of at least 256 keys (128
+// in float32): 8 requests of 16 rows over 4096 keys of 16 heads in 1 / 2 / 4 / 8 / 16 ranges
+// take 26 / 21 / 21 / 23 / 27 us at head_dim 64, 40 / 28 / 25 / 31 / 36 at 72 and 41 / 30 / 34
+// / 38 / 48 at 128; one row of 12 heads of 64 takes 25 us in one range and 9.7 in 16.
+// Many: the count with the least modelled time. Workgroups run in rounds of as many as the
+// registers let a CU hold; a round with k on a CU takes 7 us + 1.5 per further one to start
+// and end and, per 64-key tile, the tile's matrix instructions times (0.0165 + 0.008 k) us;
+// the join a launch and its parts at 5 TB/s.
+int plan_kv8_attention(int dtype, const Kv8AttnDesc& a) {
+    if (a.M == 0) return 1;
+    const int heads = a.c.heads, hd = a.c.hd;
+    const long rows = (long)a.M * a.group, segs = std::min(a.nseg, a.M), per = (rows + segs - 1) / segs;
+    const long keys = a.sel.ld_keys + a.f_list / a.sel.batch;   // fresh rows: about as many for each request
+    if (dtype != kBF16 || few_slots(a)) {
+        const long base = segs * ((per + 15) / 16) * heads, target = hd < 96 ? 512 : 256, least = dtype == kBF16 ? 256 : 128;
+        return (int)std::max<long>(1, std::min<long>({(target + base - 1) / base, (keys + least - 1) / least, kMaxRanges}));
+    }
+    const long base = segs * ((per + 127) / 128) * heads, tiles = (keys + 63) / 64;
+    const int per_cu = shared_per_cu(hd);
+    const double unit = 8 * ((hd + 31) / 32) + 4 * ((hd + 15) / 16 + (hd % 16 == 0));
+    int best = 1;
+    double least = 1e30;
+    for (int n = 1; n <= std::min<long>(tiles, kMaxRanges); ++n) {
+        const long groups = base * n, slots = 256l * per_cu, rest = groups % slots;
+        auto round_us = [&](long k) { return (tiles + n - 1) / n * unit * (0.0165 + 0.008 * k) + 7.0 + 1.5 * (k - 1); };
+        double us = (double)(groups / slots) * round_us(per_cu);
+        if (rest) us += round_us((rest + 255) / 256);
+        if (n > 1) us += 3.0 + (4.0 * n + 2) * rows * heads * hd / 5.0e6;
+        if (us < least) {
+            least = us;
+            best = n;
+        }
+    }
+    return best;
 }
 
 hipError_t launch_kv8_attention(int dtype, const Kv8AttnDesc& a, hipStream_t s) {
     if (a.M == 0) return hipSuccess;
     if (dtype == kBF16) {
-        if (few_slots(a.M, a.nseg, a.group)) launch_bf16<false>(a, s);
+        if (few_slots(a)) launch_bf16<false>(a, s);
         else launch_bf16<true>(a, s);
     } else {
-        const dim3 grid(a.M, a.c.heads * a.group), block(kWave);
-        hipLaunchKernelGGL(attend_row_kernel<float>, grid, block, 0, s, a);
+        launch_f32(a, s);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.nsplit == 1) return e;
