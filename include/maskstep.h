@@ -365,6 +365,44 @@ ms_status mask_stack_forward(ms_step* step, const ms_layer_weights* w, const voi
                              const void* d_ycache, const ms_kv_source* kv, void* d_y,
                              void* compute_stream, void* copy_stream);
 
+/* A K/V cache in 8 bits (maskstep_ops.h describes the format and writes it:
+ * ms_kv8_quantize over the image tokens' rows) for mask_stack_forward_kv8.
+ *  MS_KV_DEVICE:      layer[l] is a device buffer of codes [n_caches][N][2][d],
+ *                     scales[l] their scales [n_caches][ceil(N / block)][2][n_heads];
+ *                     request b reads cache cache_of[b] (device int32 [B], NULL:
+ *                     cache b). Nothing is written to them, so requests that
+ *                     edit the same template may share its cache.
+ *  MS_KV_HOST_PINNED: layer[l] is a pinned host buffer of codes [B][N][2][d]
+ *                     (or request_layer, as in ms_kv_source, one [N][2][d] per
+ *                     request); slots are device [B][N][2][d] bytes, used as for
+ *                     ms_kv_source. The scales are small and stay on the device,
+ *                     as above; cache_of[b] numbers request b's scale table.
+ * flags as in ms_kv_source. */
+typedef struct {
+    int32_t kind;
+    int32_t block;                  /* tokens per scale: a power of two, 1..128 */
+    int32_t n_caches;
+    const void* const* layer;       /* [n_layers] */
+    const void* const* scales;      /* [n_layers] */
+    const int32_t* cache_of;
+    int32_t n_slots;
+    void* const* slots;
+    const void* const* request_layer;
+    int32_t flags;
+} ms_kv8_source;
+
+/* mask_stack_forward over such a cache: the masked (and text) rows' fresh K/V
+ * stay in the model's type in the workspace, and every block attends over them
+ * and the unmasked tokens' codes directly (ms_kv8_attention). Half the cache
+ * bytes of bf16 K/V, from HBM and over the copy link. Everything else, the
+ * dense prefix, slots, streams, MS_SERIALIZE and MS_POISON, is as there (the
+ * loads follow the plan of a Y cache). The batch's working K/V (batch x
+ * (n_text + N) x 2 x d_model elements) and one cache's codes must stay below
+ * 4095 MiB. */
+ms_status mask_stack_forward_kv8(ms_step* step, const ms_layer_weights* w, const void* d_x,
+                                 const void* d_ycache, const ms_kv8_source* kv, void* d_y,
+                                 void* compute_stream, void* copy_stream);
+
 void mask_step_destroy(ms_step* step);
 
 /* Kernel timing (tracing). Between start and stop, every launch of a

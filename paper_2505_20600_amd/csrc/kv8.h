@@ -85,10 +85,12 @@ struct Kv8AttnDesc {
     int nseg, M, group;
     const void* kv;             // fresh rows [kv_rows][2][heads * hd], NULL: none
     const int32_t* f_rows;      // rows of kv in list order, NULL: entry i is row i
-    const int32_t* f_start;     // [batch + 1] list entries of each request
+    const int32_t* f_start;     // [batch] first list entry of each request
+    const int32_t* f_end;       // [batch] and the one past its last
     long kv_rows;               // rows of kv
     int f_list;                 // entries of the list
     float scale_log2;           // log2(e) times the score scale
+    bool few;                   // the form for few query slots (bf16)
     int nsplit;                 // key ranges; > 1: partials in part_o / part_ml
     float* part_o;              // [nsplit][M][heads * group * hd], each range's output over its own sum
     float* part_ml;             // [nsplit][M][heads * group][2]: its maximum (log2 domain) and sum
@@ -127,12 +129,17 @@ __device__ __forceinline__ Kv8Req kv8_request(const Kv8Cache& c, const Kv8Select
 __device__ __forceinline__ void kv8_fresh(const Kv8AttnDesc& a, int b, Kv8Req& r) {
     if (!a.kv) return;
     r.f0 = min(max(a.f_start[b], 0), a.f_list);
-    r.nf = min(max(a.f_start[b + 1], r.f0), a.f_list) - r.f0;
+    r.nf = min(max(a.f_end[b], r.f0), a.f_list) - r.f0;
 }
 
 // Unmasked tokens of every request in ascending order: keys[b][0 .. n_keys[b]).
 hipError_t launch_kv8_keys(const uint8_t* mask, int batch, int T, int32_t* keys, int ld_keys, int32_t* n_keys,
                            hipStream_t s);
+// The same for a step context from its inverse map inv [batch][n_text + N] (packed row of a
+// token, < 0: not recomputed): the image tokens that are not recomputed, and the recomputed
+// tokens' flat rows b * (n_text + N) + t, request b's list entries [start[b], end[b]).
+hipError_t launch_kv8_step_lists(const int32_t* inv, int batch, int N, int n_text, int32_t* keys, int32_t* n_keys,
+                                 int32_t* fresh, int32_t* start, int32_t* end, hipStream_t s);
 // K/V rows [..][2][heads * hd] -> codes and scales. src_row NULL: token t of
 // cache c is row c * row_stride + t; else row src_row[c][t] where that lies in
 // [0, kv_rows), and the token keeps its value elsewhere.
@@ -141,8 +148,9 @@ hipError_t launch_kv8_quantize(int dtype, const Kv8Cache& c, const void* kv, lon
 // kv[b * row_stride + t] = the listed tokens' values.
 hipError_t launch_kv8_dequantize(int dtype, const Kv8Cache& c, const Kv8Select& sel, void* kv, long row_stride,
                                  hipStream_t s);
-// Key ranges that an attention call is best divided into (from its sizes; its tables are not read).
-int plan_kv8_attention(int dtype, const Kv8AttnDesc& a);
+// Sets the form and the key ranges for a call over about `keys` keys per request (from its
+// sizes; its tables are not read). The caller may lower nsplit to what its buffers hold.
+void plan_kv8_attention(int dtype, Kv8AttnDesc& a, long keys);
 hipError_t launch_kv8_attention(int dtype, const Kv8AttnDesc& a, hipStream_t s);
 
 }  // namespace ms

@@ -191,6 +191,45 @@ __global__ __launch_bounds__(kScanThreads) void keys_kernel(const uint8_t* __res
     if (threadIdx.x == 0) n_keys[b] = base;
 }
 
+// Both lists of a request from its inverse map; see launch_kv8_step_lists.
+__global__ __launch_bounds__(kScanThreads) void step_lists_kernel(const int32_t* __restrict__ inv, int N, int n_text,
+                                                                  int32_t* __restrict__ keys, int32_t* __restrict__ n_keys,
+                                                                  int32_t* __restrict__ fresh, int32_t* __restrict__ start,
+                                                                  int32_t* __restrict__ end) {
+    __shared__ int s_cached[kScanThreads / kWave], s_fresh[kScanThreads / kWave];
+    const int b = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, T = n_text + N;
+    const long row0 = (long)b * T;
+    int cached = 0, news = 0;
+    for (int t0 = 0; t0 < T; t0 += kScanThreads) {
+        const int t = t0 + threadIdx.x;
+        const bool in = t < T, recomputed = in && inv[row0 + t] >= 0, keep = in && !recomputed && t >= n_text;
+        const uint64_t mc = __ballot(keep), mf = __ballot(recomputed), below = (1ull << lane) - 1;
+        if (lane == 0) {
+            s_cached[wave] = __popcll(mc);
+            s_fresh[wave] = __popcll(mf);
+        }
+        __syncthreads();
+        int c = cached, f = news;
+#pragma unroll
+        for (int w = 0; w < kScanThreads / kWave; ++w) {
+            if (w < wave) {
+                c += s_cached[w];
+                f += s_fresh[w];
+            }
+            cached += s_cached[w];
+            news += s_fresh[w];
+        }
+        if (keep) keys[(long)b * N + c + __popcll(mc & below)] = t - n_text;
+        if (recomputed) fresh[row0 + f + __popcll(mf & below)] = (int)(row0 + t);
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        n_keys[b] = cached;
+        start[b] = (int)row0;
+        end[b] = (int)row0 + news;
+    }
+}
+
 template <typename T, bool REWRITE>
 void launch_quantize(const Kv8Cache& c, const void* kv, long row_stride, const int32_t* src_row, long kv_rows,
                      hipStream_t s) {
@@ -219,6 +258,12 @@ void launch_quantize(const Kv8Cache& c, const void* kv, long row_stride, const i
 hipError_t launch_kv8_keys(const uint8_t* mask, int batch, int T, int32_t* keys, int ld_keys, int32_t* n_keys,
                            hipStream_t s) {
     hipLaunchKernelGGL(keys_kernel, dim3(batch), dim3(kScanThreads), 0, s, mask, T, keys, ld_keys, n_keys);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv8_step_lists(const int32_t* inv, int batch, int N, int n_text, int32_t* keys, int32_t* n_keys,
+                                 int32_t* fresh, int32_t* start, int32_t* end, hipStream_t s) {
+    hipLaunchKernelGGL(step_lists_kernel, dim3(batch), dim3(kScanThreads), 0, s, inv, N, n_text, keys, n_keys, fresh, start, end);
     return hipGetLastError();
 }
 

@@ -100,9 +100,11 @@ ms_status check_attn(const ms_kv8_cache* c, const ms_kv8_select* sel, const ms_k
     d->kv = a->fresh && a->fresh_rows > 0 ? a->fresh : nullptr;
     d->f_rows = a->fresh_list;
     d->f_start = a->fresh_start;
+    d->f_end = a->fresh_start ? a->fresh_start + 1 : nullptr;
     d->kv_rows = a->fresh ? a->fresh_rows : 0;
     d->f_list = (int)entries;
     d->scale_log2 = (float)(1.4426950408889634 * (a->scale != 0.f ? (double)a->scale : 1.0 / std::sqrt((double)c->head_dim)));
+    d->few = true;
     d->nsplit = 1;
     d->part_o = d->part_ml = nullptr;
     return MS_OK;
@@ -111,6 +113,11 @@ ms_status check_attn(const ms_kv8_cache* c, const ms_kv8_select* sel, const ms_k
 // Float32 words of partial results per key range.
 size_t range_floats(const ms::Kv8AttnDesc& d) {
     return (size_t)d.M * d.c.heads * d.group * (d.c.hd + 2);
+}
+
+void plan(int dtype, ms::Kv8AttnDesc& d) {
+    // the fresh rows: about as many for each request
+    ms::plan_kv8_attention(dtype, d, d.sel.ld_keys + d.f_list / d.sel.batch);
 }
 
 }  // namespace
@@ -170,8 +177,8 @@ size_t ms_kv8_attention_workspace_bytes(const ms_kv8_cache* c, const ms_kv8_sele
     ms::Kv8AttnDesc d;
     if (check_attn(c, sel, a, &d) != MS_OK) return 0;
     ms::clear_error();
-    const int n = ms::plan_kv8_attention(c->dtype, d);
-    return n > 1 ? n * range_floats(d) * sizeof(float) : 0;
+    plan(c->dtype, d);
+    return d.nsplit > 1 ? d.nsplit * range_floats(d) * sizeof(float) : 0;
 }
 
 ms_status ms_kv8_attention(const ms_kv8_cache* c, const ms_kv8_select* sel, const ms_kv8_attn* a, void* d_ws,
@@ -183,7 +190,8 @@ ms_status ms_kv8_attention(const ms_kv8_cache* c, const ms_kv8_select* sel, cons
     if (!aligned(d_ws, 16)) return set_error(MS_EALIGN, "workspace not 16-byte aligned");
     if (d.M == 0) return ms::clear_error();
     const size_t one = range_floats(d) * sizeof(float);
-    d.nsplit = std::max(1, std::min<int>(ms::plan_kv8_attention(c->dtype, d), d_ws ? (int)std::min<size_t>(ws_bytes / one, 1024) : 1));
+    plan(c->dtype, d);
+    d.nsplit = std::max(1, std::min(d.nsplit, d_ws ? (int)std::min<size_t>(ws_bytes / one, 1024) : 1));
     if (d.nsplit > 1) {
         d.part_o = static_cast<float*>(d_ws);
         d.part_ml = d.part_o + (size_t)d.nsplit * d.M * d.c.heads * d.group * d.c.hd;

@@ -987,9 +987,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Kv8AttnDesc a) {
 // or two rounds of workgroups. Few / many, 4096 keys: 8 requests of 16, 32, 48 rows of 16 heads
 // of 64 23 / 29, 33 / 33, 48 / 38 us; 4 x 32 rows of 24 heads of 128 47 / 37; 1 x 48, 64 rows
 // of 24 heads of 128 27 / 29, 32 / 28; 128 rows of 12 heads of 64 over 1024 keys 12 / 15.
-bool few_slots(const Kv8AttnDesc& a) {
+bool few_slots(const Kv8AttnDesc& a, long keys) {
     const long rows = (long)a.M * a.group, segs = std::min(a.nseg, a.M), per = (rows + segs - 1) / segs;
-    const long keys = a.sel.ld_keys + a.f_list / a.sel.batch;
     return per <= (a.c.hd < 96 ? 32 : 16) || segs * ((per + 15) / 16) * a.c.heads * keys <= 1l << 18;
 }
 
@@ -1032,19 +1031,21 @@ void launch_f32(const Kv8AttnDesc& a, hipStream_t s) {
 // registers let a CU hold; a round with k on a CU takes 7 us + 1.5 per further one to start
 // and end and, per 64-key tile, the tile's matrix instructions times (0.0165 + 0.008 k) us;
 // the join a launch and its parts at 5 TB/s.
-int plan_kv8_attention(int dtype, const Kv8AttnDesc& a) {
-    if (a.M == 0) return 1;
+void plan_kv8_attention(int dtype, Kv8AttnDesc& a, long keys) {
+    a.few = true;
+    a.nsplit = 1;
+    if (a.M == 0) return;
     const int heads = a.c.heads, hd = a.c.hd;
     const long rows = (long)a.M * a.group, segs = std::min(a.nseg, a.M), per = (rows + segs - 1) / segs;
-    const long keys = a.sel.ld_keys + a.f_list / a.sel.batch;   // fresh rows: about as many for each request
-    if (dtype != kBF16 || few_slots(a)) {
+    a.few = dtype != kBF16 || few_slots(a, keys);
+    if (a.few) {
         const long base = segs * ((per + 15) / 16) * heads, target = hd < 96 ? 512 : 256, least = dtype == kBF16 ? 256 : 128;
-        return (int)std::max<long>(1, std::min<long>({(target + base - 1) / base, (keys + least - 1) / least, kMaxRanges}));
+        a.nsplit = (int)std::max<long>(1, std::min<long>({(target + base - 1) / base, (keys + least - 1) / least, kMaxRanges}));
+        return;
     }
     const long base = segs * ((per + 127) / 128) * heads, tiles = (keys + 63) / 64;
     const int per_cu = shared_per_cu(hd);
     const double unit = 8 * ((hd + 31) / 32) + 4 * ((hd + 15) / 16 + (hd % 16 == 0));
-    int best = 1;
     double least = 1e30;
     for (int n = 1; n <= std::min<long>(tiles, kMaxRanges); ++n) {
         const long groups = base * n, slots = 256l * per_cu, rest = groups % slots;
@@ -1054,16 +1055,15 @@ int plan_kv8_attention(int dtype, const Kv8AttnDesc& a) {
         if (n > 1) us += 3.0 + (4.0 * n + 2) * rows * heads * hd / 5.0e6;
         if (us < least) {
             least = us;
-            best = n;
+            a.nsplit = n;
         }
     }
-    return best;
 }
 
 hipError_t launch_kv8_attention(int dtype, const Kv8AttnDesc& a, hipStream_t s) {
     if (a.M == 0) return hipSuccess;
     if (dtype == kBF16) {
-        if (few_slots(a)) launch_bf16<false>(a, s);
+        if (a.few) launch_bf16<false>(a, s);
         else launch_bf16<true>(a, s);
     } else {
         launch_f32(a, s);

@@ -18,6 +18,7 @@
 #include "../../include/maskstep.h"
 #include "../../include/maskstep_ops.h"
 #include "kernels.h"
+#include "kv8.h"
 #include "step_internal.h"
 
 namespace {
@@ -66,6 +67,7 @@ struct Layout {
     size_t rows_d, inv_d, seg_start_d, seg_req_d, cu_tiles_d;    // every-token packing
     size_t ones;                                                 // all-ones mask [B][N]
     size_t u_src, u_tok;                                         // unmasked image rows (Y caching)
+    size_t k8_keys, k8_n, k8_fresh, k8_start, k8_end;            // cached tokens and recomputed rows per request (8-bit cache)
     size_t xm, a, q, o, h, u, kv_dense, part_ml, gemm_part, total;
 };
 
@@ -134,6 +136,11 @@ Layout make_layout(const ms_model_desc& d, int32_t B) {
     L.ones = take((size_t)B * N);
     L.u_src = take((size_t)B * N * 4);
     L.u_tok = take((size_t)B * N * 4);
+    L.k8_keys = take((size_t)B * N * 4);
+    L.k8_n = take((size_t)B * 4);
+    L.k8_fresh = take(BT * 4);
+    L.k8_start = take((size_t)B * 4);
+    L.k8_end = take((size_t)B * 4);
     L.xm = take(BT * dm * e);
     L.a = take(BT * dm * e);
     L.q = take(BT * dm * e);
@@ -494,8 +501,11 @@ hipError_t run_gemm(ms_step* s, ms::GemmDesc& g, int cls, hipStream_t st, const 
 // holds LayerNorm 1 of xm (the previous block computed it); `next`: weights
 // of the block that follows on the same rows, whose LayerNorm 1 this block
 // then leaves in the scratch buffer.
+// `k8`: the unmasked tokens' keys and values come from this 8-bit cache, `kv` then holds the
+// fresh rows only.
 ms_status block_forward(ms_step* s, const Packing& pk, const ms_layer_weights* w, void* xm, void* kv,
-                        hipStream_t st, const ms_layer_weights* next = nullptr, bool a_ready = false) {
+                        hipStream_t st, const ms_layer_weights* next = nullptr, bool a_ready = false,
+                        const ms::Kv8Cache* k8 = nullptr, const ms::Kv8Select* k8_sel = nullptr) {
     if (pk.M == 0) return MS_OK;
     const int dt = s->desc.dtype;
     const bool dual = s->desc.dual_stream && s->desc.n_text > 0;
@@ -534,25 +544,47 @@ ms_status block_forward(ms_step* s, const Packing& pk, const ms_layer_weights* w
         g.epilogue = ms::kEpiQKV;
         MS_HIP(run_gemm(s, g, MS_K_GEMM_QKV, st));
     }
-    ms::AttnDesc ad{};
-    ad.q = q; ad.kv = kv; ad.o = o;
-    ad.seg_start = pk.segs; ad.seg_req = pk.segreq; ad.cu_tiles = pk.cutiles;
-    ad.nseg = pk.nseg; ad.T = s->T; ad.d = d; ad.hd = s->hd;
-    ad.n_qtiles = pk.n_qtiles; ad.n_heads = s->desc.n_heads;
-    ad.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)s->hd));
-    ad.M = M;
-    ad.n_qtiles_fast = pk.n_qtiles_fast;
-    ad.nsplit = pk.attn_nsplit;
-    ad.tiles_per_split = pk.attn_tps;
-    ad.part_o = static_cast<float*>(s->buf(s->lay.u));
-    ad.part_ml = static_cast<float*>(s->buf(s->lay.part_ml));
-    {
+    if (k8) {
+        ms::Kv8AttnDesc ad{};
+        ad.c = *k8;
+        ad.sel = *k8_sel;
+        ad.q = q; ad.o = o;
+        ad.seg_start = pk.segs; ad.seg_req = pk.segreq; ad.nseg = pk.nseg; ad.M = M; ad.group = 1;
+        ad.kv = kv;
+        ad.f_rows = s->at<int32_t>(s->lay.k8_fresh);
+        ad.f_start = s->at<int32_t>(s->lay.k8_start);
+        ad.f_end = s->at<int32_t>(s->lay.k8_end);
+        ad.kv_rows = (long)s->B * s->T;
+        ad.f_list = s->B * s->T;
+        ad.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)s->hd));
+        ad.part_o = static_cast<float*>(s->buf(s->lay.u));
+        ad.part_ml = static_cast<float*>(s->buf(s->lay.part_ml));
+        const size_t part_rows = std::min(attn_part_rows(s->desc, s->B), attn_part_o_rows(s->desc, s->B));
+        ms::plan_kv8_attention(dt, ad, (s->U + M) / s->B);
+        ad.nsplit = std::max(1, std::min(ad.nsplit, (int)(part_rows / M)));
         ProfScope p(MS_K_ATTENTION, st);
-        MS_HIP(ms::launch_attention(dt, ad, st));
-    }
-    {
-        ProfScope p(MS_K_ATTN_COMBINE, st);
-        MS_HIP(ms::launch_attention_combine(dt, ad, st));
+        MS_HIP(ms::launch_kv8_attention(dt, ad, st));
+    } else {
+        ms::AttnDesc ad{};
+        ad.q = q; ad.kv = kv; ad.o = o;
+        ad.seg_start = pk.segs; ad.seg_req = pk.segreq; ad.cu_tiles = pk.cutiles;
+        ad.nseg = pk.nseg; ad.T = s->T; ad.d = d; ad.hd = s->hd;
+        ad.n_qtiles = pk.n_qtiles; ad.n_heads = s->desc.n_heads;
+        ad.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)s->hd));
+        ad.M = M;
+        ad.n_qtiles_fast = pk.n_qtiles_fast;
+        ad.nsplit = pk.attn_nsplit;
+        ad.tiles_per_split = pk.attn_tps;
+        ad.part_o = static_cast<float*>(s->buf(s->lay.u));
+        ad.part_ml = static_cast<float*>(s->buf(s->lay.part_ml));
+        {
+            ProfScope p(MS_K_ATTENTION, st);
+            MS_HIP(ms::launch_attention(dt, ad, st));
+        }
+        {
+            ProfScope p(MS_K_ATTN_COMBINE, st);
+            MS_HIP(ms::launch_attention_combine(dt, ad, st));
+        }
     }
     for (const Range& r : ranges) {
         if (r.r1 <= r.r0) continue;
@@ -653,10 +685,12 @@ struct HostLayer {
     const void* const* req;
 };
 
-ms_status prefetch(ms_step* s, HostLayer h, void* d_slot, hipStream_t cs, hipEvent_t wait, bool y = false) {
+// `image`: rows of `image` bytes of the image tokens only, in place (Y caching's, an 8-bit cache's codes); 0: K/V rows
+ms_status prefetch(ms_step* s, HostLayer h, void* d_slot, hipStream_t cs, hipEvent_t wait, size_t image = 0) {
     if (wait) MS_HIP(hipStreamWaitEvent(cs, wait, 0));
     ProfScope p(MS_K_COPY, cs);
-    const size_t row_bytes = (y ? 1ull : 2ull) * s->d * s->elt;
+    const bool y = image != 0;
+    const size_t row_bytes = y ? image : 2ull * s->d * s->elt;
     const size_t drows = y ? (size_t)s->N : (size_t)s->T, dtext = y ? 0 : (size_t)s->desc.n_text;
     char* dst = static_cast<char*>(d_slot);
     const size_t pitch = (size_t)s->desc.grid_w * row_bytes;   // one grid row, host and device alike
@@ -675,8 +709,8 @@ ms_status prefetch(ms_step* s, HostLayer h, void* d_slot, hipStream_t cs, hipEve
 }
 
 ms_status prefetch_signal(ms_step* s, HostLayer h, void* d_slot, hipStream_t cs, hipEvent_t wait,
-                          hipEvent_t signal, bool y = false) {
-    ms_status st = prefetch(s, h, d_slot, cs, wait, y);
+                          hipEvent_t signal, size_t image = 0) {
+    ms_status st = prefetch(s, h, d_slot, cs, wait, image);
     if (st != MS_OK) return st;
     if (signal) MS_HIP(hipEventRecord(signal, cs));
     return MS_OK;
@@ -1122,7 +1156,7 @@ ms_status cache_prefetch_inputs(ms_step* s, int32_t layer, const void* h_yin, vo
     ms_status st = check_pinned(h_yin);
     if (st != MS_OK) return st;
     st = prefetch_signal(s, HostLayer{h_yin, nullptr}, d_slot, static_cast<hipStream_t>(copy_stream),
-                         static_cast<hipEvent_t>(wait_event), static_cast<hipEvent_t>(signal_event), true);
+                         static_cast<hipEvent_t>(wait_event), static_cast<hipEvent_t>(signal_event), (size_t)s->d * s->elt);
     return st == MS_OK ? ok() : st;
 }
 
@@ -1139,14 +1173,23 @@ ms_status mask_recompute_kv(ms_step* s, int32_t layer, const ms_layer_weights* w
     return st == MS_OK ? ok() : st;
 }
 
-ms_status mask_stack_forward(ms_step* s, const ms_layer_weights* w, const void* d_x,
-                             const void* d_ycache, const ms_kv_source* kv, void* d_y,
-                             void* compute_stream, void* copy_stream) {
+namespace {
+// The whole step. `k8`: the cache is 8-bit; `kv` then describes its codes like a Y cache (rows of
+// the image tokens only), `k8` its form and scale tables.
+struct Kv8Step {
+    ms::Kv8Cache cache;             // codes and scales: the layer's, set per block
+    ms::Kv8Select sel;
+    const void* const* scales;      // [n_layers]
+};
+
+ms_status stack_forward(ms_step* s, const ms_layer_weights* w, const void* d_x, const void* d_ycache,
+                        const ms_kv_source* kv, void* d_y, void* compute_stream, void* copy_stream, const Kv8Step* k8) {
     if (!s) return fail(MS_ESTATE, "no step context");
     if (!w || !d_x || !kv || !d_y) return fail(MS_EINVAL, "NULL argument");
     if (!d_ycache && !s->all_masked) return fail(MS_EINVAL, "y_cache may be NULL only when every token is masked");
     if (kv->kind < MS_KV_DEVICE || kv->kind > MS_Y_HOST_PINNED) return fail(MS_EINVAL, "unknown kv kind %d", kv->kind);
-    const bool ycache = kv->kind == MS_Y_DEVICE || kv->kind == MS_Y_HOST_PINNED;
+    const bool ycache = !k8 && (kv->kind == MS_Y_DEVICE || kv->kind == MS_Y_HOST_PINNED);
+    const size_t image = k8 ? 2ull * s->d : ycache ? (size_t)s->d * s->elt : 0;   // bytes of an image row (prefetch)
     const bool pinned = kv->kind == MS_KV_HOST_PINNED || kv->kind == MS_Y_HOST_PINNED;
     const bool per_req = pinned && kv->request_layer;
     if (!per_req && !kv->layer) return fail(MS_EINVAL, "kv->layer is NULL");
@@ -1244,7 +1287,7 @@ ms_status mask_stack_forward(ms_step* s, const ms_layer_weights* w, const void* 
                 if (prev_known && issued == 0) wait = prev_h > 0 ? ring->half[pp] : ring->all[pp];
                 else if (prev_known && issued == prev_h && prev_h > 0) wait = ring->all[pp];
                 ms_status st = prefetch_signal(s, host_layer(k + issued), kv->slots[sl], ps, wait, s->ev_copied[ecp + sl],
-                                               ycache);
+                                               image);
                 if (st != MS_OK) return st;
             }
             return MS_OK;
@@ -1300,13 +1343,19 @@ ms_status mask_stack_forward(ms_step* s, const ms_layer_weights* w, const void* 
             ProfScope p(MS_K_GATHER, cs);
             MS_HIP(ms::launch_gather(d_x, mp.rows, xm, mp.M, s->d * s->elt, cs));
         }
+        if (k8 && k < L) {
+            ProfScope p(MS_K_COMPACT, cs);
+            MS_HIP(ms::launch_kv8_step_lists(mp.inv, s->B, s->N, s->desc.n_text, s->at<int32_t>(s->lay.k8_keys),
+                                             s->at<int32_t>(s->lay.k8_n), s->at<int32_t>(s->lay.k8_fresh),
+                                             s->at<int32_t>(s->lay.k8_start), s->at<int32_t>(s->lay.k8_end), cs));
+        }
         for (int l = k; l < L; ++l) {
             const int j = l - k;
             void* src = pinned ? nullptr : const_cast<void*>(kv->layer[l]);
             if (pinned) {
                 src = kv->slots[j % n_slots];
                 if (serialize) {
-                    ms_status st = prefetch(s, host_layer(l), src, cs, nullptr, ycache);
+                    ms_status st = prefetch(s, host_layer(l), src, cs, nullptr, image);
                     if (st != MS_OK) return st;
                 } else if (stream_cache) {
                     ms_status st = issue_upto(allowed());   // includes load j
@@ -1322,13 +1371,22 @@ ms_status mask_stack_forward(ms_step* s, const ms_layer_weights* w, const void* 
                 ms_status st = recompute_kv(s, w + (size_t)l * wstride, src, kvbuf, cs);
                 if (st != MS_OK) return st;
             }
+            // 8-bit variant: the cache stays as it is, the fresh rows go to the workspace
+            ms::Kv8Cache cache{};
+            if (k8) {
+                cache = k8->cache;
+                cache.codes = static_cast<uint8_t*>(src);
+                cache.scales = static_cast<uint8_t*>(const_cast<void*>(k8->scales[l]));
+                kvbuf = s->buf(s->lay.kv_dense);
+            }
             const ms_layer_weights* next = l + 1 < L ? w + (size_t)(l + 1) * wstride : nullptr;
-            ms_status st = block_forward(s, mp, w + (size_t)l * wstride, xm, kvbuf, cs, next, l > k || first_ln_ready);
+            ms_status st = block_forward(s, mp, w + (size_t)l * wstride, xm, kvbuf, cs, next, l > k || first_ln_ready,
+                                         k8 ? &cache : nullptr, k8 ? &k8->sel : nullptr);
             if (st != MS_OK) return st;
             if (pinned && poison) {
                 // debugging mode: the slot's contents die with its block; a later block that read a
                 // row its own load or fresh K/V did not write would see NaN
-                const size_t slot_bytes = (size_t)s->B * (ycache ? s->N : s->T) * (ycache ? 1 : 2) * s->d * s->elt;
+                const size_t slot_bytes = image ? (size_t)s->B * s->N * image : (size_t)s->B * s->T * 2 * s->d * s->elt;
                 MS_HIP(ms::launch_fill_u8(src, 0xFF, slot_bytes, cs));
             }
             if (stream_cache && !capturing && (j + 1 == my_h || j + 1 == n_cached)) {
@@ -1357,6 +1415,56 @@ ms_status mask_stack_forward(ms_step* s, const ms_layer_weights* w, const void* 
                                   s->d * s->elt, cs));
     }
     return ok();
+}
+}  // namespace
+
+ms_status mask_stack_forward(ms_step* s, const ms_layer_weights* w, const void* d_x, const void* d_ycache,
+                             const ms_kv_source* kv, void* d_y, void* compute_stream, void* copy_stream) {
+    return stack_forward(s, w, d_x, d_ycache, kv, d_y, compute_stream, copy_stream, nullptr);
+}
+
+ms_status mask_stack_forward_kv8(ms_step* s, const ms_layer_weights* w, const void* d_x, const void* d_ycache,
+                                 const ms_kv8_source* kv, void* d_y, void* compute_stream, void* copy_stream) {
+    if (!s) return fail(MS_ESTATE, "no step context");
+    if (!kv) return fail(MS_EINVAL, "NULL argument");
+    if (kv->kind != MS_KV_DEVICE && kv->kind != MS_KV_HOST_PINNED) return fail(MS_EINVAL, "unknown kv kind %d", kv->kind);
+    if (!kv->scales) return fail(MS_EINVAL, "kv->scales is NULL");
+    for (int l = 0; l < s->desc.n_layers; ++l)
+        if (!kv->scales[l]) return fail(MS_EINVAL, "kv->scales[%d] is NULL", l);
+    if (kv->block < 1 || kv->block > 128 || (kv->block & (kv->block - 1)))
+        return fail(MS_ESHAPE, "block %d must be a power of two, 1..128", kv->block);
+    if (kv->n_caches < 1 || kv->n_caches > (1 << 20)) return fail(MS_ESHAPE, "n_caches %d outside 1..2^20", kv->n_caches);
+    if (!kv->cache_of && s->B > kv->n_caches)
+        return fail(MS_ESHAPE, "batch %d above n_caches %d needs cache_of", s->B, kv->n_caches);
+    if (reinterpret_cast<uintptr_t>(kv->cache_of) % 4) return fail(MS_EALIGN, "cache_of not 4-byte aligned");
+    if ((int64_t)s->B * s->T * 2 * s->d * s->elt >= (1ll << 32) - (1 << 20))
+        return fail(MS_ESHAPE, "the batch's fresh K/V (batch x tokens x 2 x d_model elements) must stay below 4095 MiB");
+    if (2ll * s->N * s->d >= (1ll << 32) - (1 << 20))
+        return fail(MS_ESHAPE, "one cache's codes (image tokens x 2 x d_model bytes) must stay below 4095 MiB");
+    const bool pinned = kv->kind == MS_KV_HOST_PINNED;
+    Kv8Step k8{};
+    k8.cache.n_caches = pinned ? s->B : kv->n_caches;
+    k8.cache.n_scales = kv->n_caches;
+    k8.cache.T = s->N;
+    k8.cache.heads = s->desc.n_heads;
+    k8.cache.hd = s->hd;
+    while ((1 << k8.cache.lblock) < kv->block) ++k8.cache.lblock;
+    k8.cache.blocks = (s->N + kv->block - 1) / kv->block;
+    k8.sel.codes_of = pinned ? nullptr : kv->cache_of;
+    k8.sel.scales_of = kv->cache_of;
+    k8.sel.keys = s->at<int32_t>(s->lay.k8_keys);
+    k8.sel.n_keys = s->at<int32_t>(s->lay.k8_n);
+    k8.sel.ld_keys = s->N;
+    k8.sel.batch = s->B;
+    k8.scales = kv->scales;
+    ms_kv_source src{};
+    src.kind = pinned ? MS_Y_HOST_PINNED : MS_Y_DEVICE;
+    src.layer = kv->layer;
+    src.n_slots = kv->n_slots;
+    src.slots = kv->slots;
+    src.request_layer = kv->request_layer;
+    src.flags = kv->flags;
+    return stack_forward(s, w, d_x, d_ycache, &src, d_y, compute_stream, copy_stream, &k8);
 }
 
 void mask_step_destroy(ms_step* s) {

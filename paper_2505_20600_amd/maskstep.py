@@ -53,6 +53,12 @@ class Kv8Cache(C.Structure):
                 ("head_dim", C.c_int32), ("block", C.c_int32), ("codes", C.c_void_p), ("scales", C.c_void_p)]
 
 
+class Kv8Source(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("block", C.c_int32), ("n_caches", C.c_int32), ("layer", C.POINTER(C.c_void_p)),
+                ("scales", C.POINTER(C.c_void_p)), ("cache_of", C.c_void_p), ("n_slots", C.c_int32),
+                ("slots", C.POINTER(C.c_void_p)), ("request_layer", C.POINTER(C.c_void_p)), ("flags", C.c_int32)]
+
+
 class Kv8Select(C.Structure):
     _fields_ = [("batch", C.c_int32), ("ld_keys", C.c_int32), ("cache_of", C.c_void_p), ("keys", C.c_void_p),
                 ("n_keys", C.c_void_p)]
@@ -111,6 +117,7 @@ def load() -> C.CDLL:
             "mask_recompute_kv": (i32, [vp, i32, C.POINTER(LayerWeights), vp, vp, vp]),
             "mask_stack_forward": (i32, [vp, C.POINTER(LayerWeights), vp, vp, C.POINTER(KVSource),
                                          vp, vp, vp]),
+            "mask_stack_forward_kv8": (i32, [vp, C.POINTER(LayerWeights), vp, vp, C.POINTER(Kv8Source), vp, vp, vp]),
             "mask_step_destroy": (None, [vp]),
             "mask_step_set_dense_prefix": (i32, [vp, i32, vp]),
             "mask_plan_dense_prefix": (i32, [i32, C.c_double, C.c_double, C.c_double, C.POINTER(i32),
@@ -150,7 +157,7 @@ EXPORTED = ("mask_abi_version", "mask_last_error", "mask_workspace_bytes", "mask
             "mask_step_init_static",
             "mask_step_get_info", "mask_step_index", "mask_gather_rows", "mask_block_forward",
             "mask_scatter_rows", "cache_prefetch_layer", "cache_prefetch_inputs", "mask_recompute_kv",
-            "mask_stack_forward", "mask_step_destroy",
+            "mask_stack_forward", "mask_stack_forward_kv8", "mask_step_destroy",
             "mask_step_set_dense_prefix", "mask_plan_dense_prefix",
             "mask_profiler_start", "mask_profiler_stop", "mask_profiler_intervals", "ms_linear",
             "mask_fit_linear", "mask_batch_cost", "mask_route_request", "mask_plan_copies",
@@ -650,3 +657,24 @@ class MaskStep:
         ps = _stream(copy_stream) if copy_stream is not None else cs
         _check(self._lib.mask_stack_forward(self.handle, weights_c, _ptr(x), _ptr(ycache), C.byref(src),
                                             _ptr(y), cs, ps))
+
+    def stack_forward_kv8(self, weights_c, x, ycache, codes, scales, y, *, block: int, cache_of=None, pinned: bool = False,
+                          slots=(), stream=None, copy_stream=None, per_request=None, loads_ahead: bool = False):
+        """stack_forward over a K/V cache in 8 bits. ``codes``: [L] byte tensors [caches][N][2][heads][head_dim] on the
+        device, or with ``pinned`` pinned host [B][N][2][heads][head_dim] (``per_request`` may replace them: [L][B]
+        pinned [N][2][heads][head_dim]) that stream through the device ``slots``; ``scales``: [L] device byte tensors
+        [caches][ceil(N / block)][2][heads]; ``cache_of``: device int32 [B], each request's cache (pinned: scale table)."""
+        L = len(scales)
+        S = scales[0].shape[0]
+        sc = (C.c_void_p * L)(*[_ptr(t) for t in scales])
+        ptrs = (C.c_void_p * L)(*[_ptr(t) for t in codes]) if per_request is None else (C.c_void_p * 1)()
+        req = (C.c_void_p * max(1, L * self.batch))(*[_ptr(t) for r in per_request or () for t in r])
+        sl = (C.c_void_p * max(1, len(slots)))(*[_ptr(t) for t in slots])
+        pp = C.POINTER(C.c_void_p)
+        src = Kv8Source(MS_KV_HOST_PINNED if pinned else MS_KV_DEVICE, block, S,
+                        pp() if per_request is not None else C.cast(ptrs, pp), C.cast(sc, pp),
+                        _ptr(cache_of), len(slots) if pinned else 0, C.cast(sl, pp),
+                        C.cast(req, pp) if per_request is not None else pp(), MS_KV_LOADS_AHEAD if loads_ahead else 0)
+        cs = _stream(stream)
+        ps = _stream(copy_stream) if copy_stream is not None else cs
+        _check(self._lib.mask_stack_forward_kv8(self.handle, weights_c, _ptr(x), _ptr(ycache), C.byref(src), _ptr(y), cs, ps))
