@@ -344,6 +344,9 @@ __device__ __forceinline__ void join_waves(const Kv8AttnDesc& a, const Work& w, 
     if (a.nsplit > 1 && tid % 16 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * part) = make_float2(m, sum);
 }
 
+// Workgroups of the SHARED form that the registers let a CU hold.
+constexpr int shared_per_cu(int hd) { return hd <= 16 ? 4 : hd <= 72 ? 3 : 2; }
+
 // bf16. SHARED: 128 query slots, 32 per wave, the four waves share 64-key tiles
 // in two stages. Not SHARED: 16 slots, every wave has key tiles of its own (32
 // keys, tile t0 + wave + 4 i) and the four partial results are joined at the end.
@@ -366,7 +369,7 @@ struct Bf16Cfg {
 };
 
 template <int HD, bool SHARED>
-__global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2) : HD <= 48 || HD == 64 ? 4 : HD <= 80 ? 3 : 2) void attend_bf16_kernel(Kv8AttnDesc a, int qtiles) {
+__global__ __launch_bounds__(kThreads, SHARED ? shared_per_cu(HD) : HD <= 48 || HD == 64 ? 4 : HD <= 80 ? 3 : 2) void attend_bf16_kernel(Kv8AttnDesc a, int qtiles) {
     using C = Bf16Cfg<HD, SHARED>;
     using S = typename C::S;
     constexpr int NQB = C::NQB, NKS = C::NKS;
@@ -419,13 +422,10 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
     uint32_t koff[C::NK32];
 #pragma unroll
     for (int kc = 0; kc < C::NK32; ++kc) koff[kc] = l16 * S::ROWB + (((4 * kc + grp) ^ fK) * 16);
-    uint32_t kofft[C::KTAIL ? NKS : 1];
-    if constexpr (C::KTAIL) {
-        const int col = (C::NK32 - 1) * 64 + grp * 16;   // bytes
-#pragma unroll
-        for (int ks = 0; ks < NKS; ++ks)
-            kofft[ks] = col < S::ROWB ? (ks * 16 + l16) * S::ROWB + ((col / 16) ^ fK) * 16 : S::TILEB;
-    }
+    // last QK step of a head_dim that is not a multiple of 32 (its rows are not swizzled): lanes
+    // whose slots lie past the row read the stage's block of zeros
+    static_assert(!C::KTAIL || !S::SWZ, "tail offsets");
+    const bool in_row = (C::NK32 - 1) * 64 + grp * 16 < S::ROWB;
     const int rowA = 4 * grp + (l16 >> 2);
     const int fV = v_swz<S::ROWB>(rowA);
     uint32_t voffh[C::NREAL];
@@ -462,9 +462,9 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
         for (int ks = 0; ks < NKS; ++ks) {
 #pragma unroll
             for (int kc = 0; kc < C::NK32; ++kc) {
-                const bool pad = C::KTAIL && kc == C::NK32 - 1;
-                const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(
-                    smem + sbase + (pad ? kofft[C::KTAIL ? ks : 0] : koff[kc] + ks * 16 * S::ROWB));
+                uint32_t at = koff[kc] + ks * 16 * S::ROWB;
+                if (C::KTAIL && kc == C::NK32 - 1) at = in_row ? at : (uint32_t)S::TILEB;
+                const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(smem + sbase + at);
 #pragma unroll
                 for (int qb = 0; qb < NQB; ++qb) sacc[qb][ks] = mfma32(kf, qf[qb][kc], sacc[qb][ks]);
             }
@@ -528,9 +528,11 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
                 for (int r = 0; r < 4; ++r) sacc[qb][ks][r] = fast_exp2(sacc[qb][ks][r] * cs);
     };
     auto pv = [&](uint32_t sbase, f32x4_t (&sacc)[NQB][NKS]) {
-        uint32_t vbase[C::NREAL];
+        // without a swizzle the blocks of 16 columns lie 32 bytes apart, an offset of the reads
+        constexpr int NB = S::SWZ ? C::NREAL : 1;
+        uint32_t vbase[NB];
 #pragma unroll
-        for (int h = 0; h < C::NREAL; ++h) {
+        for (int h = 0; h < NB; ++h) {
             vbase[h] = lds0 + sbase + voffh[h];
             asm volatile("" : "+v"(vbase[h]));   // keep the sum: offsets are added per read
         }
@@ -542,8 +544,8 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
                 if (h >= C::NREAL) {
                     vf[h] = onesf;
                 } else {
-                    lds_cptr p0 = (lds_cptr)(uintptr_t)vbase[h] + (32 * c) * S::ROWB;
-                    lds_cptr p1 = (lds_cptr)(uintptr_t)vbase[h] + (32 * c + 16) * S::ROWB;
+                    const lds_cptr vb = (lds_cptr)(uintptr_t)vbase[S::SWZ ? h : 0] + (S::SWZ ? 0 : 32 * h);
+                    lds_cptr p0 = vb + (32 * c) * S::ROWB, p1 = vb + (32 * c + 16) * S::ROWB;
                     if (h == C::NREAL - 1 && ones_lane) { p0 = (lds_cptr)(uintptr_t)(lds0 + ones_rel); p1 = p0; }
                     const bf16x4_t lo = ld_tr16(p0), hi = ld_tr16(p1);
                     vf[h] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -600,8 +602,17 @@ __global__ __launch_bounds__(kThreads, SHARED ? (HD <= 16 ? 4 : HD <= 64 ? 3 : 2
                     next();
                     continue;
                 }
-                qk(stage(n), sa);
-                next();
+                // under the matrix instructions of QK, or before them where the registers saved make
+                // room for a third workgroup per CU (head_dim 72: 12 x 1024 rows of 16 heads over 4096
+                // keys 347 -> 320 us; 80 and 104, with two either way, are 2% faster the first way)
+                if constexpr (S::SWZ || shared_per_cu(HD) != 3) {
+                    qk(stage(n), sa);
+                    next();
+                } else {
+                    next();
+                    __builtin_amdgcn_sched_barrier(0);
+                    qk(stage(n), sa);
+                }
                 drop_absent(now, sa);
                 softmax(sa);
                 pv(stage(n), sa);
@@ -992,8 +1003,6 @@ bool few_slots(const Kv8AttnDesc& a, long keys) {
     return per <= (a.c.hd < 96 ? 32 : 16) || segs * ((per + 15) / 16) * a.c.heads * keys <= 1l << 18;
 }
 
-// Workgroups of the SHARED form that the registers let a CU hold.
-constexpr int shared_per_cu(int hd) { return hd <= 16 ? 4 : hd <= 64 ? 3 : 2; }
 
 template <bool SHARED>
 void launch_bf16(const Kv8AttnDesc& a, hipStream_t s) {

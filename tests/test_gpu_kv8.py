@@ -331,7 +331,7 @@ def _check(g, dtype, H, G, hd, block, S, T, rows, *, lists="all", fresh="rows", 
         fine = ~np.isnan(ref)
         assert np.all(off[fine] <= tol[fine]), f"segment {s}: {(off - tol)[fine].max():.3e} beyond, {len(k)} keys"
         if fine.any() and off[fine].size:
-            worst = max(worst, float((off[fine] / tol[fine]).max()))
+            worst = max(worst, float((off[fine] / np.maximum(tol[fine], 1e-30)).max()))
         refs.append(ref)
     assert bool((out[start[-1]:] == 7.0).all())      # rows behind the last segment
     print(f"[parity] {dtype} {H}x{G} hd {hd} T {T} rows {rows[:6]}: {worst:.2f} of the bound", flush=True)
