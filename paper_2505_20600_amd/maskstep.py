@@ -239,21 +239,20 @@ def _kv8_stride(kv, c):
     return kv.shape[1] if kv.shape[0] == 1 else step // row
 
 
-class _on_device_of:
-    """The tensor's device as the current one (a launch goes to the current device's stream)."""
-    __slots__ = ("dev", "was")
-
-    def __init__(self, t):
-        self.dev = t.device.index
-
-    def __enter__(self):
-        self.was = torch.cuda.current_device()
-        if self.was != self.dev:
-            torch.cuda.set_device(self.dev)
-
-    def __exit__(self, *exc):
-        if self.was != self.dev:
-            torch.cuda.set_device(self.was)
+def _kv8_run(fn, t, stream, *args):
+    """fn(*args, stream) with the tensor's device as the current one (a launch goes to the current device) and, by
+    default, that device's current stream."""
+    dev = t.get_device()
+    was = torch._C._cuda_getDevice()
+    if was != dev:
+        torch.cuda.set_device(dev)
+    try:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream))
+    finally:
+        if was != dev:
+            torch.cuda.set_device(was)
+    if status != MS_OK:
+        _check(status)
 
 
 def ms_kv8_keys(mask, keys, n_keys, *, stream=None):
@@ -264,8 +263,7 @@ def ms_kv8_keys(mask, keys, n_keys, *, stream=None):
     B, T = mask.shape
     kp = _kv8_table(keys, mask.device, (B, keys.shape[-1]), "keys")
     np_ = _kv8_table(n_keys, mask.device, (B,), "n_keys")
-    with _on_device_of(mask):
-        _check(load().ms_kv8_keys(mask.data_ptr(), B, T, kp, keys.shape[-1], np_, _stream(stream)))
+    _kv8_run(load().ms_kv8_keys, mask, stream, mask.data_ptr(), B, T, kp, keys.shape[-1], np_)
 
 
 def ms_kv8_quantize(kv, codes, scales, *, block, src_row=None, stream=None):
@@ -285,8 +283,7 @@ def ms_kv8_quantize(kv, codes, scales, *, block, src_row=None, stream=None):
         rows, stride = kv.shape[0], 0
         if rows == 0:
             return
-    with _on_device_of(kv):
-        _check(load().ms_kv8_quantize(C.byref(c), kv.data_ptr(), rows, stride, src, _stream(stream)))
+    _kv8_run(load().ms_kv8_quantize, kv, stream, C.byref(c), kv.data_ptr(), rows, stride, src)
 
 
 def ms_kv8_dequantize(codes, scales, kv, *, block, cache_of=None, keys=None, n_keys=None, stream=None):
@@ -295,8 +292,7 @@ def ms_kv8_dequantize(codes, scales, kv, *, block, cache_of=None, keys=None, n_k
     c = _kv8_cache(codes, scales, block, kv)
     stride = _kv8_stride(kv, c)
     sel = _kv8_select(kv.device, kv.shape[0], cache_of, keys, n_keys)
-    with _on_device_of(kv):
-        _check(load().ms_kv8_dequantize(C.byref(c), C.byref(sel), kv.data_ptr(), stride, _stream(stream)))
+    _kv8_run(load().ms_kv8_dequantize, kv, stream, C.byref(c), C.byref(sel), kv.data_ptr(), stride)
 
 
 def ms_kv8_attention_workspace_bytes(q, codes, seg_start, *, keys=None, fresh=None, fresh_list=None) -> int:
@@ -358,8 +354,7 @@ def ms_kv8_attention(q, codes, scales, out, seg_start, *, block, seg_req=None, c
         if workspace.device != dev or not workspace.is_contiguous():
             raise _kv8_bad("workspace must be a contiguous tensor on q's device")
         wp, wb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    with _on_device_of(q):
-        _check(load().ms_kv8_attention(C.byref(c), C.byref(sel), C.byref(a), wp, wb, _stream(stream)))
+    _kv8_run(load().ms_kv8_attention, q, stream, C.byref(c), C.byref(sel), C.byref(a), wp, wb)
 
 
 KERNEL_CLASSES = ("compact", "gather", "layernorm", "gemm_qkv", "attention", "gemm_out", "gemm_up",
