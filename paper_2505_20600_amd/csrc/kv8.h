@@ -90,7 +90,7 @@ struct Kv8AttnDesc {
     long kv_rows;               // rows of kv
     int f_list;                 // entries of the list
     float scale_log2;           // log2(e) times the score scale
-    bool few;                   // the form for few query slots (bf16)
+    int tile;                   // query slots per workgroup: 16, or in bf16 32 or 128
     int nsplit;                 // key ranges; > 1: partials in part_o / part_ml
     float* part_o;              // [nsplit][M][heads * group * hd], each range's output over its own sum
     float* part_ml;             // [nsplit][M][heads * group][2]: its maximum (log2 domain) and sum

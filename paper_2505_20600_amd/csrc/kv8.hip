@@ -70,15 +70,24 @@ __device__ __forceinline__ vec16 load_stream(const void* p) {
 __device__ __forceinline__ void store_stream(void* p, const vec16& v) {
     __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), static_cast<u32x4_t*>(p));
 }
+// (the empty statement keeps the compiler from making one ordinary store of the two)
 __device__ __forceinline__ void store_codes(uint32_t* p, const uint32_t (&w)[1], bool stream) {
-    if (stream) __builtin_nontemporal_store(w[0], p);
-    else *p = w[0];
+    if (stream) {
+        __builtin_nontemporal_store(w[0], p);
+    } else {
+        asm volatile("");
+        *p = w[0];
+    }
 }
 __device__ __forceinline__ void store_codes(uint32_t* p, const uint32_t (&w)[2], bool stream) {
     typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
     const u32x2_t v = {w[0], w[1]};
-    if (stream) __builtin_nontemporal_store(v, reinterpret_cast<u32x2_t*>(p));
-    else *reinterpret_cast<u32x2_t*>(p) = v;
+    if (stream) {
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x2_t*>(p));
+    } else {
+        asm volatile("");
+        *reinterpret_cast<u32x2_t*>(p) = v;
+    }
 }
 
 // A workgroup takes NV rows per wave of a cache (a block of tokens or, of small blocks,

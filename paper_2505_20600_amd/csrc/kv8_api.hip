@@ -104,7 +104,7 @@ ms_status check_attn(const ms_kv8_cache* c, const ms_kv8_select* sel, const ms_k
     d->kv_rows = a->fresh ? a->fresh_rows : 0;
     d->f_list = (int)entries;
     d->scale_log2 = (float)(1.4426950408889634 * (a->scale != 0.f ? (double)a->scale : 1.0 / std::sqrt((double)c->head_dim)));
-    d->few = true;
+    d->tile = 16;
     d->nsplit = 1;
     d->part_o = d->part_ml = nullptr;
     return MS_OK;

@@ -315,8 +315,9 @@ struct FreshDma {
 // The four waves' sums of 16 slots, each relative to its own maximum (so [wave][slot][OLD]
 // and sml [wave][slot]), to the output or the key range's part.
 template <typename T, int HD, int OLD>
-__device__ __forceinline__ void join_waves(const Kv8AttnDesc& a, const Work& w, const float* so, const float2* sml, int tid) {
-    const int s = tid / 16, slot = w.q0 + s;
+__device__ __forceinline__ void join_waves(const Kv8AttnDesc& a, const Work& w, const float* so, const float2* sml, int tid,
+                                           int slot) {
+    const int s = tid / 16;
     if (slot >= w.slots) return;
     float m = -INFINITY, f[4], sum = 0.f;
 #pragma unroll
@@ -346,15 +347,18 @@ __device__ __forceinline__ void join_waves(const Kv8AttnDesc& a, const Work& w, 
 
 // Workgroups of the SHARED form that the registers let a CU hold.
 constexpr int shared_per_cu(int hd) { return hd <= 16 ? 4 : hd <= 72 ? 3 : 2; }
+// The same of the forms for few slots.
+constexpr int few_per_cu(int hd, int slots) { return slots == 16 ? (hd <= 48 || hd == 64 ? 4 : hd <= 80 ? 3 : 2) : hd <= 32 ? 4 : hd <= 64 ? 3 : 2; }
 
 // bf16. SHARED: 128 query slots, 32 per wave, the four waves share 64-key tiles
 // in two stages. Not SHARED: 16 slots, every wave has key tiles of its own (32
 // keys, tile t0 + wave + 4 i) and the four partial results are joined at the end.
-template <int HD, bool SHARED>
+template <int HD, int QT_>
 struct Bf16Cfg {
+    static constexpr int QT = QT_;
+    static constexpr bool SHARED = QT == 128;
     static constexpr int KT = SHARED ? 64 : 32;
-    static constexpr int NQB = SHARED ? 2 : 1;          // 16-slot blocks per wave
-    static constexpr int QT = SHARED ? 128 : 16;
+    static constexpr int NQB = QT == 16 ? 1 : 2;        // 16-slot blocks per wave
     static constexpr int NT = SHARED ? kThreads : kWave;
     static constexpr int STAGES = SHARED ? 2 : 1;
     using S = Stager<HD, KT, NT, false>;
@@ -368,9 +372,10 @@ struct Bf16Cfg {
     static constexpr int LDSB = (SHARED ? STAGES : 4) * S::STAGEB;
 };
 
-template <int HD, bool SHARED>
-__global__ __launch_bounds__(kThreads, SHARED ? shared_per_cu(HD) : HD <= 48 || HD == 64 ? 4 : HD <= 80 ? 3 : 2) void attend_bf16_kernel(Kv8AttnDesc a, int qtiles) {
-    using C = Bf16Cfg<HD, SHARED>;
+template <int HD, int QT>
+__global__ __launch_bounds__(kThreads, QT == 128 ? shared_per_cu(HD) : few_per_cu(HD, QT)) void attend_bf16_kernel(Kv8AttnDesc a, int qtiles) {
+    using C = Bf16Cfg<HD, QT>;
+    constexpr bool SHARED = C::SHARED;
     using S = typename C::S;
     constexpr int NQB = C::NQB, NKS = C::NKS;
     __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDSB + 16];
@@ -720,24 +725,28 @@ __global__ __launch_bounds__(kThreads, SHARED ? shared_per_cu(HD) : HD <= 48 || 
             }
         }
     } else {
-        // the four waves' sums, each relative to its own maximum, joined through LDS
+        // the four waves' sums, each relative to its own maximum, joined through LDS 16 slots at a time
         constexpr int OLD = HD + 4;
         float* const so = reinterpret_cast<float*>(smem);
         float2* const sml = reinterpret_cast<float2*>(so + 4 * 16 * OLD);
         static_assert((4 * 16 * OLD + 4 * 16 * 2) * 4 <= C::LDSB, "join fits the stages");
 #pragma unroll
-        for (int h = 0; h < C::NREAL; ++h) {
-            const int cidx = h * 16 + grp * 4;
-            if (cidx < HD) {
-                float v[4];
+        for (int qb = 0; qb < NQB; ++qb) {
+            if (qb > 0) __syncthreads();
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = oacc[0][h][r];
-                store4<float>(so + (wave * 16 + l16) * OLD + cidx, v);
+            for (int h = 0; h < C::NREAL; ++h) {
+                const int cidx = h * 16 + grp * 4;
+                if (cidx < HD) {
+                    float v[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = oacc[qb][h][r];
+                    store4<float>(so + (wave * 16 + l16) * OLD + cidx, v);
+                }
             }
+            if (grp == 0) sml[wave * 16 + l16] = make_float2(m_run[qb] * cs, l[qb]);
+            __syncthreads();
+            join_waves<bf16_t, HD, OLD>(a, w, so, sml, tid, w.q0 + qb * 16 + tid / 16);
         }
-        if (grp == 0) sml[wave * 16 + l16] = make_float2(m_run[0] * cs, l[0]);
-        __syncthreads();
-        join_waves<bf16_t, HD, OLD>(a, w, so, sml, tid);
     }
 }
 
@@ -950,7 +959,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_f32_kernel(Kv8AttnDesc a) 
     }
     if (grp == 0) sml[wave * 16 + l16] = make_float2(m_run, l);
     __syncthreads();
-    join_waves<float, HD, OLD>(a, w, so, sml, tid);
+    join_waves<float, HD, OLD>(a, w, so, sml, tid, w.q0 + tid / 16);
 }
 
 // Join of the key ranges: range s has the weight l_s 2^(m_s - m); rows of no
@@ -993,25 +1002,14 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Kv8AttnDesc a) {
     if (lane < CL) store4<T>(static_cast<T*>(a.o) + sr * hd + col * 4, o);
 }
 
-// Whether a bf16 call takes the form for few query slots, whose waves have key tiles of
-// their own: up to 16 slots per segment, up to 32 at short rows, or where all of it is one
-// or two rounds of workgroups. Few / many, 4096 keys: 8 requests of 16, 32, 48 rows of 16 heads
-// of 64 23 / 29, 33 / 33, 48 / 38 us; 4 x 32 rows of 24 heads of 128 47 / 37; 1 x 48, 64 rows
-// of 24 heads of 128 27 / 29, 32 / 28; 128 rows of 12 heads of 64 over 1024 keys 12 / 15.
-bool few_slots(const Kv8AttnDesc& a, long keys) {
-    const long rows = (long)a.M * a.group, segs = std::min(a.nseg, a.M), per = (rows + segs - 1) / segs;
-    return per <= (a.c.hd < 96 ? 32 : 16) || segs * ((per + 15) / 16) * a.c.heads * keys <= 1l << 18;
-}
-
-
-template <bool SHARED>
+template <int QT>
 void launch_bf16(const Kv8AttnDesc& a, hipStream_t s) {
-    const int QT = SHARED ? 128 : 16;
+    // slot tiles, the segments' last ones counted as full
     const int qtiles = (int)std::min<long>((long)a.M * a.group / QT + a.nseg, (long)a.M * a.group);
     const int pairs = qtiles * a.nsplit;
-    const dim3 grid((unsigned)(SHARED ? pairs : (pairs + kXcds - 1) / kXcds * kXcds) * a.c.heads), block(kThreads);
+    const dim3 grid((unsigned)(QT == 128 ? pairs : (pairs + kXcds - 1) / kXcds * kXcds) * a.c.heads), block(kThreads);
     switch (a.c.hd) {
-#define MS_HD(n) case n: hipLaunchKernelGGL((attend_bf16_kernel<n, SHARED>), grid, block, 0, s, a, qtiles); break;
+#define MS_HD(n) case n: hipLaunchKernelGGL((attend_bf16_kernel<n, QT>), grid, block, 0, s, a, qtiles); break;
         MS_HD(8) MS_HD(16) MS_HD(24) MS_HD(32) MS_HD(40) MS_HD(48) MS_HD(56) MS_HD(64)
         MS_HD(72) MS_HD(80) MS_HD(88) MS_HD(96) MS_HD(104) MS_HD(112) MS_HD(120) MS_HD(128)
 #undef MS_HD
@@ -1031,40 +1029,47 @@ void launch_f32(const Kv8AttnDesc& a, hipStream_t s) {
 
 }  // namespace
 
-// Key ranges. Few slots and float32: as many as give every CU two workgroups (one where rows
-// are long and a workgroup alone keeps its CU's loads in flight), of at least 256 keys (128
-// in float32): 8 requests of 16 rows over 4096 keys of 16 heads in 1 / 2 / 4 / 8 / 16 ranges
-// take 26 / 21 / 21 / 23 / 27 us at head_dim 64, 40 / 28 / 25 / 31 / 36 at 72 and 41 / 30 / 34
-// / 38 / 48 at 128; one row of 12 heads of 64 takes 25 us in one range and 9.7 in 16.
-// Many: the count with the least modelled time. Workgroups run in rounds of as many as the
-// registers let a CU hold; a round with k on a CU takes 7 us + 1.5 per further one to start
-// and end and, per 64-key tile, the tile's matrix instructions times (0.0165 + 0.008 k) us;
-// the join a launch and its parts at 5 TB/s.
+// Query slots per workgroup and key ranges: the pair with the least modelled time, from
+// the segments' mean length. `base` workgroups per range of `steps` key steps; up to the
+// `most` that a CU holds run at once, k on the fullest one.
+//  16 and 32 slots (waves with key tiles of their own): a step is 128 keys and takes 0.011 us
+//   per column of head_dim, a quarter more where rows are not whole 16-byte chunks, whatever
+//   the slots: staging bounds it. Steps of workgroups on one CU add up. float32: 0.016 us,
+//   its matrix instructions.
+//  128 slots: a step is 64 keys; k workgroups take the tile's matrix instructions times
+//   (0.0165 + 0.008 k) us together, and 10 us to start and end instead of 7.
+//  More than one range: the join's launch, and the parts written and read at 5 TB/s.
+// Measured in us at the best count of ranges of 1 to 16, 16 / 32 / 128 slots: 8 requests over
+// 4096 keys of 16 heads of 64, 16 rows each 22 / 23 / 29, 32 rows 29 / 24 / 33, 64 rows 47 / 33 /
+// 37, 128 rows - / 52 / 46; 4 over 24 heads of 128, 32 rows 43 / 32 / 42, 96 rows - / 69 / 55; one of
+// 128 rows over 1024 keys of 12 heads of 64 - / 12 / 14. Ranges: 8 x 16 rows of 16 heads of 72
+// in 1 / 2 / 4 / 8 / 16 take 40 / 28 / 25 / 31 / 36, one row of 12 heads of 64 25 in one and 10 in 12;
+// 8 x 123 to 2458 rows of 16 heads of 72 in 1 / 2 / 3 232 / 253 / 257.
 void plan_kv8_attention(int dtype, Kv8AttnDesc& a, long keys) {
-    a.few = true;
+    a.tile = 16;
     a.nsplit = 1;
     if (a.M == 0) return;
     const int heads = a.c.heads, hd = a.c.hd;
     const long rows = (long)a.M * a.group, segs = std::min(a.nseg, a.M), per = (rows + segs - 1) / segs;
-    a.few = dtype != kBF16 || few_slots(a, keys);
-    if (a.few) {
-        const long base = segs * ((per + 15) / 16) * heads, target = hd < 96 ? 512 : 256, least = dtype == kBF16 ? 256 : 128;
-        a.nsplit = (int)std::max<long>(1, std::min<long>({(target + base - 1) / base, (keys + least - 1) / least, kMaxRanges}));
-        return;
-    }
-    const long base = segs * ((per + 127) / 128) * heads, tiles = (keys + 63) / 64;
-    const int per_cu = shared_per_cu(hd);
-    const double unit = 8 * ((hd + 31) / 32) + 4 * ((hd + 15) / 16 + (hd % 16 == 0));
+    const double mfmas = 8 * ((hd + 31) / 32) + 4 * ((hd + 15) / 16 + (hd % 16 == 0));
     double least = 1e30;
-    for (int n = 1; n <= std::min<long>(tiles, kMaxRanges); ++n) {
-        const long groups = base * n, slots = 256l * per_cu, rest = groups % slots;
-        auto round_us = [&](long k) { return (tiles + n - 1) / n * unit * (0.0165 + 0.008 * k) + 7.0 + 1.5 * (k - 1); };
-        double us = (double)(groups / slots) * round_us(per_cu);
-        if (rest) us += round_us((rest + 255) / 256);
-        if (n > 1) us += 3.0 + (4.0 * n + 2) * rows * heads * hd / 5.0e6;
-        if (us < least) {
-            least = us;
-            a.nsplit = n;
+    for (int tile : {16, 32, 128}) {
+        if (tile > 16 && (dtype != kBF16 || per <= tile / 2)) break;
+        const long base = segs * ((per + tile - 1) / tile) * heads;
+        const long steps = std::max(1l, tile == 128 ? (keys + 63) / 64 : (keys + 127) / 128);
+        const int most = tile == 128 ? shared_per_cu(hd) : dtype == kBF16 ? few_per_cu(hd, tile) : 2;
+        for (int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (n > steps || n > kMaxRanges) break;
+            const long groups = base * n, slots = 256l * most, k = std::min((groups + 255) / 256, (long)most);
+            const double step = tile == 128 ? mfmas * (0.0165 + 0.008 * k) : k * hd * (dtype != kBF16 ? 0.016 : hd % 16 ? 0.0137 : 0.011);
+            const double round = (steps + n - 1) / n * step;    // as many as run at once
+            double us = (tile == 128 ? 10.0 : 7.0) + (groups > slots ? round * ((double)groups / slots + 0.25) : round);
+            if (n > 1) us += 3.0 + (8.0 * n + 2) * rows * heads * hd / 5.0e6;
+            if (us < least) {
+                least = us;
+                a.tile = tile;
+                a.nsplit = n;
+            }
         }
     }
 }
@@ -1072,8 +1077,9 @@ void plan_kv8_attention(int dtype, Kv8AttnDesc& a, long keys) {
 hipError_t launch_kv8_attention(int dtype, const Kv8AttnDesc& a, hipStream_t s) {
     if (a.M == 0) return hipSuccess;
     if (dtype == kBF16) {
-        if (a.few) launch_bf16<false>(a, s);
-        else launch_bf16<true>(a, s);
+        if (a.tile == 16) launch_bf16<16>(a, s);
+        else if (a.tile == 32) launch_bf16<32>(a, s);
+        else launch_bf16<128>(a, s);
     } else {
         launch_f32(a, s);
     }
