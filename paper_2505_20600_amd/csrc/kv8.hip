@@ -70,24 +70,14 @@ __device__ __forceinline__ vec16 load_stream(const void* p) {
 __device__ __forceinline__ void store_stream(void* p, const vec16& v) {
     __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), static_cast<u32x4_t*>(p));
 }
-// (the empty statement keeps the compiler from making one ordinary store of the two)
-__device__ __forceinline__ void store_codes(uint32_t* p, const uint32_t (&w)[1], bool stream) {
-    if (stream) {
-        __builtin_nontemporal_store(w[0], p);
-    } else {
-        asm volatile("");
-        *p = w[0];
-    }
-}
-__device__ __forceinline__ void store_codes(uint32_t* p, const uint32_t (&w)[2], bool stream) {
-    typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-    const u32x2_t v = {w[0], w[1]};
-    if (stream) {
-        __builtin_nontemporal_store(v, reinterpret_cast<u32x2_t*>(p));
-    } else {
-        asm volatile("");
-        *reinterpret_cast<u32x2_t*>(p) = v;
-    }
+template <bool STREAM, int N>
+__device__ __forceinline__ void store_codes(uint32_t* p, const uint32_t (&w)[N]) {
+    typedef uint32_t u32xn_t __attribute__((ext_vector_type(N)));
+    u32xn_t v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = w[i];
+    if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<u32xn_t*>(p));
+    else *reinterpret_cast<u32xn_t*>(p) = v;
 }
 
 // A workgroup takes NV rows per wave of a cache (a block of tokens or, of small blocks,
@@ -99,7 +89,7 @@ __device__ __forceinline__ void store_codes(uint32_t* p, const uint32_t (&w)[2],
 // its 144-byte rows and the values unpacked to float32, took 58 us; loads through the caches 50.
 // Codes go past the caches where a group's row of them is whole 64-byte lines (at head_dim
 // 128 55 -> 51 us; at 72, where neighbouring groups share lines, 44 -> 49).
-template <typename T, int NV, int WAVES, bool REWRITE>
+template <typename T, int NV, int WAVES, bool REWRITE, bool STREAM>
 __global__ __launch_bounds__(WAVES * kWave) void quantize_kernel(Kv8Cache c, const T* __restrict__ kv, long row_stride,
                                                             const int32_t* __restrict__ src_row, long kv_rows,
                                                             int heads_per_group, int groups, int row_groups) {
@@ -118,7 +108,6 @@ __global__ __launch_bounds__(WAVES * kWave) void quantize_kernel(Kv8Cache c, con
     const bool mine = lane < heads * C;
     const int col = which * dkv + head0 * c.hd + lane * CW;
     const int rows = min(R, c.T - t0);
-    const bool stream = heads_per_group * c.hd % 64 == 0;
     uint8_t* const codes = c.codes + ((long)cache * c.T + t0) * 2 * dkv + col;
     uint8_t* const scales = c.scales + ((long)cache * c.blocks + (t0 >> c.lblock)) * 2 * c.heads + which * c.heads + head0 + h;
 
@@ -228,7 +217,7 @@ __global__ __launch_bounds__(WAVES * kWave) void quantize_kernel(Kv8Cache c, con
         } else {
             Piece<T>::encode(v[i], kv8_scale(b), w);
         }
-        store_codes(p, w, stream);
+        store_codes<STREAM>(p, w);
         // the first row of a block, the first lane of a head
         if ((r & ((1 << c.lblock) - 1)) == 0 && lane % C == 0) scales[(long)(r >> c.lblock) * 2 * c.heads] = (uint8_t)b;
     }
@@ -344,22 +333,30 @@ __global__ __launch_bounds__(kScanThreads) void step_lists_kernel(const int32_t*
     }
 }
 
-template <typename T, bool REWRITE>
+template <typename T, bool REWRITE, bool STREAM>
 void launch_quantize(const Kv8Cache& c, const void* kv, long row_stride, const int32_t* src_row, long kv_rows,
-                     hipStream_t s) {
-    // heads in even groups of at most 64 lanes
-    const int most = kWave / (c.hd / Piece<T>::N), groups = (c.heads + most - 1) / most;
-    const int per_group = (c.heads + groups - 1) / groups;
+                     int groups, int per_group, hipStream_t s) {
     const int rows = std::max(1 << c.lblock, 16), row_groups = (c.T + rows - 1) / rows;
     const dim3 grid((unsigned)((long)c.n_caches * row_groups * 2 * groups));
     const T* p = static_cast<const T*>(kv);
 #define MS_ROWS(r, nv, waves)                                                                                          \
-    case r: hipLaunchKernelGGL((quantize_kernel<T, nv, waves, REWRITE>), grid, dim3(waves * kWave), 0, s, c, p, row_stride, \
+    case r: hipLaunchKernelGGL((quantize_kernel<T, nv, waves, REWRITE, STREAM>), grid, dim3(waves * kWave), 0, s, c, p, row_stride, \
                                src_row, kv_rows, per_group, groups, row_groups); break;
     switch (rows) {
         MS_ROWS(16, 4, 4) MS_ROWS(32, 4, 8) MS_ROWS(64, 8, 8) MS_ROWS(128, 8, 16)
     }
 #undef MS_ROWS
+}
+
+template <typename T>
+void launch_quantize(const Kv8Cache& c, const void* kv, long row_stride, const int32_t* src_row, long kv_rows,
+                     hipStream_t s) {
+    // heads in even groups of at most 64 lanes
+    const int most = kWave / (c.hd / Piece<T>::N), groups = (c.heads + most - 1) / most;
+    const int per_group = (c.heads + groups - 1) / groups;
+    if (src_row) launch_quantize<T, true, false>(c, kv, row_stride, src_row, kv_rows, groups, per_group, s);
+    else if (per_group * c.hd % 64 == 0) launch_quantize<T, false, true>(c, kv, row_stride, src_row, kv_rows, groups, per_group, s);
+    else launch_quantize<T, false, false>(c, kv, row_stride, src_row, kv_rows, groups, per_group, s);
 }
 
 }  // namespace
@@ -378,13 +375,8 @@ hipError_t launch_kv8_step_lists(const int32_t* inv, int batch, int N, int n_tex
 
 hipError_t launch_kv8_quantize(int dtype, const Kv8Cache& c, const void* kv, long row_stride, const int32_t* src_row,
                                long kv_rows, hipStream_t s) {
-    if (dtype == kBF16) {
-        if (src_row) launch_quantize<bf16_t, true>(c, kv, row_stride, src_row, kv_rows, s);
-        else launch_quantize<bf16_t, false>(c, kv, row_stride, src_row, kv_rows, s);
-    } else {
-        if (src_row) launch_quantize<float, true>(c, kv, row_stride, src_row, kv_rows, s);
-        else launch_quantize<float, false>(c, kv, row_stride, src_row, kv_rows, s);
-    }
+    if (dtype == kBF16) launch_quantize<bf16_t>(c, kv, row_stride, src_row, kv_rows, s);
+    else launch_quantize<float>(c, kv, row_stride, src_row, kv_rows, s);
     return hipGetLastError();
 }
 
