@@ -68,7 +68,8 @@ ms_status ms_linear(int32_t dtype, int32_t M, int32_t N, int32_t K, const void* 
  * Limits: n_caches 1..2^20; tokens 1..2^20; block a power of two, 1..128;
  * head_dim a multiple of 8, <= 128 (float32: <= 64); n_kv_heads 1..1024; one
  * cache's codes below 4095 MiB; batch and n_seg 1..128; rows x n_heads at
- * most 2^28. */
+ * most 2^27; one ms_kv8_quantize below 2^28 pieces of at most 1 KiB of a K or V
+ * row (whole heads), tokens counted up to whole blocks of at least 16. */
 typedef struct {
     int32_t dtype;          /* ms_dtype */
     int32_t n_caches, tokens, n_kv_heads, head_dim, block;

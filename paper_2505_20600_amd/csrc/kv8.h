@@ -143,6 +143,8 @@ hipError_t launch_kv8_step_lists(const int32_t* inv, int batch, int N, int n_tex
 // K/V rows [..][2][heads * hd] -> codes and scales. src_row NULL: token t of
 // cache c is row c * row_stride + t; else row src_row[c][t] where that lies in
 // [0, kv_rows), and the token keeps its value elsewhere.
+// kv8_quantize_fits: whether one launch can have the whole.
+bool kv8_quantize_fits(int dtype, const Kv8Cache& c);
 hipError_t launch_kv8_quantize(int dtype, const Kv8Cache& c, const void* kv, long row_stride, const int32_t* src_row,
                                long kv_rows, hipStream_t s);
 // kv[b * row_stride + t] = the listed tokens' values.

@@ -333,30 +333,43 @@ __global__ __launch_bounds__(kScanThreads) void step_lists_kernel(const int32_t*
     }
 }
 
+// How a cache is divided among workgroups.
+struct QuantizeGrid {
+    int groups, per_group;      // groups of heads, even ones of at most 64 lanes
+    int rows, row_groups;
+    long workgroups;
+};
+QuantizeGrid quantize_grid(int dtype, const Kv8Cache& c) {
+    QuantizeGrid g;
+    const int most = kWave / (c.hd / (dtype == kBF16 ? Piece<bf16_t>::N : Piece<float>::N));
+    g.groups = (c.heads + most - 1) / most;
+    g.per_group = (c.heads + g.groups - 1) / g.groups;
+    g.rows = std::max(1 << c.lblock, 16);
+    g.row_groups = (c.T + g.rows - 1) / g.rows;
+    g.workgroups = (long)c.n_caches * g.row_groups * 2 * g.groups;
+    return g;
+}
+
 template <typename T, bool REWRITE, bool STREAM>
-void launch_quantize(const Kv8Cache& c, const void* kv, long row_stride, const int32_t* src_row, long kv_rows,
-                     int groups, int per_group, hipStream_t s) {
-    const int rows = std::max(1 << c.lblock, 16), row_groups = (c.T + rows - 1) / rows;
-    const dim3 grid((unsigned)((long)c.n_caches * row_groups * 2 * groups));
+void launch_quantize(const Kv8Cache& c, const QuantizeGrid& g, const void* kv, long row_stride, const int32_t* src_row,
+                     long kv_rows, hipStream_t s) {
+    const dim3 grid((unsigned)g.workgroups);
     const T* p = static_cast<const T*>(kv);
 #define MS_ROWS(r, nv, waves)                                                                                          \
     case r: hipLaunchKernelGGL((quantize_kernel<T, nv, waves, REWRITE, STREAM>), grid, dim3(waves * kWave), 0, s, c, p, row_stride, \
-                               src_row, kv_rows, per_group, groups, row_groups); break;
-    switch (rows) {
+                               src_row, kv_rows, g.per_group, g.groups, g.row_groups); break;
+    switch (g.rows) {
         MS_ROWS(16, 4, 4) MS_ROWS(32, 4, 8) MS_ROWS(64, 8, 8) MS_ROWS(128, 8, 16)
     }
 #undef MS_ROWS
 }
 
 template <typename T>
-void launch_quantize(const Kv8Cache& c, const void* kv, long row_stride, const int32_t* src_row, long kv_rows,
-                     hipStream_t s) {
-    // heads in even groups of at most 64 lanes
-    const int most = kWave / (c.hd / Piece<T>::N), groups = (c.heads + most - 1) / most;
-    const int per_group = (c.heads + groups - 1) / groups;
-    if (src_row) launch_quantize<T, true, false>(c, kv, row_stride, src_row, kv_rows, groups, per_group, s);
-    else if (per_group * c.hd % 64 == 0) launch_quantize<T, false, true>(c, kv, row_stride, src_row, kv_rows, groups, per_group, s);
-    else launch_quantize<T, false, false>(c, kv, row_stride, src_row, kv_rows, groups, per_group, s);
+void launch_quantize(const Kv8Cache& c, const QuantizeGrid& g, const void* kv, long row_stride, const int32_t* src_row,
+                     long kv_rows, hipStream_t s) {
+    if (src_row) launch_quantize<T, true, false>(c, g, kv, row_stride, src_row, kv_rows, s);
+    else if (g.per_group * c.hd % 64 == 0) launch_quantize<T, false, true>(c, g, kv, row_stride, src_row, kv_rows, s);
+    else launch_quantize<T, false, false>(c, g, kv, row_stride, src_row, kv_rows, s);
 }
 
 }  // namespace
@@ -373,10 +386,17 @@ hipError_t launch_kv8_step_lists(const int32_t* inv, int batch, int N, int n_tex
     return hipGetLastError();
 }
 
+// 16 threads or fewer per row of a workgroup: fewer than the 2^32 threads that end a launch.
+bool kv8_quantize_fits(int dtype, const Kv8Cache& c) {
+    const QuantizeGrid g = quantize_grid(dtype, c);
+    return g.workgroups * g.rows < 1l << 28;
+}
+
 hipError_t launch_kv8_quantize(int dtype, const Kv8Cache& c, const void* kv, long row_stride, const int32_t* src_row,
                                long kv_rows, hipStream_t s) {
-    if (dtype == kBF16) launch_quantize<bf16_t>(c, kv, row_stride, src_row, kv_rows, s);
-    else launch_quantize<float>(c, kv, row_stride, src_row, kv_rows, s);
+    const QuantizeGrid g = quantize_grid(dtype, c);
+    if (dtype == kBF16) launch_quantize<bf16_t>(c, g, kv, row_stride, src_row, kv_rows, s);
+    else launch_quantize<float>(c, g, kv, row_stride, src_row, kv_rows, s);
     return hipGetLastError();
 }
 

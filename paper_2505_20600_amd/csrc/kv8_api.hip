@@ -71,7 +71,8 @@ ms_status check_attn(const ms_kv8_cache* c, const ms_kv8_select* sel, const ms_k
     if (a->rows < 0 || a->rows > (1 << 26)) return set_error(MS_ESHAPE, "rows %d outside 0..2^26", a->rows);
     if (a->n_heads < 1 || a->n_heads % c->n_kv_heads || a->n_heads > 1024)
         return set_error(MS_ESHAPE, "n_heads %d must be a multiple of n_kv_heads %d, at most 1024", a->n_heads, c->n_kv_heads);
-    if ((int64_t)a->rows * a->n_heads > (1 << 28)) return set_error(MS_ESHAPE, "rows x n_heads above 2^28");
+    // at most one workgroup per 16 of them, 2^23 of 256 threads: a launch takes fewer than 2^32 threads
+    if ((int64_t)a->rows * a->n_heads > (1 << 27)) return set_error(MS_ESHAPE, "rows x n_heads above 2^27");
     if (a->n_seg < 1 || a->n_seg > ms::kKv8MaxSegments)
         return set_error(MS_ESHAPE, "n_seg %d outside 1..%d", a->n_seg, ms::kKv8MaxSegments);
     if (!a->seg_req && a->n_seg > sel->batch) return set_error(MS_ESHAPE, "n_seg %d above batch %d needs seg_req", a->n_seg, sel->batch);
@@ -104,6 +105,7 @@ ms_status check_attn(const ms_kv8_cache* c, const ms_kv8_select* sel, const ms_k
     d->kv_rows = a->fresh ? a->fresh_rows : 0;
     d->f_list = (int)entries;
     d->scale_log2 = (float)(1.4426950408889634 * (a->scale != 0.f ? (double)a->scale : 1.0 / std::sqrt((double)c->head_dim)));
+    if (!std::isfinite(d->scale_log2)) return set_error(MS_EINVAL, "scale too large");
     d->tile = 16;
     d->nsplit = 1;
     d->part_o = d->part_ml = nullptr;
@@ -152,6 +154,9 @@ ms_status ms_kv8_quantize(const ms_kv8_cache* c, const void* kv, int64_t kv_rows
                      (int64_t)(c->n_caches - 1) * row_stride + c->tokens > kv_rows))
         return set_error(MS_ESHAPE, "row_stride %lld: need at least tokens, and %d caches of it within %lld rows",
                          (long long)row_stride, c->n_caches, (long long)kv_rows);
+    if (!ms::kv8_quantize_fits(c->dtype, k))
+        return set_error(MS_ESHAPE, "%d caches of %d tokens of %d heads are too many for one call", c->n_caches, c->tokens,
+                         c->n_kv_heads);
     hipError_t e = ms::launch_kv8_quantize(c->dtype, k, kv, row_stride, src_row, kv_rows, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return set_error(MS_EHIP, "quantize launch: %s", hipGetErrorString(e));
     return ms::clear_error();

@@ -614,3 +614,55 @@ def test_binding_refusals_on_the_gpu():
             f()
     torch.cuda.synchronize()
     assert bool((codes == 0x55).all()) and bool((scales == 0x55).all())
+
+
+@pytest.mark.parametrize("dtype,H,hd", [("bf16", 31, 128), ("fp32", 62, 64)])
+@pytest.mark.parametrize("rows", [2, 300])
+def test_attention_at_the_end_of_the_largest_cache(dtype, H, hd, rows):
+    """One cache of 3968 MiB of codes: row offsets just below 2^32."""
+    T, block, n = 1 << 19, 64, 200
+    codes = torch.zeros(1, T, 2, H, hd, dtype=torch.uint8, device=DEV)
+    scales = torch.full((1, T // block, 2, H), 127, dtype=torch.uint8, device=DEV)
+    g = torch.Generator().manual_seed(19)
+    kv = _rows(g, (1, 256, 2, H, hd), dtype)
+    MS.ms_kv8_quantize(kv, codes[:, T - 256:], scales[:, -256 // block:], block=block)
+    c, e = _oracle_cache(kv, block)
+    k = kv8.values(c[0], e[0], block)[256 - n:]
+    q = torch.randn(rows, H, hd, generator=g).to(DT[dtype]).to(DEV)
+    keys = torch.arange(T - n, T, dtype=torch.int32, device=DEV)[None]
+    out, start = torch.zeros_like(q), torch.tensor([0, rows], dtype=torch.int32, device=DEV)
+    MS.ms_kv8_attention(q, codes, scales, out, start, block=block, keys=keys)
+    ref, spread = kv8.attention(_np(q), k[:, 0], k[:, 1], hd ** -0.5)
+    assert np.all(np.abs(_np(out) - ref) <= _bound(q, k, ref, spread, hd ** -0.5, dtype))
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured calls with one workspace, replayed in turn on one stream: the bits of each alone."""
+    g = torch.Generator().manual_seed(20)
+    codes, scales = _cache(g, 2, 3000, 4, 64, 64, "bf16")
+    calls, need = [], 0
+    for rows in (3, 40):
+        q = torch.randn(2 * rows, 4, 64, generator=g).bfloat16().to(DEV)
+        start = torch.tensor([0, rows, 2 * rows], dtype=torch.int32, device=DEV)
+        need = max(need, MS.ms_kv8_attention_workspace_bytes(q, codes, start))
+        calls.append((q, start, torch.zeros_like(q)))
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    graphs, alone = [], []
+    for q, start, out in calls:
+        MS.ms_kv8_attention(q, codes, scales, out, start, block=64, workspace=ws)
+        torch.cuda.synchronize()
+        alone.append(out.clone())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            MS.ms_kv8_attention(q, codes, scales, out, start, block=64, workspace=ws)
+        graphs.append(graph)
+    for _ in range(3):
+        for _, _, out in calls:
+            out.zero_()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (_, _, out), want in zip(calls, alone):
+            assert torch.equal(out, want)
+        ws.fill_(0xFF)

@@ -49,7 +49,7 @@ BAD_SELECT = [
 ]
 BAD_ATTN = [
     (dict(rows=-1), MS.MS_ESHAPE), (dict(rows=(1 << 26) + 1), MS.MS_ESHAPE),
-    (dict(rows=(1 << 25) + 1), MS.MS_ESHAPE),                        # x 8 heads above 2^28
+    (dict(rows=(1 << 24) + 1), MS.MS_ESHAPE),                        # x 8 heads above 2^27
     (dict(n_heads=0), MS.MS_ESHAPE), (dict(n_heads=6), MS.MS_ESHAPE), (dict(n_heads=2048), MS.MS_ESHAPE),
     (dict(n_seg=0), MS.MS_ESHAPE), (dict(n_seg=129, seg_req=P), MS.MS_ESHAPE), (dict(n_seg=3), MS.MS_ESHAPE),
     (dict(q=None), MS.MS_EINVAL), (dict(out=None), MS.MS_EINVAL), (dict(seg_start=None), MS.MS_EINVAL),
@@ -58,6 +58,7 @@ BAD_ATTN = [
     (dict(fresh_list=P + 1), MS.MS_EALIGN),
     (dict(fresh_start=None), MS.MS_EINVAL), (dict(fresh_rows=-1), MS.MS_ESHAPE), (dict(fresh_list=P, fresh_entries=-1), MS.MS_ESHAPE),
     (dict(scale=float("nan")), MS.MS_EINVAL), (dict(scale=float("inf")), MS.MS_EINVAL),
+    (dict(scale=3e38), MS.MS_EINVAL),                                # x log2 e is no float32
 ]
 _id = lambda v: "-".join(f"{k}={x}" for k, x in v.items()) if isinstance(v, dict) else str(v)
 
@@ -114,6 +115,18 @@ def test_null_descriptions_rows_and_strides_are_refused():
                                             (P, 1, 8, P, 7, P, MS.MS_ESHAPE), (P, 1, 8, None, 8, P, MS.MS_EINVAL),
                                             (P, 1, 8, P, 8, None, MS.MS_EINVAL), (P, 1, 8, P + 1, 8, P, MS.MS_EALIGN)):
         assert lib.ms_kv8_keys(mask, b, t, keys, ld, n, None) == status
+
+
+@pytest.mark.parametrize("dtype,block,caches,tokens", [(MS.MS_BF16, 1, 1 << 20, 1), (MS.MS_BF16, 128, 1 << 17, 128),
+                                                       (MS.MS_FP32, 32, 1 << 18, 31)])
+def test_more_than_one_launch_can_write_is_refused(dtype, block, caches, tokens):
+    """At 1024 heads of 8: 16 (bf16) or 32 (float32) KiB-pieces per row, K and V, tokens up to whole blocks of 16 or more."""
+    lib = MS.load()
+    at = _cache(dtype=dtype, n_caches=caches, tokens=tokens, n_kv_heads=1024, head_dim=8, block=block)
+    assert caches * 2 * (16 if dtype == MS.MS_BF16 else 32) * max(16, block) >= 1 << 28
+    for src in (None, P):
+        assert lib.ms_kv8_quantize(C.byref(at), P, 1 << 30, tokens, src, None) == MS.MS_ESHAPE
+        assert b"one call" in lib.mask_last_error()
 
 
 def test_no_rows_is_not_an_error():
