@@ -14,6 +14,7 @@
 // ds_read_b64_tr_b16, rows of ones in V^T give the denominator. Absent keys
 // (past a list's end, numbers out of range) are zero rows with score -inf.
 #include <algorithm>
+#include <cmath>
 
 #include "attn_tiles.h"
 #include "kernels.h"
@@ -1029,18 +1030,21 @@ void launch_f32(const Kv8AttnDesc& a, hipStream_t s) {
 
 }  // namespace
 
-// Query slots per workgroup and key ranges: the pair with the least modelled time, from
-// the segments' mean length. `base` workgroups per range of `steps` key steps; up to the
-// `most` that a CU holds run at once, k on the fullest one.
-//  16 and 32 slots (waves with key tiles of their own): a step is 128 keys and takes 0.011 us
-//   per column of head_dim, a quarter more where rows are not whole 16-byte chunks, whatever
-//   the slots: staging bounds it. Steps of workgroups on one CU add up. float32: 0.016 us,
-//   its matrix instructions.
+// Query slots per workgroup and key ranges: the pair with the least modelled time, from the
+// segments' mean length (how many slot tiles ragged segments fill: half a tile more each than
+// rows / tile). `base` workgroups per range of `steps` key steps; up to the `most` that a CU
+// holds run at once, k on the fullest one.
+//  16 and 32 slots (waves with key tiles of their own): a step is 128 keys and takes 0.0015 +
+//   0.009 k us per column of head_dim, a quarter more where rows are not whole 16-byte
+//   chunks, whatever the slots: staging bounds it. float32: 0.016 k, its matrix instructions.
 //  128 slots: a step is 64 keys; k workgroups take the tile's matrix instructions times
-//   (0.0165 + 0.008 k) us together, and 10 us to start and end instead of 7.
-//  More than one range: the join's launch, and the parts written and read at 5 TB/s.
-// Measured in us at the best count of ranges of 1 to 16, 16 / 32 / 128 slots: 8 requests over
-// 4096 keys of 16 heads of 64, 16 rows each 22 / 23 / 29, 32 rows 29 / 24 / 33, 64 rows 47 / 33 /
+//   (0.014 + 0.010 k) us together, and a longer start and end.
+//  No less than the codes' bytes at 4.5 TB/s. More than one range: the join's launch, and the
+//  parts written and read.
+// Fitted to 5159 measured times (16 shapes of 1 to 64 requests of 500 to 16000 keys, head_dim 32 to
+// 128, 1 to 1600 rows, equal and ragged, every form, 1 to 64 ranges): the chosen pair takes 1.06
+// times the fastest on average. In us at the best count of ranges, 16 / 32 / 128 slots: 8 requests
+// over 4096 keys of 16 heads of 64, 16 rows each 22 / 23 / 29, 32 rows 29 / 24 / 33, 64 rows 47 / 33 /
 // 37, 128 rows - / 52 / 46; 4 over 24 heads of 128, 32 rows 43 / 32 / 42, 96 rows - / 69 / 55; one of
 // 128 rows over 1024 keys of 12 heads of 64 - / 12 / 14. Ranges: 8 x 16 rows of 16 heads of 72
 // in 1 / 2 / 4 / 8 / 16 take 40 / 28 / 25 / 31 / 36, one row of 12 heads of 64 25 in one and 10 in 12;
@@ -1052,19 +1056,22 @@ void plan_kv8_attention(int dtype, Kv8AttnDesc& a, long keys) {
     const int heads = a.c.heads, hd = a.c.hd;
     const long rows = (long)a.M * a.group, segs = std::min(a.nseg, a.M), per = (rows + segs - 1) / segs;
     const double mfmas = 8 * ((hd + 31) / 32) + 4 * ((hd + 15) / 16 + (hd % 16 == 0));
+    const double bytes = 2.0 * segs * keys * heads * hd / 4.5e6;
     double least = 1e30;
     for (int tile : {16, 32, 128}) {
-        if (tile > 16 && (dtype != kBF16 || per <= tile / 2)) break;
-        const long base = segs * ((per + tile - 1) / tile) * heads;
+        if (tile > 16 && (dtype != kBF16 || per <= tile / 4)) break;
+        const double tiles = segs == 1 ? (double)((per + tile - 1) / tile) : segs * std::max(1.0, (double)(per - 1) / tile + 0.5);
+        const double base = tiles * heads;
         const long steps = std::max(1l, tile == 128 ? (keys + 63) / 64 : (keys + 127) / 128);
         const int most = tile == 128 ? shared_per_cu(hd) : dtype == kBF16 ? few_per_cu(hd, tile) : 2;
         for (int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (n > steps || n > kMaxRanges) break;
-            const long groups = base * n, slots = 256l * most, k = std::min((groups + 255) / 256, (long)most);
-            const double step = tile == 128 ? mfmas * (0.0165 + 0.008 * k) : k * hd * (dtype != kBF16 ? 0.016 : hd % 16 ? 0.0137 : 0.011);
+            const double groups = base * n, slots = 256.0 * most, k = std::min(std::ceil(groups / 256), (double)most);
+            const double step = tile == 128 ? mfmas * (0.014 + 0.010 * k)
+                : dtype != kBF16 ? k * hd * 0.016 : (hd * (hd % 16 ? 1.25 : 1.0) + 2) * (0.0015 + 0.009 * k);
             const double round = (steps + n - 1) / n * step;    // as many as run at once
-            double us = (tile == 128 ? 10.0 : 7.0) + (groups > slots ? round * ((double)groups / slots + 0.25) : round);
-            if (n > 1) us += 3.0 + (8.0 * n + 2) * rows * heads * hd / 5.0e6;
+            double us = (tile == 128 ? 10.5 : 7.3) + std::max(bytes, groups > slots ? round * (groups / slots + 0.25) : round);
+            if (n > 1) us += 2.6 + (8.0 * n + 2) * rows * heads * hd / 2.7e6;
             if (us < least) {
                 least = us;
                 a.tile = tile;
