@@ -13,6 +13,9 @@
 // weights in the operand layout of O^T = V^T P^T, V is read transposed by
 // ds_read_b64_tr_b16, rows of ones in V^T give the denominator. Absent keys
 // (past a list's end, numbers out of range) are zero rows with score -inf.
+// Scores, maxima, sums and the parts of key ranges are float32. bf16 rounds
+// twice: the weights, the matrix cores' operand of the second product (both
+// numerator and denominator take the rounded ones), and the output.
 #include <algorithm>
 #include <cmath>
 
@@ -351,9 +354,17 @@ constexpr int shared_per_cu(int hd) { return hd <= 16 ? 4 : hd <= 72 ? 3 : 2; }
 // The same of the forms for few slots.
 constexpr int few_per_cu(int hd, int slots) { return slots == 16 ? (hd <= 48 || hd == 64 ? 4 : hd <= 80 ? 3 : 2) : hd <= 32 ? 4 : hd <= 64 ? 3 : 2; }
 
-// bf16. SHARED: 128 query slots, 32 per wave, the four waves share 64-key tiles
-// in two stages. Not SHARED: 16 slots, every wave has key tiles of its own (32
-// keys, tile t0 + wave + 4 i) and the four partial results are joined at the end.
+// bf16. SHARED: 128 query slots, 32 per wave; the four waves share 64-key tiles in two stages, so
+// that a key is converted once for 128 slots. Bound by the waves' own work on a tile (converting,
+// softmax, products, each a sixth to a third of it, and little of one wave's under another's): 8
+// requests of 123 to 2458 rows over 4096 keys of 16 heads of 72 (129 GFLOP) 215 to 230 us, 4 of 922
+// to 2150 rows over 4608 keys of 24 heads of 128 (327 GFLOP) 375 us, 0.6 and 0.87 PFLOP/s; the
+// matrix cores are busy 37% and 44% of the time. 256 slots (eight waves) gained 3 to 7% on long
+// segments and lost more on short ones.
+// Not SHARED: 16 or 32 slots, all of them in every wave, and every wave has key tiles of its own (32
+// keys, tile t0 + wave + 4 i); the four partial results are joined at the end. Bound by the way of
+// the codes through registers and LDS: 8 requests of 4 to 48 rows over 4096 keys of 16 heads of 72
+// (77 MB, not in a cache) 30 us, 2.5 TB/s; 24 requests over 4096 keys of 16 heads of 64 4.5 TB/s.
 template <int HD, int QT_>
 struct Bf16Cfg {
     static constexpr int QT = QT_;
@@ -850,6 +861,10 @@ struct StagerF32 {
     }
 };
 
+// float32: 16 query slots in every wave, 32-key tiles of its own per wave as in the bf16 forms for
+// few slots, products on the float32 matrix instructions. Bound by them and by the staging in
+// turn at few rows: 205 rows of 4 heads of 64 over 1024 keys (0.21 GFLOP) 14.5 us with the join, of
+// which two launches are 8; two workgroups per CU hold 70 KB of LDS each.
 template <int HD>
 __global__ __launch_bounds__(kThreads, 2) void attend_f32_kernel(Kv8AttnDesc a) {
     using S = StagerF32<HD, false>;
