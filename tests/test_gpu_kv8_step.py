@@ -237,3 +237,40 @@ def test_refusals():
                                       None) == MS.MS_EINVAL
     torch.cuda.synchronize()
     assert bool((run.y == 3.0).all())
+
+
+@pytest.mark.parametrize("block", [1, 32, 128])
+def test_more_tokens_than_one_pass_of_the_lists(block, monkeypatch):
+    """1600 image tokens and 9 of text: the lists of cached and fresh tokens take several passes; every size of block."""
+    monkeypatch.setattr(f"{__name__}.BLOCK", block)
+    shape = W.ModelShape("k8_1600", 2, 128, 2, 4, 40, 40, n_text=9, dtype="bf16", batch=2)
+    ws, xt, codes, scales, kv, yc = _inputs(shape, 89)
+    mask = _masks(shape, (0.5, 0.05), 12)
+    x = W.edited_hidden(shape, 89, xt, mask)
+    y = Run(shape, mask, x, codes, scales, yc, ws).out()
+    G.assert_close(y, oracle.masked_stack(x, mask, kv, yc, ws, shape, round_p=True), "bf16", f"1600 tokens, block {block}",
+                   blocks=shape.n_layers, inp=x)
+    np.testing.assert_array_equal(Run(shape, mask, x, codes, scales, yc, ws, pinned=True).out(), y)
+
+
+def test_largest_batch():
+    """64 requests with two streams, 128 packed segments, masks of 0 to 100% in turn."""
+    shape = W.ModelShape("k8_b64", 1, 128, 2, 4, 8, 8, n_text=5, dual_stream=True, dtype="bf16", batch=64)
+    ws, xt, codes, scales, kv, yc = _inputs(shape, 90)
+    mask = _masks(shape, [(0.0, 0.1, 0.5, 1.0)[b % 4] for b in range(64)], 13)
+    x = W.edited_hidden(shape, 90, xt, mask)
+    y = Run(shape, mask, x, codes, scales, yc, ws).out()
+    G.assert_close(y, oracle.masked_stack(x, mask, kv, yc, ws, shape, round_p=True), "bf16", "64 requests", blocks=1, inp=x)
+
+
+def test_a_cache_number_out_of_range_is_no_cache():
+    """Its request attends over its own fresh rows; the other one is as it was."""
+    shape = SHAPES[2]
+    ws, xt, codes, scales, kv, yc = _inputs(shape, 91)
+    mask = _masks(shape, (0.3, 0.2), 14)
+    x = W.edited_hidden(shape, 91, xt, mask)
+    want = Run(shape, mask, x, codes, scales, yc, ws).out()
+    for bad in (2, -1, 2 ** 31 - 1):
+        y = Run(shape, mask, x, codes, scales, yc, ws, cache_of=(bad, 1)).out()
+        np.testing.assert_array_equal(y[1], want[1])
+        assert np.isfinite(y[0]).all() and not np.array_equal(y[0], want[0])
