@@ -88,16 +88,17 @@ __device__ __forceinline__ void store_codes(uint32_t* p, const uint32_t (&w)[N])
 // 4 of 24 heads of 128 (302 MB) 51 us, 5.1 and 5.9 TB/s. A wave per (block, head) tile, lanes over
 // its 144-byte rows and the values unpacked to float32, took 58 us; loads through the caches 50.
 // Codes go past the caches where a group's row of them is whole 64-byte lines (at head_dim
-// 128 55 -> 51 us; at 72, where neighbouring groups share lines, 44 -> 49). Rewriting
-// 410 of one cache's 4096 tokens of 16 heads of 72 takes 11 us where a whole write takes 8: the
-// rows' bookkeeping, not bytes, bounds it.
+// 128 55 -> 51 us; at 72, where neighbouring groups share lines, 44 -> 49).
+// Rewriting 410 of one cache's 4096 tokens of 16 heads of 72 takes 10 us: two loads one after the
+// other (which row, then the row), three barriers and the stores, on few workgroups; a fifth of
+// the tokens of 8 such caches, every block of them touched, 48.
 template <typename T, int NV, int WAVES, bool REWRITE, bool STREAM>
 __global__ __launch_bounds__(WAVES * kWave) void quantize_kernel(Kv8Cache c, const T* __restrict__ kv, long row_stride,
                                                             const int32_t* __restrict__ src_row, long kv_rows,
                                                             int heads_per_group, int groups, int row_groups) {
     constexpr int CW = Piece<T>::N, R = WAVES * NV, kGroup = WAVES * kWave;
     __shared__ uint32_t s_max[R][kWave];    // [block of the rows][head of the group]
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     unsigned at = blockIdx.x;
     const int group = at % groups;
     at /= groups;
@@ -357,11 +358,13 @@ void launch_quantize(const Kv8Cache& c, const QuantizeGrid& g, const void* kv, l
                      long kv_rows, hipStream_t s) {
     const dim3 grid((unsigned)g.workgroups);
     const T* p = static_cast<const T*>(kv);
+    // a rewrite does more per row: blocks of 64 by 16 waves of four rows, not 8 of eight (one cache of 4096
+    // tokens of 16 heads of 72, half of them new 7.3 instead of 8.8 us, all of them 11.1 instead of 12.7)
 #define MS_ROWS(r, nv, waves)                                                                                          \
-    case r: hipLaunchKernelGGL((quantize_kernel<T, nv, waves, REWRITE, STREAM>), grid, dim3(waves * kWave), 0, s, c, p, row_stride, \
+    case r: hipLaunchKernelGGL((quantize_kernel<T, (nv), (waves), REWRITE, STREAM>), grid, dim3((waves) * kWave), 0, s, c, p, row_stride, \
                                src_row, kv_rows, g.per_group, g.groups, g.row_groups); break;
     switch (g.rows) {
-        MS_ROWS(16, 4, 4) MS_ROWS(32, 4, 8) MS_ROWS(64, 8, 8) MS_ROWS(128, 8, 16)
+        MS_ROWS(16, 4, 4) MS_ROWS(32, 4, 8) MS_ROWS(64, (REWRITE ? 4 : 8), (REWRITE ? 16 : 8)) MS_ROWS(128, 8, 16)
     }
 #undef MS_ROWS
 }
