@@ -130,7 +130,10 @@ struct Stager {
     static constexpr int gcd16(int x) { return x % 16 == 0 ? 16 : x % 8 == 0 ? 8 : x % 4 == 0 ? 4 : x % 2 == 0 ? 2 : 1; }
     static constexpr int PER = SWZ ? 16 / gcd16(RS) : 1;    // the swizzles repeat every 16 rows
     static constexpr int ND = PER < NCH ? PER : NCH;
-    static constexpr uint32_t kAbsent = 0xfff00000u;    // row offset past every cache's end
+    // Offset of an absent key: past every cache's end and every scale table's, so that codes and
+    // exponent bytes read as zeros. (An absent key with some present token's scale would be NaN
+    // where that is NaN, and 0 weight times NaN in the second product.)
+    static constexpr uint32_t kAbsent = 0xfff00000u;
 
     __amdgpu_buffer_rsrc_t rsrc, rscale, rlist;
     int lane, r0;
@@ -188,10 +191,9 @@ struct Stager {
         const int v = listed ? num : (FRESH ? w.r.f0 : 0) + i;
         const bool there = t < end && lane < KT && i < count && v >= 0 && (FRESH ? v < a.kv_rows : v < a.c.T);
         valid = __ballot(there);
-        const int row = there ? v : 0;
         if constexpr (!FRESH) {
             const uint32_t off = there ? (uint32_t)v * row_bytes : kAbsent;
-            const int so = (row >> a.c.lblock) * (2 * a.c.heads) + w.kvh;
+            const int so = there ? (v >> a.c.lblock) * (2 * a.c.heads) + w.kvh : (int)kAbsent;
             sk = __builtin_amdgcn_raw_buffer_load_b8(rscale, so, 0, 0);
             sv = __builtin_amdgcn_raw_buffer_load_b8(rscale, so, a.c.heads, 0);
 #pragma unroll
@@ -205,6 +207,7 @@ struct Stager {
                 }
             }
         } else {
+            const int row = there ? v : 0;
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
                 const long from = __shfl(row, key(i), kWave);
@@ -775,7 +778,7 @@ struct StagerF32 {
     static constexpr int P = HD + 4;
     static constexpr int TRASH = 2 * KT * P;            // words past the K and V rows: spare chunks, reads past the last row
     static constexpr int WORDS = TRASH + 16;
-    static constexpr uint32_t kAbsent = 0xfff00000u;
+    static constexpr uint32_t kAbsent = 0xfff00000u;    // as in Stager
 
     __amdgpu_buffer_rsrc_t rsrc, rscale, rlist;
     int lane, r0, col, count;
@@ -817,7 +820,7 @@ struct StagerF32 {
         valid = __ballot(there);
         const uint32_t off = there ? (uint32_t)v * row_elts * (FRESH ? 4u : 1u) : kAbsent;   // absent rows read as zeros
         if constexpr (!FRESH) {
-            const int so = ((there ? v : 0) >> a.c.lblock) * (2 * a.c.heads) + w.kvh;
+            const int so = there ? (v >> a.c.lblock) * (2 * a.c.heads) + w.kvh : (int)kAbsent;
             sk = __builtin_amdgcn_raw_buffer_load_b8(rscale, so, 0, 0);
             sv = __builtin_amdgcn_raw_buffer_load_b8(rscale, so, a.c.heads, 0);
         }

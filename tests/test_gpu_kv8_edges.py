@@ -1,0 +1,64 @@
+"""The 8-bit K/V cache where it could go wrong unseen."""
+import numpy as np
+import pytest
+import torch
+
+from tests import test_gpu_kv8 as K
+from tests import test_gpu_kv8_step as S
+
+pytestmark = pytest.mark.gpu
+DEV = K.DEV
+
+
+# ------------------------------------------------------------------ absent keys
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [1, 25, 200])
+@pytest.mark.parametrize("block", [1, 32])
+@pytest.mark.parametrize("T", [45, 180])
+@pytest.mark.parametrize("fresh", ["none", "rows"])
+def test_unlisted_first_block_of_nan_scales_has_no_effect(dtype, rows, block, T, fresh):
+    """Token 0's block holds NaN codes and NaN scales and is not listed: neither the lanes past the list's end (45 and 180
+    keys end inside every tile) nor list entries outside the cache may take them."""
+    for bad in (False, True):
+        g = torch.Generator().manual_seed(T + rows)
+
+        def edit(codes, scales, q, kv, keys):
+            keys[0] = torch.randint(block, T, (T,), generator=g).int()
+            if bad:
+                keys[0, 3::7] = -1
+                keys[0, T // 2] = 1 << 30
+            codes[0, :block] = 0x7f
+            scales[0, 0] = 255
+        _, _, refs = K._check(g, dtype, 2, 1, 64, block, 1, T, [rows], lists="keys", fresh=fresh, edit=edit)
+        assert np.isfinite(refs[0]).all()
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", h) for h in range(8, 129, 8)] + [("fp32", h) for h in range(8, 65, 8)])
+def test_unlisted_first_block_at_every_head_dim(dtype, hd):
+    for rows in (3, 40, 130):
+        g = torch.Generator().manual_seed(hd + rows)
+
+        def edit(codes, scales, q, kv, keys):
+            keys[0] = torch.randint(16, 77, (77,), generator=g).int()
+            codes[0, :16] = 0xff
+            scales[0, 0] = 255
+        _, _, refs = K._check(g, dtype, 1, 2, hd, 16, 1, 77, [rows], lists="keys", fresh="none", edit=edit)
+        assert np.isfinite(refs[0]).all()
+
+
+@pytest.mark.parametrize("shape", S.SHAPES, ids=lambda s: s.name)
+@pytest.mark.parametrize("pinned", [False, True], ids=["resident", "streamed"])
+def test_step_does_not_read_scales_of_masked_blocks(shape, pinned):
+    """A mask over the first 40 tokens: their block's NaN scales and codes change no bit of the step."""
+    ws, xt, codes, scales, kv, yc = S._inputs(shape, 92)
+    mask = np.zeros((shape.batch, shape.n_image), np.uint8)
+    mask[:, :40] = 1
+    x = S.W.edited_hidden(shape, 92, xt, mask)
+    want = S.Run(shape, mask, x, codes, scales, yc, ws, pinned=pinned).out()
+    assert np.isfinite(want).all()
+    codes, scales = [c.copy() for c in codes], [s.copy() for s in scales]
+    for c, s in zip(codes, scales):
+        c[:, :40] = 0x7f
+        s[:, 0] = 255                                   # tokens 0 to 31, all masked
+    np.testing.assert_array_equal(S.Run(shape, mask, x, codes, scales, yc, ws, pinned=pinned).out(), want)
