@@ -149,9 +149,9 @@ __global__ __launch_bounds__(WAVES * kWave) void quantize_kernel(Kv8Cache c, con
     for (int i = 0; i < NV; ++i) {
         const int r = row_of(i);
         v[i] = vec16{{0u, 0u, 0u, 0u}};
+        if constexpr (REWRITE) mul[i] = 1.0f;   // for rows past the last one too: `maxima` takes every row
         if (!mine || r >= rows) continue;
         if constexpr (REWRITE) {
-            mul[i] = 1.0f;
             if (!bit(touched, r)) continue;
             if (bit(fresh, r)) {
                 v[i] = ld16(kv + (long)src_row[(long)cache * c.T + t0 + r] * 2 * dkv + col);

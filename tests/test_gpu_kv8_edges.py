@@ -3,6 +3,8 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import kv8
+from paper_2505_20600_amd import maskstep as MS
 from tests import test_gpu_kv8 as K
 from tests import test_gpu_kv8_step as S
 
@@ -62,3 +64,20 @@ def test_step_does_not_read_scales_of_masked_blocks(shape, pinned):
         c[:, :40] = 0x7f
         s[:, 0] = 255                                   # tokens 0 to 31, all masked
     np.testing.assert_array_equal(S.Run(shape, mask, x, codes, scales, yc, ws, pinned=pinned).out(), want)
+
+
+# ------------------------------------------------------------------ rewriting
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("block,T", [(1, 17), (8, 31), (32, 33), (64, 65), (64, 127), (128, 129), (128, 200)])
+def test_rewrite_of_a_ragged_last_group(dtype, block, T):
+    """The last workgroup of tokens holds 1 to 72 of its 16 to 128 rows; the rewritten rows are in it."""
+    g = torch.Generator().manual_seed(T)
+    codes, scales = K._cache(g, 2, T, 3, 40, block, dtype)
+    kv = K._rows(g, (T, 2, 3, 40), dtype, width=5.0)
+    src = torch.full((2, T), -1, dtype=torch.int32)
+    src[:, T - 1], src[1, T - 5] = 0, 3
+    want = [kv8.rewrite(codes[s].cpu().numpy(), scales[s].cpu().numpy(), block, K._np(kv), src[s].numpy()) for s in range(2)]
+    MS.ms_kv8_quantize(kv, codes, scales, block=block, src_row=src.to(DEV))
+    assert np.array_equal(scales.cpu().numpy(), np.stack([e for _, e in want]))
+    assert K._same_codes(codes.cpu().numpy(), np.stack([c for c, _ in want]))
