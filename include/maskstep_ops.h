@@ -49,7 +49,9 @@ ms_status ms_linear(int32_t dtype, int32_t M, int32_t N, int32_t K, const void* 
  * scales  uint8 [n_caches][ceil(tokens / block)][2][n_kv_heads], exponent
  *         bytes b of powers of two 2^(b - 127), one per block of `block`
  *         consecutive tokens, K or V, and head (255 stands for NaN).
- * value = code * scale, exact in bf16 and float32 (down to 2^-126).
+ * value = code * scale, exact in bf16 and float32 from 2^-126 up to the type's
+ * largest value; one beyond that (code 256 at the scale 2^120, to which the
+ * largest bf16 and float32 values round, stands for 2^128) is read as infinite.
  *
  * Element type `dtype` is that of the K/V rows written or read, of the queries
  * and of the output. Pointers are device pointers, 16-byte aligned but for

@@ -22,17 +22,15 @@ __device__ __forceinline__ float kv8_scale(uint32_t b) {
     return __uint_as_float(b == 0 ? 0x00400000u : b == 255 ? 0x7fc00000u : b << 23);
 }
 
-// Exponent byte of a block whose largest finite magnitude is `amax`: the
-// smallest power of two s >= 2^-126 with amax <= 448 s = 1.75 * 2^8 s (1 for a
-// block of zeros).
-__device__ __forceinline__ uint32_t kv8_exponent(float amax) {
-    const uint32_t u = __float_as_uint(amax);
-    const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
-    return u == 0 ? 127u : (uint32_t)max(e, 1);
+// Exponent byte that values of the magnitudes up to |x| 2^(from - 127) need (`u`: the bits of
+// |x|, finite): the smallest power of two s >= 2^-126 with |x| 2^(from - 127) <= 448 s =
+// 1.75 * 2^8 s; 0 for x = 0. A block takes the largest need among its values, and the scale 1
+// (kv8_block_exponent) where all are zero.
+__device__ __forceinline__ uint32_t kv8_need(uint32_t u, int from) {
+    const int e = (int)((u + 0x1fffffu) >> 23) + from - 135;    // a mantissa above 0.75 carries into the exponent
+    return u == 0 ? 0u : (uint32_t)max(e, 1);
 }
-
-// 2^(127 - b): multiplying by it divides by the scale, exactly (1 <= b <= 247).
-__device__ __forceinline__ float kv8_inverse(uint32_t b) { return __uint_as_float((254u - b) << 23); }
+__device__ __forceinline__ uint32_t kv8_block_exponent(uint32_t need) { return need == 0 ? 127u : need; }
 
 __device__ __forceinline__ bool kv8_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
@@ -47,12 +45,20 @@ __device__ __forceinline__ float2 kv8_to_f32x2(uint32_t w, float s) {
     return make_float2(v[0], v[1]);
 }
 
-// Four values -> four codes, round to nearest even; |x| <= 448 inv^-1 for finite
-// x (inv = 1 / scale); NaN and infinities become NaN.
-__device__ __forceinline__ uint32_t kv8_encode4(const float x[4], float inv) {
+// What x 2^(from - 127) is multiplied by, as x, for codes at the exponent byte b >= its need: 2^(from - b),
+// at least 2^-127 (below that every x of a code is far below half the smallest code, and so is its
+// product). Exact where the product is a normal float32; what is not is below half the smallest code.
+__device__ __forceinline__ float kv8_ratio(int from, uint32_t b) {
+    const int e = from - (int)b + 127;      // at most 253
+    return __uint_as_float(e <= 0 ? 0x00400000u : (uint32_t)e << 23);
+}
+
+// Four values times ratio -> four codes, round to nearest even; at most 448 for finite x; NaN and
+// infinities become NaN.
+__device__ __forceinline__ uint32_t kv8_encode4(const float x[4], float ratio) {
     float y[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = kv8_finite(x[i]) ? x[i] * inv : __uint_as_float(0x7fc00000u);
+    for (int i = 0; i < 4; ++i) y[i] = kv8_finite(x[i]) ? x[i] * ratio : __uint_as_float(0x7fc00000u);
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
     return (uint32_t)w;

@@ -83,21 +83,26 @@ __device__ __forceinline__ void store_codes(uint32_t* p, const uint32_t (&w)[N])
 // A workgroup takes NV rows per wave of a cache (a block of tokens or, of small blocks,
 // several), K or V, and as many heads as 64 lanes of 16 bytes cover: lane = column, the waves
 // take the rows in turn, so that a load is a contiguous kilobyte of a row and each value is read
-// once, kept in registers until its block's largest magnitude is known (LDS, one maximum per
-// block and head). Bound by memory: 8 caches of 4096 tokens of 16 heads of 72 (227 MB) 44 us,
+// once, kept in registers until the exponent byte that its block needs is known (LDS, one
+// maximum per block and head). Bound by memory: 8 caches of 4096 tokens of 16 heads of 72 (227 MB) 44 us,
 // 4 of 24 heads of 128 (302 MB) 51 us, 5.1 and 5.9 TB/s. A wave per (block, head) tile, lanes over
 // its 144-byte rows and the values unpacked to float32, took 58 us; loads through the caches 50.
 // Codes go past the caches where a group's row of them is whole 64-byte lines (at head_dim
 // 128 55 -> 51 us; at 72, where neighbouring groups share lines, 44 -> 49).
-// Rewriting 410 of one cache's 4096 tokens of 16 heads of 72 takes 10 us: two loads one after the
-// other (which row, then the row), three barriers and the stores, on few workgroups; a fifth of
-// the tokens of 8 such caches, every block of them touched, 48.
+// Rewriting: kept rows need what their codes' largest magnitude needs at the old scale, and are
+// encoded by the ratio of the two scales. Two loads one after the other (which row, then the row),
+// three barriers and the stores, on the workgroups with a new row: one cache of 4096 tokens of 16
+// heads of 72, a tenth of them in four runs 9.3 us; a fifth of the tokens of 8 such caches in runs 24,
+// scattered over every block 57 (166 MB). Four rows per wave ask for eight waves per SIMD: the
+// compiler then keeps its scalar registers few enough for two workgroups of 16 waves per CU (the
+// last case 77 us without).
 template <typename T, int NV, int WAVES, bool REWRITE, bool STREAM>
-__global__ __launch_bounds__(WAVES * kWave) void quantize_kernel(Kv8Cache c, const T* __restrict__ kv, long row_stride,
+__global__ __launch_bounds__(WAVES * kWave, REWRITE && NV == 4 ? 8 : 1) void quantize_kernel(Kv8Cache c, const T* __restrict__ kv, long row_stride,
                                                             const int32_t* __restrict__ src_row, long kv_rows,
                                                             int heads_per_group, int groups, int row_groups) {
     constexpr int CW = Piece<T>::N, R = WAVES * NV, kGroup = WAVES * kWave;
-    __shared__ uint32_t s_max[R][kWave];    // [block of the rows][head of the group]
+    __shared__ uint32_t s_need[R][kWave];   // [block of the rows][head of the group]: exponent byte, kNotFinite beside NaN and infinities
+    constexpr uint32_t kNotFinite = 256;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     unsigned at = blockIdx.x;
     const int group = at % groups;
@@ -116,7 +121,6 @@ __global__ __launch_bounds__(WAVES * kWave) void quantize_kernel(Kv8Cache c, con
 
     // which rows are new, one lane a row, and which are in a block with a new one
     uint64_t fresh[(R + kWave - 1) / kWave], touched[(R + kWave - 1) / kWave];
-    int from = -1;
     if constexpr (REWRITE) {
         bool any = false;
 #pragma unroll
@@ -134,68 +138,91 @@ __global__ __launch_bounds__(WAVES * kWave) void quantize_kernel(Kv8Cache c, con
             uint64_t m = fresh[r / kWave] >> (r % kWave);
             if (block < kWave) m &= (1ull << block) - 1;
             else if (block > kWave) m = fresh[0] | fresh[(R + kWave - 1) / kWave - 1];
-            touched[j] = __ballot(m != 0);
+            touched[j] = __ballot(m != 0 && j * kWave + lane < rows);
         }
     }
-    for (int i = threadIdx.x; i < (R >> c.lblock ? R >> c.lblock : 1) * kWave; i += kGroup) (&s_max[0][0])[i] = 0u;
+    for (int i = threadIdx.x; i < (R >> c.lblock ? R >> c.lblock : 1) * kWave; i += kGroup) (&s_need[0][0])[i] = 0u;
 
-    // REWRITE: a kept row holds its codes' values unscaled, to be multiplied in float32 (a bf16
-    // would lose the bits of scaled values below 2^-126)
+    // REWRITE: a kept row holds its codes' values unscaled, `from` their scale's exponent byte (127
+    // for new rows, whose values stand for themselves): scaled values reach from 2^-136 to 448 times
+    // 2^127, beyond both ends of bf16 and float32
     vec16 v[NV];
-    float mul[REWRITE ? NV : 1];
+    int from[REWRITE ? NV : 1];
     auto row_of = [&](int i) { return i * WAVES + wave; };
     auto bit = [&](const uint64_t* m, int r) { return (m[R > kWave ? r / kWave : 0] >> (r % kWave)) & 1; };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int r = row_of(i);
         v[i] = vec16{{0u, 0u, 0u, 0u}};
-        if constexpr (REWRITE) mul[i] = 1.0f;   // for rows past the last one too: `maxima` takes every row
-        if (!mine || r >= rows) continue;
         if constexpr (REWRITE) {
-            if (!bit(touched, r)) continue;
+            from[i] = 127;
+            if (!mine || !bit(touched, r)) continue;
             if (bit(fresh, r)) {
                 v[i] = ld16(kv + (long)src_row[(long)cache * c.T + t0 + r] * 2 * dkv + col);
             } else {
-                uint32_t w[CW / 4];
 #pragma unroll
-                for (int k = 0; k < CW / 4; ++k) w[k] = reinterpret_cast<const uint32_t*>(codes + (long)r * 2 * dkv)[k];
-                v[i] = Piece<T>::decode(w, 1.0f);
-                mul[i] = kv8_scale(scales[(long)(r >> c.lblock) * 2 * c.heads]);
+                for (int k = 0; k < CW / 4; ++k) v[i].w[k] = reinterpret_cast<const uint32_t*>(codes + (long)r * 2 * dkv)[k];
+                from[i] = scales[(long)(r >> c.lblock) * 2 * c.heads];
             }
-        } else {
+        } else if (mine && r < rows) {
             v[i] = load_stream(kv + ((long)cache * row_stride + t0 + r) * 2 * dkv + col);
         }
     }
-    // this lane's largest magnitude per block to s_max
-    auto maxima = [&](auto of_row) {
-        uint32_t most = 0;
+    if constexpr (REWRITE) {    // the kept rows' codes, when all loads are under way
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int r = row_of(i);
-            most = max(most, of_row(i));
+            if (bit(fresh, r) || !bit(touched, r)) continue;
+            uint32_t w[CW / 4];
+#pragma unroll
+            for (int k = 0; k < CW / 4; ++k) w[k] = v[i].w[k];
+            v[i] = Piece<T>::decode(w, 1.0f);
+            const bool nan = from[i] == 255;    // a scale of NaN
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[i].w[k] = nan ? 0xffffffffu : v[i].w[k];
+            from[i] = nan ? 127 : from[i];
+        }
+    }
+    // this lane's largest need per block to s_need, from the bits of each row's largest magnitude
+    auto scale_from = [&](int i) { return REWRITE ? from[REWRITE ? i : 0] : 127; };
+    auto needs = [&](auto of_row) {
+        auto need = [&](uint32_t u, int b) { return u >= 0x7f800000u ? kNotFinite : kv8_need(u, b); };
+        uint32_t most = 0, kept = 0;    // of a block's new and kept rows; the latter have one scale
+        int kept_from = 127;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int r = row_of(i);
+            const uint32_t u = of_row(i);
+            if (!REWRITE || bit(fresh, r)) {
+                most = max(most, u);
+            } else if (bit(touched, r)) {
+                kept = max(kept, u);
+                kept_from = scale_from(i);
+            }
             if (i + 1 == NV || row_of(i + 1) >> c.lblock != r >> c.lblock) {
-                if (mine) atomicMax(&s_max[r >> c.lblock][h], most);
-                most = 0;
+                uint32_t n = need(most, 127);
+                if constexpr (REWRITE) n = max(n, need(kept, kept_from));
+                if (mine) atomicMax(&s_need[r >> c.lblock][h], n);
+                most = kept = 0;
             }
         }
     };
     __syncthreads();
-    maxima([&](int i) {
-        const uint32_t m = Piece<T>::most(v[i]);
-        return REWRITE ? __float_as_uint(__uint_as_float(m) * mul[REWRITE ? i : 0]) & 0x7fffffffu : m;
-    });
+    needs([&](int i) { return Piece<T>::most(v[i]); });
     __syncthreads();
     bool odd = false;       // infinities or NaN somewhere
-    for (int i = threadIdx.x; i < (R >> c.lblock ? R >> c.lblock : 1) * kWave; i += kGroup) odd |= (&s_max[0][0])[i] >= 0x7f800000u;
+    for (int i = threadIdx.x; i < (R >> c.lblock ? R >> c.lblock : 1) * kWave; i += kGroup) odd |= (&s_need[0][0])[i] == kNotFinite;
     odd = __syncthreads_or(odd);
-    auto value = [&](int i, int e) { return REWRITE ? Piece<T>::at(v[i], e) * mul[REWRITE ? i : 0] : Piece<T>::at(v[i], e); };
     if (odd) {              // the scale is that of the finite values
-        for (int i = threadIdx.x; i < (R >> c.lblock ? R >> c.lblock : 1) * kWave; i += kGroup) (&s_max[0][0])[i] = 0u;
+        for (int i = threadIdx.x; i < (R >> c.lblock ? R >> c.lblock : 1) * kWave; i += kGroup) (&s_need[0][0])[i] = 0u;
         __syncthreads();
-        maxima([&](int i) {
+        needs([&](int i) {
             uint32_t m = 0;
 #pragma unroll
-            for (int e = 0; e < CW; ++e) m = max(m, kv8_finite(value(i, e)) ? __float_as_uint(fabsf(value(i, e))) : 0u);
+            for (int e = 0; e < CW; ++e) {
+                const float x = Piece<T>::at(v[i], e);
+                m = max(m, kv8_finite(x) ? __float_as_uint(fabsf(x)) : 0u);
+            }
             return m;
         });
         __syncthreads();
@@ -203,19 +230,17 @@ __global__ __launch_bounds__(WAVES * kWave) void quantize_kernel(Kv8Cache c, con
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int r = row_of(i);
-        if (!mine || r >= rows) continue;
-        if constexpr (REWRITE) {
-            if (!bit(touched, r)) continue;
-        }
-        const uint32_t b = kv8_exponent(__uint_as_float(s_max[r >> c.lblock][h]));
+        if (!mine || (REWRITE ? !bit(touched, r) : r >= rows)) continue;
+        const uint32_t b = kv8_block_exponent(s_need[r >> c.lblock][h]);
         uint32_t* const p = reinterpret_cast<uint32_t*>(codes + (long)r * 2 * dkv);
         uint32_t w[CW / 4];
         if (odd || REWRITE) {
-            const float inv = kv8_inverse(b);
+            const float ratio = kv8_ratio(scale_from(i), b);
 #pragma unroll
             for (int k = 0; k < CW / 4; ++k) {
-                const float x[4] = {value(i, 4 * k), value(i, 4 * k + 1), value(i, 4 * k + 2), value(i, 4 * k + 3)};
-                w[k] = kv8_encode4(x, inv);
+                const float x[4] = {Piece<T>::at(v[i], 4 * k), Piece<T>::at(v[i], 4 * k + 1), Piece<T>::at(v[i], 4 * k + 2),
+                                    Piece<T>::at(v[i], 4 * k + 3)};
+                w[k] = kv8_encode4(x, ratio);
             }
         } else {
             Piece<T>::encode(v[i], kv8_scale(b), w);

@@ -81,3 +81,54 @@ def test_rewrite_of_a_ragged_last_group(dtype, block, T):
     MS.ms_kv8_quantize(kv, codes, scales, block=block, src_row=src.to(DEV))
     assert np.array_equal(scales.cpu().numpy(), np.stack([e for _, e in want]))
     assert K._same_codes(codes.cpu().numpy(), np.stack([c for c, _ in want]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("width", [-1, 1])
+def test_rewrite_beside_the_largest_value(dtype, width):
+    """The type's largest value is written as code 256 at the scale 2^120, a value of 2^128 that no float32 holds: it keeps
+    its code when a neighbour is rewritten."""
+    big = torch.finfo(K.DT[dtype]).max
+    kv = torch.ones(1, 16, 2, 1, 8)
+    kv[0, 3], kv[0, 4, 0, 0, 1] = big, -big
+    kv = kv.to(K.DT[dtype]).to(DEV)
+    codes, scales = K._empty_cache(1, 16, 1, 8, 16)
+    MS.ms_kv8_quantize(kv, codes, scales, block=16)
+    assert bool((scales == 247).all()) and int(codes[0, 3, 0, 0, 0]) == 120
+    new = torch.full((1, 2, 1, 8), 2.0 ** (100 * width), dtype=K.DT[dtype], device=DEV)
+    src = torch.full((1, 16), -1, dtype=torch.int32, device=DEV)
+    src[0, 7] = 0
+    c, e = kv8.rewrite(codes[0].cpu().numpy(), scales[0].cpu().numpy(), 16, K._np(new), src[0].cpu().numpy())
+    MS.ms_kv8_quantize(new, codes, scales, block=16, src_row=src)
+    assert np.array_equal(scales[0].cpu().numpy(), e) and K._same_codes(codes[0].cpu().numpy(), c)
+    assert int(codes[0, 3, 0, 0, 0]) == 120
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("block,T", [(1, 40), (4, 70), (32, 100), (64, 200), (128, 300)])
+@pytest.mark.parametrize("special", [False, True], ids=["finite", "nan"])
+def test_rewrite_of_every_scale_is_exact(dtype, block, T, special):
+    """Caches of random codes at every exponent byte (foreign ones too: quantize itself writes 1..247), new rows of every
+    magnitude down to zero and the subnormals, with and without NaN and infinities in both; ragged last groups."""
+    g = torch.Generator().manual_seed(T + block)
+    H, hd = 2, 16
+    codes = torch.randint(0, 127, (3, T, 2, H, hd), generator=g) + 128 * torch.randint(0, 2, (3, T, 2, H, hd), generator=g)
+    scales = torch.randint(0, 255, (3, -(-T // block), 2, H), generator=g)
+    codes[2] = codes[2] & 0x87                                      # magnitudes of the subnormal codes only
+    kv = torch.randn(50, 2, H, hd, generator=g, dtype=torch.float64)
+    kv *= torch.exp2(torch.randint(-140, 126, (50, 1, H, 1), generator=g).double())
+    kv[::9] = 0
+    kv = kv.to(torch.float32).to(K.DT[dtype])
+    kv[4] = torch.finfo(K.DT[dtype]).max
+    if special:
+        scales[torch.rand(scales.shape, generator=g) < 0.1] = 255
+        codes[torch.rand(codes.shape, generator=g) < 0.003] = 0x7f
+        kv[torch.rand(kv.shape, generator=g) < 0.003] = float("inf")
+        kv[torch.rand(kv.shape, generator=g) < 0.003] = float("nan")
+    src = torch.where(torch.rand(3, T, generator=g) < 0.2, torch.randint(0, 50, (3, T), generator=g), -1).int()
+    codes, scales = codes.to(torch.uint8), scales.to(torch.uint8)
+    want = [kv8.rewrite(codes[s].numpy(), scales[s].numpy(), block, K._np(kv), src[s].numpy()) for s in range(3)]
+    dc, ds = codes.to(DEV), scales.to(DEV)
+    MS.ms_kv8_quantize(kv.to(DEV), dc, ds, block=block, src_row=src.to(DEV))
+    assert np.array_equal(ds.cpu().numpy(), np.stack([e for _, e in want]))
+    assert K._same_codes(dc.cpu().numpy(), np.stack([c for c, _ in want]))
