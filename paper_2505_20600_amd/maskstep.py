@@ -653,14 +653,60 @@ class MaskStep:
         _check(self._lib.mask_stack_forward(self.handle, weights_c, _ptr(x), _ptr(ycache), C.byref(src),
                                             _ptr(y), cs, ps))
 
+    def _check_kv8(self, codes, scales, block, cache_of, pinned, slots, per_request) -> int:
+        """Number of caches of stack_forward_kv8's tensors, which must be as large as the library takes them to be
+        (addresses given as int are taken as they are, and NULL is left to the library)."""
+        d, B, N = self.desc, self.batch, self.desc.grid_h * self.desc.grid_w
+        L, H, row = d.n_layers, d.n_heads, 2 * d.d_model
+
+        def is_bytes(t, lead, n):
+            return (t is None or isinstance(t, int)
+                    or (t.element_size() == 1 and t.shape[:len(lead)] == lead and t.numel() == n and t.is_contiguous()))
+
+        if len(scales) != L or len((() if codes is None else codes) if per_request is None else per_request) != L:
+            raise _kv8_bad(f"codes and scales need one tensor per layer ({L})")
+        if isinstance(block, bool) or not isinstance(block, int) or block < 1:
+            raise _kv8_bad(f"block must be a positive int, not {block!r}")
+        S, blocks = scales[0].shape[0], -(-N // block)
+        for l, t in enumerate(scales):
+            if t is not None and (t.shape != (S, blocks, 2, H) or t.element_size() != 1 or not t.is_contiguous()):
+                raise _kv8_bad(f"scales[{l}] must be contiguous bytes [{S}][{blocks}][2][{H}] (block {block}), not {t.dtype} "
+                               f"{tuple(t.shape)}")
+        if per_request is None:
+            n = B if pinned else S
+            for l, t in enumerate(codes):
+                if not is_bytes(t, (n, N, 2), n * N * row):
+                    raise _kv8_bad(f"codes[{l}] must be contiguous bytes [{n}][{N}][2][{H}][{d.d_model // H}], not {t.dtype} "
+                                   f"{tuple(t.shape)}")
+        else:
+            for l, r in enumerate(per_request):
+                if len(r) != B or not all(is_bytes(t, (N, 2), N * row) for t in r):
+                    raise _kv8_bad(f"per_request[{l}] must be {B} buffers of contiguous bytes [{N}][2][{H}][{d.d_model // H}]")
+        if pinned:
+            for i, t in enumerate(slots):
+                if not (t is None or isinstance(t, int)) and (t.numel() * t.element_size() < B * N * row or not t.is_contiguous()):
+                    raise _kv8_bad(f"slots[{i}] must be contiguous and hold {B * N * row} bytes")
+        dev = scales[0].device
+        on_gpu = [t for t in (*scales, *(slots if pinned else codes if per_request is None else ()))
+                  if isinstance(t, torch.Tensor)]
+        if dev.type != "cuda" or any(t.device != dev for t in on_gpu):
+            raise _kv8_bad("scales, and codes or slots, must be on one GPU")
+        if pinned and any(t.is_cuda for r in (per_request if per_request is not None else [codes]) for t in r
+                          if isinstance(t, torch.Tensor)):
+            raise _kv8_bad("pinned codes must be host tensors")
+        if not isinstance(cache_of, int):
+            _kv8_table(cache_of, dev, (B,), "cache_of")
+        return S
+
     def stack_forward_kv8(self, weights_c, x, ycache, codes, scales, y, *, block: int, cache_of=None, pinned: bool = False,
                           slots=(), stream=None, copy_stream=None, per_request=None, loads_ahead: bool = False):
         """stack_forward over a K/V cache in 8 bits. ``codes``: [L] byte tensors [caches][N][2][heads][head_dim] on the
         device, or with ``pinned`` pinned host [B][N][2][heads][head_dim] (``per_request`` may replace them: [L][B]
-        pinned [N][2][heads][head_dim]) that stream through the device ``slots``; ``scales``: [L] device byte tensors
-        [caches][ceil(N / block)][2][heads]; ``cache_of``: device int32 [B], each request's cache (pinned: scale table)."""
-        L = len(scales)
-        S = scales[0].shape[0]
+        pinned [N][2][heads][head_dim]) that stream through the device ``slots`` (each at least the bytes of a layer's
+        codes); ``scales``: [L] device byte tensors [caches][ceil(N / block)][2][heads]; ``cache_of``: device int32 [B],
+        each request's cache (pinned: scale table)."""
+        L = self.desc.n_layers
+        S = self._check_kv8(codes, scales, block, cache_of, pinned, slots, per_request)
         sc = (C.c_void_p * L)(*[_ptr(t) for t in scales])
         ptrs = (C.c_void_p * L)(*[_ptr(t) for t in codes]) if per_request is None else (C.c_void_p * 1)()
         req = (C.c_void_p * max(1, L * self.batch))(*[_ptr(t) for r in per_request or () for t in r])

@@ -132,3 +132,35 @@ def test_rewrite_of_every_scale_is_exact(dtype, block, T, special):
     MS.ms_kv8_quantize(kv.to(DEV), dc, ds, block=block, src_row=src.to(DEV))
     assert np.array_equal(ds.cpu().numpy(), np.stack([e for _, e in want]))
     assert K._same_codes(dc.cpu().numpy(), np.stack([c for c, _ in want]))
+
+
+# ------------------------------------------------------------------ the step's tensors
+
+def test_step_refuses_tables_and_caches_of_another_kind():
+    """int64, short and host cache_of; scales for another block; caches of another count; codes on the host, pinned ones
+    on the GPU. Addresses given as int and stacked tensors are taken."""
+    shape = S.SHAPES[1]
+    ws, xt, codes, scales, kv, yc = S._inputs(shape, 94)
+    mask = S._masks(shape, (0.3, 0.1), 15)
+    x = S.W.edited_hidden(shape, 94, xt, mask)
+    run, streamed = (S.Run(shape, mask, x, codes, scales, yc, ws, pinned=p) for p in (False, True))
+    want = run.out()
+    of = torch.tensor([0, 1], dtype=torch.int32, device=DEV)
+    run.y.fill_(3.0)
+    held, host = run.codes, [c.cpu() for c in run.codes]
+    for change in (dict(cache_of=of.long()), dict(cache_of=of[:1]), dict(cache_of=of.cpu()), dict(block=16), dict(block=64)):
+        with pytest.raises(MS.MaskStepError):
+            run.step.stack_forward_kv8(run.wc, run.x, run.yc, run.codes, run.scales, run.y, **{**run.kw, **change})
+    for codes_, scales_ in ((host, run.scales), ([c[:1].contiguous() for c in held], run.scales),
+                            (held, [s[:1].contiguous() for s in run.scales]), (held, [s.cpu() for s in run.scales])):
+        with pytest.raises(MS.MaskStepError):
+            run.step.stack_forward_kv8(run.wc, run.x, run.yc, codes_, scales_, run.y, **run.kw)
+    with pytest.raises(MS.MaskStepError):
+        streamed.step.stack_forward_kv8(run.wc, run.x, run.yc, held, run.scales, run.y, **streamed.kw)
+    torch.cuda.synchronize()
+    assert bool((run.y == 3.0).all())
+    for codes_, kw in ((torch.stack(held), dict(cache_of=of)), ([c.data_ptr() for c in held], dict(cache_of=of.data_ptr()))):
+        run.y.fill_(3.0)
+        run.step.stack_forward_kv8(run.wc, run.x, run.yc, codes_, run.scales, run.y, **{**run.kw, **kw})
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(K._np(run.y), want)
