@@ -186,6 +186,7 @@ def ms_linear(A, W, bias, out, *, resid=None, epilogue=MS_EPI_BIAS, tile=(0, 0),
 # ---------------------------------------------------------------------------
 
 _KV8_DTYPES = {torch.bfloat16: MS_BF16, torch.float32: MS_FP32}
+_KV8_NO_ENTRIES = 16   # an aligned address that nothing reads
 
 
 def _kv8_bad(what):
@@ -193,12 +194,14 @@ def _kv8_bad(what):
 
 
 def _kv8_table(t, dev, shape, name):
+    """Address of an int32 table, None where there is none. A table without entries has one too: NULL would stand for
+    every token, or every row."""
     if t is None:
         return None
     if not (t.dtype == torch.int32 and t.device == dev and t.shape == shape and t.is_contiguous()):
         raise _kv8_bad(f"{name} must be a contiguous int32 tensor {tuple(shape)} on {dev}, not {t.dtype} {tuple(t.shape)} "
                        f"on {t.device}")
-    return t.data_ptr()
+    return t.data_ptr() or _KV8_NO_ENTRIES
 
 
 def _kv8_cache(codes, scales, block, like):

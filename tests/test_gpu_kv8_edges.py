@@ -164,3 +164,34 @@ def test_step_refuses_tables_and_caches_of_another_kind():
         run.step.stack_forward_kv8(run.wc, run.x, run.yc, codes_, run.scales, run.y, **{**run.kw, **kw})
         torch.cuda.synchronize()
         np.testing.assert_array_equal(K._np(run.y), want)
+
+
+# ------------------------------------------------------------------ empty tables
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [2, 140])
+def test_tables_without_entries_name_nothing(dtype, rows):
+    """keys of no columns: no cached token is read; a fresh_list of no entries: no fresh row."""
+    g = torch.Generator().manual_seed(21)
+    codes, scales = K._cache(g, 1, 60, 2, 64, 32, dtype)
+    q = torch.randn(rows, 2, 64, generator=g).to(K.DT[dtype]).to(DEV)
+    start = torch.tensor([0, rows], dtype=torch.int32, device=DEV)
+    none = torch.zeros(1, 0, dtype=torch.int32, device=DEV)
+    fresh = K._rows(g, (rows, 2, 2, 64), dtype)
+    out = torch.full_like(q, 7.0)
+    MS.ms_kv8_attention(q, codes, scales, out, start, block=32, keys=none)
+    assert bool((out == 0).all())
+    MS.ms_kv8_attention(q, codes, scales, out, start, block=32, keys=none, fresh=fresh, fresh_start=start)
+    k = K._np(fresh)
+    ref, spread = kv8.attention(K._np(q), k[:, 0], k[:, 1], 0.125)
+    assert np.all(np.abs(K._np(out) - ref) <= K._bound(q, k, ref, spread, 0.125, dtype))
+    want = torch.empty_like(q)
+    MS.ms_kv8_attention(q, codes, scales, want, start, block=32)
+    MS.ms_kv8_attention(q, codes, scales, out, start, block=32, fresh=fresh, fresh_list=none[0], fresh_start=start)
+    k = kv8.values(codes[0].cpu().numpy(), scales[0].cpu().numpy(), 32)
+    ref, spread = kv8.attention(K._np(q), k[:, 0], k[:, 1], 0.125)
+    for t in (want, out):
+        assert np.all(np.abs(K._np(t) - ref) <= K._bound(q, k, ref, spread, 0.125, dtype))
+    kv = torch.full((1, 60, 2, 2, 64), 7.0, dtype=K.DT[dtype], device=DEV)
+    MS.ms_kv8_dequantize(codes, scales, kv, block=32, keys=none)
+    assert bool((kv == 7.0).all())
