@@ -298,13 +298,29 @@ def ms_kv8_dequantize(codes, scales, kv, *, block, cache_of=None, keys=None, n_k
     _kv8_run(load().ms_kv8_dequantize, kv, stream, C.byref(c), C.byref(sel), kv.data_ptr(), stride)
 
 
-def ms_kv8_attention_workspace_bytes(q, codes, seg_start, *, keys=None, fresh=None, fresh_list=None) -> int:
-    """Bytes of workspace with which ms_kv8_attention may split the keys as it sees fit, for tensors of these shapes."""
+def _kv8_batch(codes, n_seg, seg_req, cache_of, keys, n_keys, fresh, fresh_start):
+    """Number of requests, from the first table that has a row for each of them."""
+    if cache_of is not None:
+        return cache_of.shape[0]
+    if n_keys is not None:
+        return n_keys.shape[0]
+    if keys is not None:
+        return keys.shape[0]
+    if fresh is not None and fresh_start is not None:
+        return fresh_start.shape[0] - 1
+    return n_seg if seg_req is None else codes.shape[0]
+
+
+def ms_kv8_attention_workspace_bytes(q, codes, seg_start, *, seg_req=None, cache_of=None, keys=None, n_keys=None, fresh=None,
+                                     fresh_list=None, fresh_start=None) -> int:
+    """Bytes of workspace with which ms_kv8_attention may split the keys as it sees fit, for tensors of these shapes (the
+    call's own tables; any that it takes and this one is not given count as one request per segment)."""
     S, T, _, H, hd = codes.shape
     n_seg = seg_start.shape[0] - 1
-    some = 16   # an address that is checked but not read
+    batch = _kv8_batch(codes, n_seg, seg_req, cache_of, keys, n_keys, fresh, fresh_start)
+    some = _KV8_NO_ENTRIES   # addresses are checked but not read
     c = Kv8Cache(_KV8_DTYPES.get(q.dtype, -1), S, T, H, hd, 1, some, some)
-    sel = Kv8Select(n_seg, 0 if keys is None else keys.shape[-1], some, None if keys is None else some, None)
+    sel = Kv8Select(batch, 0 if keys is None else keys.shape[-1], some, None if keys is None else some, None)
     f_rows = 0 if fresh is None else fresh.shape[0]
     a = Kv8Attn(some, some, q.shape[0], q.shape[1], n_seg, some, some, some if f_rows else None, f_rows,
                 None if fresh_list is None else some, 0 if fresh_list is None else fresh_list.numel(), some, 0.0)
@@ -325,15 +341,7 @@ def ms_kv8_attention(q, codes, scales, out, seg_start, *, block, seg_req=None, c
     if out.shape != q.shape or out.dtype != q.dtype or out.device != dev or not out.is_contiguous():
         raise _kv8_bad("out must be like q")
     n_seg = seg_start.shape[0] - 1
-    batch = n_seg if seg_req is None else c.n_caches
-    if cache_of is not None:
-        batch = cache_of.shape[0]
-    elif n_keys is not None:
-        batch = n_keys.shape[0]
-    elif keys is not None:
-        batch = keys.shape[0]
-    elif fresh is not None and fresh_start is not None:
-        batch = fresh_start.shape[0] - 1
+    batch = _kv8_batch(codes, n_seg, seg_req, cache_of, keys, n_keys, fresh, fresh_start)
     sel = _kv8_select(dev, batch, cache_of, keys, n_keys)
     fp, f_rows, fl, fe, fs = None, 0, None, 0, None
     if fresh is not None:

@@ -1,4 +1,6 @@
 """What the Python binding of the 8-bit cache refuses before it hands addresses to the library (no GPU needed)."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -78,3 +80,31 @@ def test_step_refuses_host_scales():
               lambda: _pinned(slots=[torch.zeros(B, N, 2, H, HD, dtype=torch.bfloat16)])):
         with pytest.raises(MS.MaskStepError, match="on one GPU"):
             f()
+
+
+# ------------------------------------------------------------------ workspace
+
+@pytest.mark.parametrize("rows", [1, 150, 600])
+@pytest.mark.parametrize("by", ["cache_of", "n_keys", "keys", "fresh_start", "codes"])
+def test_workspace_is_planned_for_the_calls_requests(rows, by):
+    """Two and three segments per request: the bytes that the library plans for the call's own batch, whichever table says
+    how many requests there are."""
+    lib, T, fresh_rows = MS.load(), 3000, 7000
+    codes = torch.empty(2 if by == "codes" else 9, T, 2, 3, 64, dtype=torch.uint8)
+    start, req = torch.zeros(6, dtype=torch.int32), torch.zeros(5, dtype=torch.int32)
+    q, fresh = torch.empty(5 * rows, 6, 64, dtype=torch.bfloat16), torch.empty(fresh_rows, 2, 3, 64, dtype=torch.bfloat16)
+    tables = {"cache_of": torch.zeros(2, dtype=torch.int32), "n_keys": torch.zeros(2, dtype=torch.int32),
+              "keys": torch.zeros(2, 2000, dtype=torch.int32), "fresh_start": torch.zeros(3, dtype=torch.int32)}
+    kw = {"fresh": fresh} if by == "codes" else {by: tables[by], "fresh": fresh}
+    cache = MS.Kv8Cache(MS.MS_BF16, codes.shape[0], T, 3, 64, 64, 16, 16)
+    ld = 2000 if by == "keys" else 0
+    args = MS.Kv8Attn(16, 16, 5 * rows, 6, 5, 16, 16, 16, fresh_rows, None, 0, 16, 0.0)
+
+    def planned(batch):
+        sel = MS.Kv8Select(batch, ld, 16, 16 if ld else None, None)
+        return lib.ms_kv8_attention_workspace_bytes(C.byref(cache), C.byref(sel), C.byref(args))
+    assert MS.ms_kv8_attention_workspace_bytes(q, codes, start, seg_req=req, **kw) == planned(2)
+    if rows == 150:
+        assert planned(2) != planned(5)
+    one = MS.ms_kv8_attention_workspace_bytes(q, codes, start, fresh=fresh)
+    assert by == "keys" or one == planned(5)
