@@ -333,7 +333,10 @@ def ms_kv8_attention_workspace_bytes(q, codes, seg_start, *, seg_req=None, cache
 def ms_kv8_attention(q, codes, scales, out, seg_start, *, block, seg_req=None, cache_of=None, keys=None, n_keys=None,
                      fresh=None, fresh_list=None, fresh_start=None, scale=None, workspace=None, stream=None):
     """out[rows][heads][head_dim] = attention of the packed query rows q over the listed cached tokens of their request
-    and its fresh K/V rows ([rows][2][kv_heads][head_dim], by fresh_list and fresh_start [batch + 1])."""
+    and its fresh K/V rows ([rows][2][kv_heads][head_dim], by fresh_list and fresh_start [batch + 1]). ``scale``: of the
+    scores, None: 1 / sqrt(head_dim); one that float32 holds as 0 is refused, since 0 stands for None in the library."""
+    if scale is not None and C.c_float(scale).value == 0.0:
+        raise _kv8_bad(f"scale {scale!r} is 0 in float32; None stands for 1 / sqrt(head_dim)")
     c = _kv8_cache(codes, scales, block, q)
     dev = q.device
     if q.dim() != 3 or q.shape[2] != c.head_dim or not q.is_contiguous():

@@ -108,3 +108,16 @@ def test_workspace_is_planned_for_the_calls_requests(rows, by):
         assert planned(2) != planned(5)
     one = MS.ms_kv8_attention_workspace_bytes(q, codes, start, fresh=fresh)
     assert by == "keys" or one == planned(5)
+
+
+# ------------------------------------------------------------------ score scale
+
+@pytest.mark.parametrize("scale", [0, 0.0, -0.0, 1e-60])
+def test_a_score_scale_of_zero_is_refused(scale):
+    """The library takes 0 as 1 / sqrt(head_dim)."""
+    codes, scales = torch.zeros(1, 40, 2, 4, 64, dtype=torch.uint8), torch.zeros(1, 3, 2, 4, dtype=torch.uint8)
+    q, start = torch.zeros(10, 8, 64, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(MS.MaskStepError, match="scale"):
+        MS.ms_kv8_attention(q, codes, scales, q, start, block=16, scale=scale)
+    with pytest.raises(MS.MaskStepError, match="one GPU"):
+        MS.ms_kv8_attention(q, codes, scales, q, start, block=16, scale=1e-40)
