@@ -1022,10 +1022,22 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Kv8AttnDesc a) {
     if (lane < CL) store4<T>(static_cast<T*>(a.o) + sr * hd + col * 4, o);
 }
 
+// Slot tiles, the segments' last ones counted as full.
+int slot_tiles(const Kv8AttnDesc& a, int tile) {
+    return (int)std::min<long>((long)a.M * a.group / tile + a.nseg, (long)a.M * a.group);
+}
+
+// Whether a split into n ranges stays below the 2^32 threads that end a launch: the attention's
+// (its pairs of tile and range rounded up to the XCDs) and the join's, a wave per row and head.
+bool ranges_fit(const Kv8AttnDesc& a, int tile, int n) {
+    constexpr long most = (1l << 32) / kThreads;
+    return ((long)slot_tiles(a, tile) * n + kXcds) * a.c.heads < most &&
+           (long)a.M * a.c.heads * a.group / (kThreads / kWave) + 1 < most;
+}
+
 template <int QT>
 void launch_bf16(const Kv8AttnDesc& a, hipStream_t s) {
-    // slot tiles, the segments' last ones counted as full
-    const int qtiles = (int)std::min<long>((long)a.M * a.group / QT + a.nseg, (long)a.M * a.group);
+    const int qtiles = slot_tiles(a, QT);
     const int pairs = qtiles * a.nsplit;
     const dim3 grid((unsigned)(QT == 128 ? pairs : (pairs + kXcds - 1) / kXcds * kXcds) * a.c.heads), block(kThreads);
     switch (a.c.hd) {
@@ -1037,7 +1049,7 @@ void launch_bf16(const Kv8AttnDesc& a, hipStream_t s) {
 }
 
 void launch_f32(const Kv8AttnDesc& a, hipStream_t s) {
-    const int qtiles = (int)std::min<long>((long)a.M * a.group / 16 + a.nseg, (long)a.M * a.group);
+    const int qtiles = slot_tiles(a, 16);
     const int pairs = qtiles * a.nsplit;
     const dim3 grid((unsigned)(pairs + kXcds - 1) / kXcds * kXcds * a.c.heads), block(kThreads);
     switch (a.c.hd) {
@@ -1084,7 +1096,7 @@ void plan_kv8_attention(int dtype, Kv8AttnDesc& a, long keys) {
         const long steps = std::max(1l, tile == 128 ? (keys + 63) / 64 : (keys + 127) / 128);
         const int most = tile == 128 ? shared_per_cu(hd) : dtype == kBF16 ? few_per_cu(hd, tile) : 2;
         for (int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-            if (n > steps || n > kMaxRanges) break;
+            if (n > steps || n > kMaxRanges || (n > 1 && !ranges_fit(a, tile, n))) break;
             const double groups = base * n, slots = 256.0 * most, k = std::min(std::ceil(groups / 256), (double)most);
             const double step = tile == 128 ? mfmas * (0.014 + 0.010 * k)
                 : dtype != kBF16 ? k * hd * 0.016 : (hd * (hd % 16 ? 1.25 : 1.0) + 2) * (0.0015 + 0.009 * k);

@@ -121,3 +121,30 @@ def test_a_score_scale_of_zero_is_refused(scale):
         MS.ms_kv8_attention(q, codes, scales, q, start, block=16, scale=scale)
     with pytest.raises(MS.MaskStepError, match="one GPU"):
         MS.ms_kv8_attention(q, codes, scales, q, start, block=16, scale=1e-40)
+
+
+# ------------------------------------------------------------------ launch sizes
+
+@pytest.mark.parametrize("dtype,heads,group,hd", [(MS.MS_BF16, 1, 1, 8), (MS.MS_BF16, 64, 8, 64), (MS.MS_BF16, 1024, 1, 16),
+                                                  (MS.MS_FP32, 1, 1, 8), (MS.MS_FP32, 1024, 1, 64)])
+@pytest.mark.parametrize("segments", [1, 8, 128])
+def test_key_ranges_stay_within_one_launch(dtype, heads, group, hd, segments):
+    """However many keys are to be expected (here a list of up to 2^28 entries), the planned ranges are launches below
+    2^32 threads: 256 per 16 query slots (or more), K/V head and range, and a wave per row and head for the join."""
+    lib, split = MS.load(), 0
+    cache = MS.Kv8Cache(dtype, 128, 64, heads, hd, 64, 16, 16)
+    sel = MS.Kv8Select(segments, 0, 16, None, None)
+    for bits in range(27):
+        rows = 1 << bits
+        if rows * heads * group > 1 << 27:
+            break
+        for entries in (1 << 20, 1 << 28):
+            a = MS.Kv8Attn(16, 16, rows, heads * group, segments, 16, 16, 16, 1, 16, entries, 16, 0.0)
+            n = lib.ms_kv8_attention_workspace_bytes(C.byref(cache), C.byref(sel), C.byref(a)) // (rows * heads * group * (hd + 2) * 4)
+            assert not lib.mask_last_error()
+            split = max(split, n)
+            if n:
+                tile = 128 if dtype == MS.MS_BF16 and rows * group > 8 * 128 * segments else 16   # many rows: the form for many
+                assert (rows * group // tile * n) * heads * 256 < 1 << 32
+                assert rows * heads * group * 64 < 1 << 32
+    assert split > 1
