@@ -160,5 +160,7 @@ hipError_t launch_kv8_dequantize(int dtype, const Kv8Cache& c, const Kv8Select& 
 // sizes; its tables are not read). The caller may lower nsplit to what its buffers hold.
 void plan_kv8_attention(int dtype, Kv8AttnDesc& a, long keys);
 hipError_t launch_kv8_attention(int dtype, const Kv8AttnDesc& a, hipStream_t s);
+// Joins the key ranges' parts into the output; nothing where there is one range.
+hipError_t launch_kv8_join(int dtype, const Kv8AttnDesc& a, hipStream_t s);
 
 }  // namespace ms

@@ -202,6 +202,7 @@ ms_status ms_kv8_attention(const ms_kv8_cache* c, const ms_kv8_select* sel, cons
         d.part_ml = d.part_o + (size_t)d.nsplit * d.M * d.c.heads * d.group * d.c.hd;
     }
     hipError_t e = ms::launch_kv8_attention(c->dtype, d, static_cast<hipStream_t>(stream));
+    if (e == hipSuccess) e = ms::launch_kv8_join(c->dtype, d, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return set_error(MS_EHIP, "attention launch: %s", hipGetErrorString(e));
     return ms::clear_error();
 }

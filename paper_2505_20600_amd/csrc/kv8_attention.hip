@@ -1121,8 +1121,11 @@ hipError_t launch_kv8_attention(int dtype, const Kv8AttnDesc& a, hipStream_t s) 
     } else {
         launch_f32(a, s);
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.nsplit == 1) return e;
+    return hipGetLastError();
+}
+
+hipError_t launch_kv8_join(int dtype, const Kv8AttnDesc& a, hipStream_t s) {
+    if (a.M == 0 || a.nsplit == 1) return hipSuccess;
     const long n = (long)a.M * a.c.heads * a.group;
     const dim3 grid((unsigned)((n + kThreads / kWave - 1) / (kThreads / kWave))), block(kThreads);
     if (dtype == kBF16) hipLaunchKernelGGL(join_kernel<bf16_t>, grid, block, 0, s, a);

@@ -562,8 +562,14 @@ ms_status block_forward(ms_step* s, const Packing& pk, const ms_layer_weights* w
         const size_t part_rows = std::min(attn_part_rows(s->desc, s->B), attn_part_o_rows(s->desc, s->B));
         ms::plan_kv8_attention(dt, ad, (s->U + M) / s->B);
         ad.nsplit = std::max(1, std::min(ad.nsplit, (int)(part_rows / M)));
-        ProfScope p(MS_K_ATTENTION, st);
-        MS_HIP(ms::launch_kv8_attention(dt, ad, st));
+        {
+            ProfScope p(MS_K_ATTENTION, st);
+            MS_HIP(ms::launch_kv8_attention(dt, ad, st));
+        }
+        if (ad.nsplit > 1) {
+            ProfScope p(MS_K_ATTN_COMBINE, st);
+            MS_HIP(ms::launch_kv8_join(dt, ad, st));
+        }
     } else {
         ms::AttnDesc ad{};
         ad.q = q; ad.kv = kv; ad.o = o;

@@ -5,6 +5,7 @@ import torch
 
 from oracle import kv8
 from paper_2505_20600_amd import maskstep as MS
+from tests import gpu_helpers as G
 from tests import test_gpu_kv8 as K
 from tests import test_gpu_kv8_step as S
 
@@ -195,3 +196,21 @@ def test_tables_without_entries_name_nothing(dtype, rows):
     kv = torch.full((1, 60, 2, 2, 64), 7.0, dtype=K.DT[dtype], device=DEV)
     MS.ms_kv8_dequantize(codes, scales, kv, block=32, keys=none)
     assert bool((kv == 7.0).all())
+
+
+# ------------------------------------------------------------------ the step's timing classes
+
+def test_step_books_the_join_of_key_ranges_as_such():
+    """attention and attn_combine of a step over an 8-bit cache, one each per block, as over a K/V cache."""
+    shape = S.W.ModelShape("k8_join", 3, 256, 4, 4, 32, 32, dtype="bf16", batch=1)
+    ws, xt, codes, scales, kv, yc = S._inputs(shape, 93)
+    mask = np.zeros((1, shape.n_image), np.uint8)
+    mask[0, 100:104] = 1
+    run = S.Run(shape, mask, S.W.edited_hidden(shape, 93, xt, mask), codes, scales, yc, ws)
+    run.out()
+    MS.profiler_start(("attention", "attn_combine"), capacity=64)
+    y = run.out()
+    tot = MS.profiler_stop()
+    assert tot["attention"][1] == 3 and tot["attn_combine"][1] == 3
+    G.assert_close(y, S.oracle.masked_stack(S.W.edited_hidden(shape, 93, xt, mask), mask, kv, yc, ws, shape, round_p=True),
+                   "bf16", "joined ranges", blocks=3, inp=S.W.edited_hidden(shape, 93, xt, mask))
