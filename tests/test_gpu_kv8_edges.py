@@ -214,3 +214,39 @@ def test_step_books_the_join_of_key_ranges_as_such():
     assert tot["attention"][1] == 3 and tot["attn_combine"][1] == 3
     G.assert_close(y, S.oracle.masked_stack(S.W.edited_hidden(shape, 93, xt, mask), mask, kv, yc, ws, shape, round_p=True),
                    "bf16", "joined ranges", blocks=3, inp=S.W.edited_hidden(shape, 93, xt, mask))
+
+
+# ------------------------------------------------------------------ scores beyond float32
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [3, 25, 200])
+@pytest.mark.parametrize("ws", [0, "need"])
+def test_scores_of_minus_infinity_weigh_nothing(dtype, rows, ws):
+    """Scores that overflow float32 downwards: beside finite ones they weigh nothing, and a row of nothing else is 0.
+    Query column 0 is -2^100; a key's column 0 is 2^100 or 0."""
+    g = torch.Generator().manual_seed(22)
+    T = 1500
+    codes, scales = K._cache(g, 1, T, 2, 64, 1, dtype)
+    far = torch.rand(T, generator=g) < 0.5
+    codes[0, :, 0, :, 0] = 0
+    q = torch.randn(rows, 2, 64, generator=g).to(K.DT[dtype])
+    q[:, :, 0] = -2.0 ** 100
+    q = q.to(DEV)
+    start = torch.tensor([0, rows], dtype=torch.int32, device=DEV)
+    work = None
+    if ws:
+        work = torch.full((MS.ms_kv8_attention_workspace_bytes(q, codes, start) // 4 + 4,), float("nan"), device=DEV)
+    k = kv8.values(codes[0].cpu().numpy(), scales[0].cpu().numpy(), 1)
+    k = k[~far.numpy()]
+    codes[0, far.to(DEV), 0] = 0
+    codes[0, far.to(DEV), 0, :, 0] = 0x38               # 1.0
+    scales[0, far.to(DEV), 0] = 227                     # 2^100
+    out = torch.empty_like(q)
+    MS.ms_kv8_attention(q, codes, scales, out, start, block=1, workspace=work)
+    q0 = q.clone()
+    q0[:, :, 0] = 0                                     # the finite keys' column 0 is 0
+    ref, spread = kv8.attention(K._np(q0), k[:, 0], k[:, 1], 0.125)
+    assert np.all(np.abs(K._np(out) - ref) <= K._bound(q0, k, ref, spread, 0.125, dtype))
+    only = far.nonzero().flatten().int()[None].to(DEV)
+    MS.ms_kv8_attention(q, codes, scales, out, start, block=1, keys=only, workspace=work)
+    assert bool((out == 0).all())
