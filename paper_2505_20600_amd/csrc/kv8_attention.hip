@@ -622,10 +622,11 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? shared_per_cu(HD) : few_per_c
                     next();
                     continue;
                 }
-                // under the matrix instructions of QK, or before them where the registers saved make
-                // room for a third workgroup per CU (head_dim 72: 12 x 1024 rows of 16 heads over 4096
-                // keys 347 -> 320 us; 80 and 104, with two either way, are 2% faster the first way)
-                if constexpr (S::SWZ || shared_per_cu(HD) != 3) {
+                // under the matrix instructions of QK, or before them at head_dim 72, the largest with
+                // three workgroups per CU, which the registers saved make room for. In us, under / before:
+                // 12 x 1024 rows of 16 heads over 4096 keys at 24 195 / 196, 40 234 / 237, 48 241 / 243, 56
+                // 257 / 264, 72 320 / 305; 8 x 900 rows at 56 179 / 182, at 72 264 / 215
+                if constexpr (S::SWZ || HD <= 64 || shared_per_cu(HD) != 3) {
                     qk(stage(n), sa);
                     next();
                 } else {
