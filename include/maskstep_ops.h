@@ -120,8 +120,8 @@ ms_status ms_kv8_dequantize(const ms_kv8_cache* c, const ms_kv8_select* sel, voi
  *   out[m][h] = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q[m][h].k_j),
  * K/V head h / (n_heads / n_kv_heads). A row without any key gives zeros, and so
  * does one whose scores are all -infinity (scores are float32, and one beyond
- * its range is infinite). Rows outside [seg_start[0], seg_start[n_seg]) are left
- * as they are. A NaN in a query or in a key or value that is listed makes its
+ * its range is infinite; one of +infinity makes its row NaN). Rows outside
+ * [seg_start[0], seg_start[n_seg]) are left as they are. A NaN in a query or in a key or value that is listed makes its
  * rows NaN; tokens that are not listed have no effect whatever they hold.
  * Scores, maxima, sums and the parts of key ranges are float32. bf16 rounds
  * twice: the weights w_j relative to the running maximum, the matrix cores'

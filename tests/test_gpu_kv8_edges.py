@@ -250,3 +250,33 @@ def test_scores_of_minus_infinity_weigh_nothing(dtype, rows, ws):
     only = far.nonzero().flatten().int()[None].to(DEV)
     MS.ms_kv8_attention(q, codes, scales, out, start, block=1, keys=only, workspace=work)
     assert bool((out == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [3, 25, 200])
+@pytest.mark.parametrize("ws", [0, "need"])
+@pytest.mark.parametrize("where", [0, 700, 1499])
+def test_a_score_of_infinity_makes_its_row_nan(dtype, rows, ws, where):
+    """One key's score overflows float32 upwards for every other row; the rows between are as without that key's."""
+    g = torch.Generator().manual_seed(23)
+    T = 1500
+    codes, scales = K._cache(g, 1, T, 1, 64, 1, dtype)
+    codes[0, :, 0, :, 0] = 0
+    codes[0, where, 0] = 0
+    codes[0, where, 0, :, 0] = 0x38
+    scales[0, where, 0] = 227
+    q = torch.randn(rows, 1, 64, generator=g).to(K.DT[dtype])
+    q[:, :, 0] = 0
+    q[::2, :, 0] = 2.0 ** 100
+    q = q.to(DEV)
+    start = torch.tensor([0, rows], dtype=torch.int32, device=DEV)
+    work = None
+    if ws:
+        work = torch.full((MS.ms_kv8_attention_workspace_bytes(q, codes, start) // 4 + 4,), float("nan"), device=DEV)
+    out = torch.empty_like(q)
+    MS.ms_kv8_attention(q, codes, scales, out, start, block=1, workspace=work)
+    assert bool(out[::2].isnan().all())
+    k = kv8.values(codes[0].cpu().numpy(), scales[0].cpu().numpy(), 1)
+    ref, spread = kv8.attention(K._np(q[1::2]), k[:, 0], k[:, 1], 0.125)
+    k[where, 0] = 0                                     # its score in these rows is 0
+    assert np.all(np.abs(K._np(out[1::2]) - ref) <= K._bound(q[1::2], k, ref, spread, 0.125, dtype))
