@@ -84,22 +84,26 @@ __device__ __forceinline__ void store_codes(uint32_t* p, const uint32_t (&w)[N])
 // several), K or V, and as many heads as 64 lanes of 16 bytes cover: lane = column, the waves
 // take the rows in turn, so that a load is a contiguous kilobyte of a row and each value is read
 // once, kept in registers until the exponent byte that its block needs is known (LDS, one
-// maximum per block and head). Bound by memory: 8 caches of 4096 tokens of 16 heads of 72 (227 MB) 44 us,
-// 4 of 24 heads of 128 (302 MB) 51 us, 5.1 and 5.9 TB/s. A wave per (block, head) tile, lanes over
-// its 144-byte rows and the values unpacked to float32, took 58 us; loads through the caches 50.
-// Codes go past the caches where a group's row of them is whole 64-byte lines (at head_dim
-// 128 55 -> 51 us; at 72, where neighbouring groups share lines, 44 -> 49).
+// maximum per block and head). Bound by memory. Over buffers that no cache holds, where a copy
+// takes 5.65 TB/s: 8 caches of 4096 tokens of 16 heads of 72 (227 MB) 58 us, 3.9 TB/s (its groups of
+// heads share lines of codes), 4 of 24 heads of 128 (302 MB) 51 us, 5.9 TB/s, 8 of 16 heads of 64 in
+// float32 (335 MB) 55 us, 6.1 TB/s; the first over the same buffers again and again 44 us. A wave per
+// (block, head) tile, lanes over its 144-byte rows and the values unpacked to float32, took 58 us
+// there; loads through the caches 50. Codes go past the caches where a group's row of them is whole
+// 64-byte lines (at head_dim 128 55 -> 51 us; at 72, where neighbouring groups share lines, 44 -> 49).
 // Rewriting: kept rows need what their codes' largest magnitude needs at the old scale, and are
 // encoded by the ratio of the two scales. Two loads one after the other (which row, then the row),
 // three barriers and the stores, on the workgroups with a new row: one cache of 4096 tokens of 16
-// heads of 72, a tenth of them in four runs 9.3 us; a fifth of the tokens of 8 such caches in runs 24,
-// scattered over every block 57 (166 MB). Four rows per wave ask for eight waves per SIMD: the
-// compiler then keeps its scalar registers few enough for two workgroups of 16 waves per CU (the
-// last case 77 us without).
+// heads of 72 a tenth of them in four runs 9.0 us, half 8.4, all 10.1, in float32 of 64 columns 6.2, 8.3,
+// 8.9; a fifth of the tokens of 8 such caches in runs 19, scattered over every block 52 (166 MB).
+// Except for blocks of 64 the rewriting forms ask for eight waves per SIMD: the compiler then
+// keeps its scalar registers few enough for them (blocks of 128, that scattered fifth 72 -> 57 us, one
+// cache's tenth 10.7 -> 11.0; blocks of 32 58 -> 52). Blocks of 64 run as well without (52 and 51 us,
+// the tenth 9.0 and 9.3).
 template <typename T, int NV, int WAVES, bool REWRITE, bool STREAM>
-__global__ __launch_bounds__(WAVES * kWave, REWRITE && NV == 4 ? 8 : 1) void quantize_kernel(Kv8Cache c, const T* __restrict__ kv, long row_stride,
-                                                            const int32_t* __restrict__ src_row, long kv_rows,
-                                                            int heads_per_group, int groups, int row_groups) {
+__global__ __launch_bounds__(WAVES * kWave, REWRITE && WAVES * NV != 64 ? 8 : 1) void quantize_kernel(
+    Kv8Cache c, const T* __restrict__ kv, long row_stride, const int32_t* __restrict__ src_row, long kv_rows,
+    int heads_per_group, int groups, int row_groups) {
     constexpr int CW = Piece<T>::N, R = WAVES * NV, kGroup = WAVES * kWave;
     __shared__ uint32_t s_need[R][kWave];   // [block of the rows][head of the group]: exponent byte, kNotFinite beside NaN and infinities
     constexpr uint32_t kNotFinite = 256;
@@ -254,7 +258,9 @@ __global__ __launch_bounds__(WAVES * kWave, REWRITE && NV == 4 ? 8 : 1) void qua
 // Values of the listed tokens: a workgroup takes `rows` of a request's list, its threads 16
 // bytes of output each (two such stores of every other 16 bytes were 10% slower), four at a
 // time so that their loads are in flight together. Bound by memory: 4 x ~3100 listed tokens of
-// 24 heads of 128 (233 MB) 36 us, 6.4 TB/s; with stores through the caches 57.
+// 24 heads of 128 (233 MB) 36 us, 6.4 TB/s, over the same buffers again and again; with stores
+// through the caches 57. Over buffers that no cache holds 43 (a copy of as much 41), in float32 of 64
+// columns (189 MB) 37.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dequantize_kernel(Kv8Cache c, Kv8Select sel, T* __restrict__ kv,
                                                               long row_stride, int rows) {
@@ -294,7 +300,8 @@ __global__ __launch_bounds__(kThreads) void dequantize_kernel(Kv8Cache c, Kv8Sel
 }
 
 // Ascending numbers of a request's tokens whose mask byte is zero: one workgroup
-// per request, kScanThreads tokens at a time, their places from a prefix sum.
+// per request, kScanThreads tokens at a time, their places from a prefix sum. A pass takes 0.6
+// us (a load, two barriers): 4096 tokens 4.1 us, 128 requests of them 4.6, 2^17 tokens 80 us, 2^20 630.
 constexpr int kScanThreads = 1024;
 __global__ __launch_bounds__(kScanThreads) void keys_kernel(const uint8_t* __restrict__ mask, int T,
                                                             int32_t* __restrict__ keys, int ld_keys,
@@ -383,13 +390,11 @@ void launch_quantize(const Kv8Cache& c, const QuantizeGrid& g, const void* kv, l
                      long kv_rows, hipStream_t s) {
     const dim3 grid((unsigned)g.workgroups);
     const T* p = static_cast<const T*>(kv);
-    // a rewrite does more per row: blocks of 64 by 16 waves of four rows, not 8 of eight (one cache of 4096
-    // tokens of 16 heads of 72, half of them new 7.3 instead of 8.8 us, all of them 11.1 instead of 12.7)
 #define MS_ROWS(r, nv, waves)                                                                                          \
     case r: hipLaunchKernelGGL((quantize_kernel<T, (nv), (waves), REWRITE, STREAM>), grid, dim3((waves) * kWave), 0, s, c, p, row_stride, \
                                src_row, kv_rows, g.per_group, g.groups, g.row_groups); break;
     switch (g.rows) {
-        MS_ROWS(16, 4, 4) MS_ROWS(32, 4, 8) MS_ROWS(64, (REWRITE ? 4 : 8), (REWRITE ? 16 : 8)) MS_ROWS(128, 8, 16)
+        MS_ROWS(16, 4, 4) MS_ROWS(32, 4, 8) MS_ROWS(64, 8, 8) MS_ROWS(128, 8, 16)
     }
 #undef MS_ROWS
 }
