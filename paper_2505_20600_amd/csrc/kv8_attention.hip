@@ -1074,8 +1074,8 @@ void launch_f32(const Kv8AttnDesc& a, hipStream_t s) {
 //  No less than the codes' bytes at 4.5 TB/s. More than one range: the join's launch, and the
 //  parts written and read.
 // Fitted to 5159 measured times (16 shapes of 1 to 64 requests of 500 to 16000 keys, head_dim 32 to
-// 128, 1 to 1600 rows, equal and ragged, every form, 1 to 64 ranges): the chosen pair takes 1.06
-// times the fastest on average. In us at the best count of ranges, 16 / 32 / 128 slots: 8 requests
+// 128, 1 to 1600 rows, equal and ragged, every form, 1 to 64 ranges): the chosen pair takes 1.05
+// times the fastest on average, 1.40 times at most (profiles/kv8_attention_plan_times.txt). In us at the best count of ranges, 16 / 32 / 128 slots: 8 requests
 // over 4096 keys of 16 heads of 64, 16 rows each 22 / 23 / 29, 32 rows 29 / 24 / 33, 64 rows 47 / 33 /
 // 37, 128 rows - / 52 / 46; 4 over 24 heads of 128, 32 rows 43 / 32 / 42, 96 rows - / 69 / 55; one of
 // 128 rows over 1024 keys of 12 heads of 64 - / 12 / 14. Ranges: 8 x 16 rows of 16 heads of 72
