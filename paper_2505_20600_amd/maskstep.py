@@ -683,7 +683,7 @@ class MaskStep:
             raise _kv8_bad(f"block must be a positive int, not {block!r}")
         S, blocks = scales[0].shape[0], -(-N // block)
         for l, t in enumerate(scales):
-            if t is not None and (t.shape != (S, blocks, 2, H) or t.element_size() != 1 or not t.is_contiguous()):
+            if t is not None and not isinstance(t, int) and (t.shape != (S, blocks, 2, H) or t.element_size() != 1 or not t.is_contiguous()):
                 raise _kv8_bad(f"scales[{l}] must be contiguous bytes [{S}][{blocks}][2][{H}] (block {block}), not {t.dtype} "
                                f"{tuple(t.shape)}")
         if per_request is None:
@@ -720,6 +720,10 @@ class MaskStep:
         codes); ``scales``: [L] device byte tensors [caches][ceil(N / block)][2][heads]; ``cache_of``: device int32 [B],
         each request's cache (pinned: scale table)."""
         L = self.desc.n_layers
+        if per_request is not None:
+            per_request = [list(r) for r in per_request]
+        elif codes is not None:
+            codes = list(codes)
         S = self._check_kv8(codes, scales, block, cache_of, pinned, slots, per_request)
         sc = (C.c_void_p * L)(*[_ptr(t) for t in scales])
         ptrs = (C.c_void_p * L)(*[_ptr(t) for t in codes]) if per_request is None else (C.c_void_p * 1)()
