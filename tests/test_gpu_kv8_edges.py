@@ -67,6 +67,62 @@ def test_step_does_not_read_scales_of_masked_blocks(shape, pinned):
     np.testing.assert_array_equal(S.Run(shape, mask, x, codes, scales, yc, ws, pinned=pinned).out(), want)
 
 
+@pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 72), ("bf16", 40), ("fp32", 64), ("fp32", 24)])
+@pytest.mark.parametrize("rows", [2, 30, 150])
+def test_unlisted_fresh_rows_have_no_effect(dtype, hd, rows):
+    """NaN in every fresh row that the list does not name, row 0 among them; list entries outside the rows; ranges that end
+    inside a tile; a request without fresh rows."""
+    g = torch.Generator().manual_seed(hd + rows)
+    codes, scales = K._cache(g, 2, 50, 2, hd, 16, dtype)
+    q = torch.randn(2 * rows, 2, hd, generator=g).to(K.DT[dtype]).to(DEV)
+    kv = K._rows(g, (120, 2, 2, hd), dtype)
+    rest = torch.randperm(119, generator=g)[:77] + 1
+    left = torch.ones(120, dtype=torch.bool)
+    left[rest] = False
+    kv[left.to(DEV)] = float("nan")
+    named = rest.int()
+    named[5], named[40] = -1, 120
+    start, fs = (torch.tensor(t, dtype=torch.int32, device=DEV) for t in ([0, rows, 2 * rows], [0, 77, 77]))
+    out = torch.empty_like(q)
+    MS.ms_kv8_attention(q, codes, scales, out, start, block=16, fresh=kv, fresh_list=named.to(DEV), fresh_start=fs)
+    for b in range(2):
+        k = kv8.values(codes[b].cpu().numpy(), scales[b].cpu().numpy(), 16)
+        if b == 0:
+            k = np.concatenate([k, K._np(kv)[named[(named >= 0) & (named < 120)].numpy()]])
+        rs = slice(b * rows, (b + 1) * rows)
+        ref, spread = kv8.attention(K._np(q[rs]), k[:, 0], k[:, 1], hd ** -0.5)
+        assert np.isfinite(ref).all()
+        assert np.all(np.abs(K._np(out[rs]) - ref) <= K._bound(q[rs], k, ref, spread, hd ** -0.5, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("block", [1, 8, 32, 64, 128])
+@pytest.mark.parametrize("fill", [0xff, 0x7f])
+def test_cache_filled_in_part(dtype, block, fill):
+    """Codes and scales of NaN all over, some tokens written through src_row: they read back and are attended over as if
+    the cache held nothing else; the rest stays NaN."""
+    g = torch.Generator().manual_seed(block)
+    T, H, hd = 300, 2, 64
+    codes, scales = K._empty_cache(1, T, H, hd, block, fill)
+    scales.fill_(255)
+    kv = K._rows(g, (90, 2, H, hd), dtype)
+    src = torch.full((1, T), -1, dtype=torch.int32)
+    src[0, 130:220] = torch.arange(90, dtype=torch.int32)
+    c, e = kv8.rewrite(codes[0].cpu().numpy(), scales[0].cpu().numpy(), block, K._np(kv), src[0].numpy())
+    MS.ms_kv8_quantize(kv, codes, scales, block=block, src_row=src.to(DEV))
+    assert np.array_equal(scales[0].cpu().numpy(), e) and K._same_codes(codes[0].cpu().numpy(), c)
+    vals = kv8.values(c, e, block)
+    assert np.isfinite(vals[130:220]).all() and np.isnan(vals[:130]).all() and np.isnan(vals[220:]).all()
+    keys = (130 + torch.randperm(90, generator=g)).int()[None].to(DEV)
+    for rows in (1, 30, 150):
+        q = torch.randn(rows, H, hd, generator=g).to(K.DT[dtype]).to(DEV)
+        out, start = torch.empty_like(q), torch.tensor([0, rows], dtype=torch.int32, device=DEV)
+        MS.ms_kv8_attention(q, codes, scales, out, start, block=block, keys=keys)
+        k = vals[keys[0].cpu().numpy()]
+        ref, spread = kv8.attention(K._np(q), k[:, 0], k[:, 1], 0.125)
+        assert np.all(np.abs(K._np(out) - ref) <= K._bound(q, k, ref, spread, 0.125, dtype))
+
+
 # ------------------------------------------------------------------ rewriting
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
