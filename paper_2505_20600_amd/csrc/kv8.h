@@ -47,9 +47,10 @@ __device__ __forceinline__ float2 kv8_to_f32x2(uint32_t w, float s) {
 
 // What x 2^(from - 127) is multiplied by, as x, for codes at the exponent byte b >= its need: 2^(from - b),
 // at least 2^-127 (below that every x of a code is far below half the smallest code, and so is its
-// product). Exact where the product is a normal float32; what is not is below half the smallest code.
+// product) and at most 2^127 (a code other than 0 never takes more than 2^17). Exact where the product is
+// a normal float32; what is not is below half the smallest code.
 __device__ __forceinline__ float kv8_ratio(int from, uint32_t b) {
-    const int e = from - (int)b + 127;      // at most 253
+    const int e = min(from - (int)b + 127, 254);
     return __uint_as_float(e <= 0 ? 0x00400000u : (uint32_t)e << 23);
 }
 

@@ -162,6 +162,29 @@ def test_rewrite_beside_the_largest_value(dtype, width):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_kept_zeros_of_a_large_scale_stay_zeros(dtype):
+    """One row of large values in every block is replaced by small ones of 1 to 2^-150 times their size (from every scale
+    to every smaller one, those more than 2^127 apart included); the zeros beside it, of both signs, keep their codes."""
+    scales = torch.arange(120, 255).view(1, -1, 1, 1).expand(1, -1, 2, 1)
+    n = scales.shape[1]
+    codes = torch.zeros(1, n, 4, 2, 1, 8, dtype=torch.uint8)
+    codes[..., 1::2] = 0x80
+    codes[:, :, 2] = 126
+    for less in range(0, 151):
+        kv = torch.ldexp(torch.ones(n, 2, 1, 8, dtype=torch.float64), (scales[0, :, :1].view(n, 1, 1, 1) - 127 - less).int())
+        kv = kv.to(torch.float32).to(K.DT[dtype])
+        src = torch.full((1, n, 4), -1, dtype=torch.int32)
+        src[0, :, 2] = torch.arange(n, dtype=torch.int32)
+        dc, ds = codes.view(1, 4 * n, 2, 1, 8).to(DEV), scales.to(torch.uint8).to(DEV).contiguous()
+        MS.ms_kv8_quantize(kv.to(DEV), dc, ds, block=4, src_row=src.view(1, -1).to(DEV))
+        assert torch.equal(dc.view(1, n, 4, 2, 1, 8)[:, :, [0, 1, 3]].cpu(), codes[:, :, [0, 1, 3]]), f"2^-{less}"
+        if less % 25 == 0:
+            c, e = kv8.rewrite(codes.view(4 * n, 2, 1, 8).numpy(), scales[0].to(torch.uint8).numpy(), 4, K._np(kv),
+                               src.view(-1).numpy())
+            assert np.array_equal(ds[0].cpu().numpy(), e) and K._same_codes(dc[0].cpu().numpy(), c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("block,T", [(1, 40), (4, 70), (32, 100), (64, 200), (128, 300)])
 @pytest.mark.parametrize("special", [False, True], ids=["finite", "nan"])
 def test_rewrite_of_every_scale_is_exact(dtype, block, T, special):
