@@ -18,8 +18,10 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmaskstep.so")
 
 SOURCES = ["compact.hip", "rows.hip", "gemm.hip", "attention.hip", "maskstep.hip", "noalloc.hip",
-           "copyplan.hip", "probes.hip", "kv8.hip", "kv8_attention.hip", "kv8_api.hip"]
-HEADERS = ["attn_tiles.h", "common.h", "kernels.h", "kv8.h", "step_internal.h"]
+           "copyplan.hip", "probes.hip", "kv8.hip", "kv8_attention.hip", "kv8_api.hip",
+           "mx4.hip", "mx4_linear.hip", "qk_norm_rope.hip", "shared_attention.hip", "block_ops_api.hip"]
+HEADERS = ["attn_tiles.h", "common.h", "gelu.h", "kernels.h", "kv8.h", "mx4.h", "qk_norm_rope.h", "shared_attention.h",
+           "step_internal.h"]
 
 ARCH = "gfx950"
 FLAGS = [

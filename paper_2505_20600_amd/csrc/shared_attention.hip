@@ -1,0 +1,936 @@
+// Attention of a batch whose requests share a long prefix: packed query rows over
+// one prefix's K/V rows, less the tokens that the row's request hides, and over
+// the request's own K/V rows, one softmax over both. A row without any key is 0.
+//
+// A query slot is a (packed row, query head of one K/V head's group) pair. Slots of
+// all requests stand in one row and are cut into tiles that go across requests, so
+// that a prefix tile is fetched and multiplied once for as many slots as a tile
+// has, however few rows each request brings. What a request does not see is a
+// matter of each score: every lane has the hidden tokens of its slot's request as one
+// word per key tile. Own rows lie behind each other in the order of the requests; a
+// slot tile walks over those of its first to its last request, and a slot sees its
+// own request's.
+//
+// Tiles of K and V rows land in LDS by direct loads. The products run in the layout
+// of attention.hip: S^T = K Q^T leaves the weights in the operand layout of O^T =
+// V^T P^T, V is read transposed by ds_read_b64_tr_b16, rows of ones in V^T give the
+// denominator. Scores, maxima, sums and the parts of key ranges are float32. bf16
+// rounds twice: the weights, the matrix cores' operand of the second product (numerator
+// and denominator take the same rounded ones), and the output.
+//
+// A hidden key's weight is 0, and 0 times an infinity or NaN in its V row is NaN: a
+// slot whose result is not finite is computed again over the keys that it sees, one
+// wave at a slot (recompute). Finite inputs never come there.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "attn_tiles.h"
+#include "kernels.h"
+#include "shared_attention.h"
+
+namespace ms {
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// A workgroup's query slots and key tiles.
+struct Work {
+    int row0;       // first packed row of all
+    int slots;      // slots in all
+    int q0;         // first slot of this tile
+    int kvh;        // K/V head
+    int split;
+    int t0, t1;     // key tiles: those of the prefix, then the own ones
+    int ntp;        // prefix tiles
+    int f0, f1;     // own rows of the tile's requests
+};
+
+// The tables of a workgroup's requests in LDS: where each one's rows start, and its own rows.
+struct Tables {
+    int32_t row[kSharedMaxBatch + 1];
+    int32_t own[kSharedMaxBatch + 1];
+};
+
+// Request of packed row r: the last one that starts at or before it (any request where starts do not ascend).
+__device__ __forceinline__ int request_of(const SharedAttnDesc& a, const Tables& t, int r) {
+    int lo = 0, hi = a.batch;               // row[lo] <= r or lo = 0, row[hi] > r or hi = batch
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (t.row[mid] <= r) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Row index of a query slot's (row, query head) in [M][n_heads].
+__device__ __forceinline__ long slot_row(const SharedAttnDesc& a, const Work& w, int slot) {
+    const int HG = a.heads * a.group;
+    const int r = a.group == 1 ? slot : slot / a.group;
+    return (long)(w.row0 + r) * HG + w.kvh * a.group + (slot - r * a.group);
+}
+
+// Fills the tables and the workgroup's work; false where it has no slot. A barrier for the whole workgroup.
+template <int QT, int KT>
+__device__ __forceinline__ bool find_work(const SharedAttnDesc& a, int tile, int kvh, int split, Tables& t, Work& w) {
+    for (int i = threadIdx.x; i <= a.batch; i += kThreads) {
+        t.row[i] = a.seg_start ? min(max(a.seg_start[i], 0), a.M) : i == 0 ? 0 : a.M;
+        t.own[i] = a.fresh ? min(max(a.fresh_start[i], 0), a.fresh_rows) : 0;
+    }
+    __syncthreads();
+    w.row0 = uniform(t.row[0]);
+    w.slots = uniform(max(t.row[a.batch] - w.row0, 0)) * a.group;
+    w.q0 = tile * QT;
+    w.kvh = kvh;
+    w.split = split;
+    if (w.q0 >= w.slots) return false;
+    const int first = request_of(a, t, w.row0 + w.q0 / a.group);
+    const int last = request_of(a, t, w.row0 + (min(w.q0 + QT, w.slots) - 1) / a.group);
+    w.f0 = uniform(t.own[first]);
+    w.f1 = max(uniform(t.own[last + 1]), w.f0);
+    w.ntp = (a.T + KT - 1) / KT;
+    const uint32_t nt = w.ntp + (w.f1 - w.f0 + KT - 1) / KT;    // below 2^24; times 64 ranges below 2^32
+    w.t0 = uniform((int)(nt * split / a.nsplit));
+    w.t1 = uniform((int)(nt * (split + 1) / a.nsplit));
+    return true;
+}
+
+// KT low bits: those of the positions below n.
+template <int KT>
+__device__ __forceinline__ uint64_t below(int n) {
+    return n >= KT ? (KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1) : n <= 0 ? 0ull : (1ull << n) - 1;
+}
+
+// Which keys of the tiles one slot sees.
+template <int KT>
+struct Sight {
+    const uint64_t* bits;       // its request's hidden tokens, NULL: it sees every one
+    int lo, hi;                 // its request's own rows
+    __device__ __forceinline__ void init(const SharedAttnDesc& a, const Tables& t, const Work& w, int slot) {
+        const int s = min(slot, w.slots - 1);
+        const int b = request_of(a, t, w.row0 + s / a.group);
+        bits = a.bits ? a.bits + (long)b * a.words : nullptr;
+        lo = t.own[b];
+        hi = max(t.own[b + 1], lo);
+    }
+    // hidden ones among prefix tile t's keys, as loaded
+    __device__ __forceinline__ uint64_t fetch(const SharedAttnDesc& a, int t) const {
+        if (!bits) return 0ull;
+        if constexpr (KT == 64) return bits[min(t, a.words - 1)];
+        else return reinterpret_cast<const uint32_t*>(bits)[min(t, 2 * a.words - 1)];
+    }
+    __device__ __forceinline__ uint64_t prefix(const SharedAttnDesc& a, uint64_t hidden, int t) const {
+        return ~hidden & below<KT>(a.T - t * KT);
+    }
+    // of the own tile of rows k0 on
+    __device__ __forceinline__ uint64_t own(int k0) const { return below<KT>(hi - k0) & ~below<KT>(lo - k0); }
+};
+
+// One slot's result over the keys [t0, t1) that it sees, by a wave: 64 keys at a time, a
+// lane's key's score, then the lanes as columns of the weighted sum.
+template <typename T, int KT>
+__device__ __forceinline__ void recompute(const SharedAttnDesc& a, const Work& w, const Tables& t, int slot) {
+    const int lane = threadIdx.x % kWave, hd = a.hd, dkv = a.heads * hd;
+    Sight<64> sight;
+    sight.init(a, t, w, slot);
+    const long at = slot_row(a, w, slot);
+    const T* const q = static_cast<const T*>(a.q) + at * hd;
+    float m = -INFINITY, l = 0.f, o[2] = {0.f, 0.f};
+    for (int part = 0; part < 2; ++part) {
+        const T* const kv = static_cast<const T*>(part ? a.fresh : a.kv) + w.kvh * hd;
+        const int k0 = part ? max(w.f0 + (w.t0 - w.ntp) * KT, sight.lo) : w.t0 * KT;
+        const int k1 = part ? min(w.f0 + (w.t1 - w.ntp) * KT, sight.hi) : min(min(w.t1, w.ntp) * KT, a.T);
+        for (int k = k0; k < k1; k += kWave) {
+            const int key = k + lane;
+            bool sees = key < k1;
+            if (sees && !part && sight.bits) sees = !((sight.bits[key / 64] >> (key % 64)) & 1);
+            float s = -INFINITY;
+            if (sees) {
+                const T* const row = kv + (long)key * 2 * dkv;
+                float dot = 0.f;
+                for (int c = 0; c < hd; ++c) dot = fmaf(Elt<T>::to_f32(q[c]), Elt<T>::to_f32(row[c]), dot);
+                s = dot * a.scale_log2;
+            }
+            const uint64_t seen = __ballot(sees);
+            const uint64_t nan = __ballot(s != s);
+            float up = fmaxf(m, wave_max(s));
+            if (nan) up = __uint_as_float(0x7fc00000u);         // maxima drop NaN
+            const float ref = up == -INFINITY ? 0.f : up;
+            const float corr = m == -INFINITY ? 0.f : fast_exp2(m - ref);
+            const float p = sees ? fast_exp2(s - ref) : 0.f;
+            m = up;
+            l = l * corr + wave_sum(p);
+            o[0] *= corr;
+            o[1] *= corr;
+            for (int j = 0; j < kWave; ++j) {
+                if (!((seen >> j) & 1)) continue;
+                const float pj = __shfl(p, j, kWave);
+                const T* const row = kv + (long)(k + j) * 2 * dkv + dkv;
+                if (lane < hd) o[0] = fmaf(pj, Elt<T>::to_f32(row[lane]), o[0]);
+                if (lane + kWave < hd) o[1] = fmaf(pj, Elt<T>::to_f32(row[lane + kWave]), o[1]);
+            }
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const long part = (long)w.split * a.M * a.heads * a.group + at;
+    for (int i = 0; i < 2; ++i) {
+        const int c = lane + i * kWave;
+        if (c >= hd) continue;
+        if (a.nsplit == 1) static_cast<T*>(a.o)[at * hd + c] = Elt<T>::from_f32(o[i] * inv);
+        else a.part_o[part * hd + c] = o[i] * inv;
+    }
+    if (a.nsplit > 1 && lane == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * part) = make_float2(m, l);
+}
+
+// The flagged slots of a tile again, the waves in turn; `bad` [QT / 32] in LDS, complete.
+template <typename T, int QT, int KT>
+__device__ __forceinline__ void recompute_bad(const SharedAttnDesc& a, const Work& w, const Tables& t, const uint32_t* bad, int wave) {
+    for (int i = 0; i < (QT + 31) / 32; ++i) {
+        const uint32_t b = uniform((int)bad[i]);
+        if (!b) continue;
+        for (int s = wave; s < 32; s += kThreads / kWave)
+            if ((b >> s) & 1) recompute<T, KT>(a, w, t, w.q0 + i * 32 + s);
+    }
+}
+
+// The four waves' sums of 16 slots, from slot `first` of the tile on, each relative to its own maximum (so
+// [wave][slot][OLD] and sml [wave][slot]), to the output or the key range's part; slots without a finite result are flagged.
+template <typename T, int HD, int OLD>
+__device__ __forceinline__ void join_waves(const SharedAttnDesc& a, const Work& w, const float* so, const float2* sml, int tid,
+                                           int first, uint32_t* bad) {
+    const int s = tid / 16, slot = w.q0 + first + s;
+    if (slot >= w.slots) return;
+    float m = -INFINITY, f[4], sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) m = fmaxf(m, sml[v * 16 + s].x);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const float2 ml = sml[v * 16 + s];
+        f[v] = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
+        sum += f[v] * ml.y;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    bool fine = finite(sum);
+    const long row = slot_row(a, w, slot), part = (long)w.split * a.M * a.heads * a.group + row;
+    for (int c = (tid % 16) * 4; c < HD; c += 64) {
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const float4 x = *reinterpret_cast<const float4*>(so + (v * 16 + s) * OLD + c);
+            o[0] += f[v] * x.x; o[1] += f[v] * x.y; o[2] += f[v] * x.z; o[3] += f[v] * x.w;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            fine = fine && finite(o[r]);
+            o[r] *= inv;
+        }
+        if (a.nsplit == 1) store4<T>(static_cast<T*>(a.o) + row * HD + c, o);
+        else store4<float>(a.part_o + part * HD + c, o);
+    }
+    if (a.nsplit > 1 && tid % 16 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * part) = make_float2(m, sum);
+    if (!fine) atomicOr(bad, 1u << (first + s));
+}
+
+// Tiles of KT K rows and V rows by direct-to-LDS loads of NW waves, [K rows][V rows][zeros].
+template <int HD, int KT, int NW>
+struct Tiles {
+    static constexpr int ROWB = HD * 2, TILEB = KT * ROWB, PAD = 64;
+    static constexpr int STAGEB = 2 * TILEB + PAD;
+    static constexpr int NQ = 2 * TILEB / 1024;             // 1 KB copies per tile
+    static constexpr int IPW = (NQ + NW - 1) / NW;          // per wave, most
+    static_assert(2 * TILEB % 1024 == 0, "tile copies");
+    static constexpr bool SWZ = ROWB == 128 || ROWB == 256 || ROWB % 128 == 64;
+    static constexpr uint32_t kAbsent = 0xfff00000u;
+    u32x4_t rsrc;
+    uint32_t row_bytes, voff[IPW];
+    int rl[IPW], end;
+
+    // rows [0, rows) of kv
+    __device__ __forceinline__ void init(const void* kv, int rows, int heads, int kvh, int wave, int lane) {
+        row_bytes = 4u * heads * HD;
+        rsrc = raw_rsrc(kv, (uint32_t)rows * row_bytes);
+        end = rows;
+#pragma unroll
+        for (int i = 0; i < IPW; ++i) {
+            const int pos = min(i * NW + wave, NQ - 1) * 1024 + lane * 16;
+            const bool isv = pos >= TILEB;
+            const int p = isv ? pos - TILEB : pos, r = p / ROWB;
+            rl[i] = r;
+            voff[i] = (uint32_t)r * row_bytes + (isv ? row_bytes / 2 : 0u) + kvh * ROWB +
+                      (((p % ROWB) / 16) ^ (isv ? v_swz<ROWB>(r) : k_swz<ROWB>(r))) * 16;
+        }
+    }
+    // rows k0 on into the stage at LDS address `lds`; rows past the last read as zeros
+    __device__ __forceinline__ void issue(int k0, int wave, uint32_t lds) {
+        const uint32_t base = (uint32_t)k0 * row_bytes;
+        const bool whole = k0 + KT <= end;
+#pragma unroll
+        for (int i = 0; i < IPW; ++i) {
+            const uint32_t o = whole || k0 + rl[i] < end ? voff[i] + base : kAbsent;
+            if (NQ % NW == 0 || i * NW + wave < NQ) dma_buf16(rsrc, o, 0, lds + (uint32_t)(i * NW + wave) * 1024u);
+        }
+    }
+};
+
+template <int HD, int QT_>
+struct Cfg {
+    static constexpr int QT = QT_;
+    static constexpr bool WIDE = QT == 128;             // waves have slots of their own and share the key tiles
+    static constexpr int KT = WIDE ? 64 : 32;
+    static constexpr int NQB = QT == 16 ? 1 : 2;        // 16-slot blocks per wave
+    static constexpr int NW = WIDE ? 4 : 1;             // waves that load a tile
+    using S = Tiles<HD, KT, NW>;
+    static constexpr int NKS = KT / 16;
+    static constexpr int NK32 = (HD + 31) / 32;
+    static constexpr bool KTAIL = HD % 32 != 0;
+    static constexpr bool SUM_IN_PAD = HD % 16 != 0;
+    static constexpr int NREAL = (HD + 15) / 16;
+    static constexpr int NHS = NREAL + (SUM_IN_PAD ? 0 : 1);
+    static constexpr int OLD = HD + 4;
+    static constexpr int STAGES = 2;
+    static constexpr int TILES = (WIDE ? STAGES : 4 * STAGES) * S::STAGEB;
+    static constexpr int JOIN = WIDE ? 4 * 32 * 2 * S::ROWB : (4 * 16 * OLD + 4 * 16 * 2) * 4;
+    static constexpr int LDSB = ((TILES > JOIN ? TILES : JOIN) + 63) / 64 * 64;
+};
+
+constexpr int wide_per_cu(int hd) { return hd <= 48 ? 4 : hd <= 64 ? 3 : 2; }
+constexpr int few_per_cu(int hd) { return hd <= 32 ? 4 : hd <= 48 ? 3 : hd <= 72 ? 2 : 1; }
+
+// bf16. WIDE: 128 slots, 32 per wave; the four waves share 64-key tiles in two stages.
+// Not WIDE: 16 or 32 slots, all of them in every wave, and every wave has 32-key tiles of its own (tile
+// t0 + wave + 4 i) in two stages of its own, without a barrier; the four partial results are joined at the end.
+template <int HD, int QT>
+__global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(HD)) void shared_bf16_kernel(SharedAttnDesc a, int qtiles) {
+    using C = Cfg<HD, QT>;
+    using S = typename C::S;
+    constexpr bool WIDE = C::WIDE;
+    constexpr int NQB = C::NQB, NKS = C::NKS, KT = C::KT;
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDSB + 16];
+    __shared__ Tables tables;
+    __shared__ uint32_t bad[QT / 32 + 1];
+    const uint32_t lds0 = lds_addr(smem);
+    const uint32_t ones_rel = C::LDSB;                  // 8 bytes of bf16 ones (SUM_IN_PAD)
+    const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave);
+    const int grp = lane / 16, l16 = lane % 16;
+    // WIDE: a head's slot tiles side by side, so that an XCD's L2 serves the head's rows to all of
+    // them. Else a (tile, range) pair's heads side by side, which read neighbouring parts of the same rows.
+    Work w;
+    if constexpr (WIDE) {
+        const int lb = xcd_logical_block(blockIdx.x, qtiles * a.nsplit * a.heads);
+        if (!find_work<QT, KT>(a, lb % qtiles, lb / (qtiles * a.nsplit), lb / qtiles % a.nsplit, tables, w)) return;
+    } else {
+        const int i = blockIdx.x / kXcds, pair = i / a.heads * kXcds + blockIdx.x % kXcds;
+        if (pair >= qtiles * a.nsplit) return;
+        if (!find_work<QT, KT>(a, pair / a.nsplit, i % a.heads, pair % a.nsplit, tables, w)) return;
+    }
+    constexpr int step = WIDE ? 1 : 4;
+
+    // constant LDS: zeros behind the tiles, the ones block
+    constexpr int NSTG = (WIDE ? 1 : 4) * C::STAGES;
+    if (tid < 4 * NSTG) *reinterpret_cast<uint4*>(smem + (tid / 4) * S::STAGEB + 2 * S::TILEB + (tid % 4) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == 4 * NSTG) *reinterpret_cast<uint2*>(smem + C::LDSB) = make_uint2(0x3f803f80u, 0x3f803f80u);
+    if (tid < QT / 32 + 1) bad[tid] = 0;
+
+    // Q^T fragments (B operand), their sign that of the score scale
+    bf16x8_t qf[NQB][C::NK32];
+    Sight<KT> sight[NQB];
+    const bf16_t* __restrict__ q = static_cast<const bf16_t*>(a.q);
+    const int wq0 = w.q0 + (WIDE ? wave * 32 : 0);
+    const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+        const int slot = wq0 + qb * 16 + l16;
+        const bf16_t* qp = q + slot_row(a, w, slot) * HD;
+        sight[qb].init(a, tables, w, slot);
+#pragma unroll
+        for (int kc = 0; kc < C::NK32; ++kc) {
+            vec16 v = {{0u, 0u, 0u, 0u}};
+            if (slot < w.slots && kc * 32 + grp * 8 < HD) v = ld16(qp + kc * 32 + grp * 8);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v.w[j] ^= flip;
+            qf[qb][kc] = __builtin_bit_cast(bf16x8_t, v);
+        }
+    }
+
+    // fragment read offsets inside a stage (bytes)
+    const int fK = k_swz<S::ROWB>(l16);
+    uint32_t koff[C::NK32];
+#pragma unroll
+    for (int kc = 0; kc < C::NK32; ++kc) koff[kc] = l16 * S::ROWB + (((4 * kc + grp) ^ fK) * 16);
+    // last QK step of a head_dim that is not a multiple of 32: lanes whose columns lie past the row read zeros
+    static_assert(!C::KTAIL || !S::SWZ, "tail offsets");
+    const bool in_row = (C::NK32 - 1) * 64 + grp * 16 < S::ROWB;
+    const int rowA = 4 * grp + (l16 >> 2);
+    const int fV = v_swz<S::ROWB>(rowA);
+    uint32_t voffh[C::NREAL];
+#pragma unroll
+    for (int h = 0; h < C::NREAL; ++h) {
+        const int hd = 16 * h + 4 * (l16 & 3);
+        voffh[h] = S::TILEB + rowA * S::ROWB + (((hd / 8) ^ fV) * 16) + (hd % 8) * 2;
+    }
+    const bool ones_lane = C::SUM_IN_PAD && (16 * (C::NREAL - 1) + 4 * (l16 & 3)) >= HD;
+
+    f32x4_t oacc[NQB][C::NHS];
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+        for (int h = 0; h < C::NHS; ++h) oacc[qb][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const float cs = fabsf(a.scale_log2), rescale_at = kRescaleLog2 / cs;
+    float m_run[NQB];
+    f32x4_t negm[NQB];
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+        m_run[qb] = -INFINITY;
+        negm[qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    bool beyond = true;
+    const bf16x8_t onesf = __builtin_bit_cast(bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
+    constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
+
+    auto qk = [&](uint32_t sbase, f32x4_t (&sacc)[NQB][NKS]) {
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) sacc[qb][ks] = negm[qb];
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+#pragma unroll
+            for (int kc = 0; kc < C::NK32; ++kc) {
+                uint32_t at = koff[kc] + ks * 16 * S::ROWB;
+                if (C::KTAIL && kc == C::NK32 - 1) at = in_row ? at : (uint32_t)(2 * S::TILEB);
+                const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(smem + sbase + at);
+#pragma unroll
+                for (int qb = 0; qb < NQB; ++qb) sacc[qb][ks] = mfma32(kf, qf[qb][kc], sacc[qb][ks]);
+            }
+        }
+    };
+    // scores of keys that a slot does not see become -infinity, whatever they were
+    auto hide = [&](const uint64_t (&sees)[NQB], f32x4_t (&sacc)[NQB][NKS]) {
+        bool all = true;
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) all = all && sees[qb] == kAll;
+        if (__all(all)) return;
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+            const uint64_t mine = sees[qb] >> (grp * 4);
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (!((mine >> (ks * 16 + r)) & 1)) sacc[qb][ks][r] = -INFINITY;
+        }
+    };
+    // online softmax in place: sacc becomes the weights; running maxima and accumulators
+    // updated, a rescale only where a score exceeds its slot's maximum by more than 2^8
+    auto softmax = [&](f32x4_t (&sacc)[NQB][NKS]) {
+        float mx[NQB];
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+            mx[qb] = sacc[qb][0][0];
+#pragma unroll
+            for (int i = 1; i < 4 * NKS; ++i) mx[qb] = fmaxf(mx[qb], sacc[qb][i / 4][i % 4]);
+        }
+        float most = mx[0];
+#pragma unroll
+        for (int qb = 1; qb < NQB; ++qb) most = fmaxf(most, mx[qb]);
+        if (beyond || __any(most > rescale_at)) {
+            bool far = false;
+#pragma unroll
+            for (int qb = 0; qb < NQB; ++qb) {
+                const float rm = rows_max(mx[qb]);
+                const bool none = m_run[qb] == -INFINITY;
+                const float was = none ? -INFINITY : m_run[qb] + negm[qb][0];
+                const float up = fmaxf(rm, was);
+                const bool still = up == -INFINITY;
+                const float corr = none ? 0.f : fast_exp2((was - up) * cs);
+#pragma unroll
+                for (int h = 0; h < C::NHS; ++h) oacc[qb][h] *= corr;
+                m_run[qb] = fmaxf(m_run[qb], rm - negm[qb][0]);
+                const float n = m_run[qb] == -INFINITY ? 0.f : -fminf(fmaxf(m_run[qb], -kStartMax), kStartMax);
+                negm[qb] = f32x4_t{n, n, n, n};
+                far |= fabsf(m_run[qb]) > kStartMax;
+                const float off = still ? 0.f : up;
+#pragma unroll
+                for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sacc[qb][ks][r] -= off;
+            }
+            beyond = __any(far);
+        }
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sacc[qb][ks][r] = fast_exp2(sacc[qb][ks][r] * cs);
+    };
+    auto pv = [&](uint32_t sbase, f32x4_t (&sacc)[NQB][NKS]) {
+        // without a swizzle the blocks of 16 columns lie 32 bytes apart, an offset of the reads
+        constexpr int NB = S::SWZ ? C::NREAL : 1;
+        uint32_t vbase[NB];
+#pragma unroll
+        for (int h = 0; h < NB; ++h) {
+            vbase[h] = lds0 + sbase + voffh[h];
+            asm volatile("" : "+v"(vbase[h]));   // keep the sum: offsets are added per read
+        }
+#pragma unroll
+        for (int c = 0; c < KT / 32; ++c) {
+            bf16x8_t vf[C::NHS];
+#pragma unroll
+            for (int h = 0; h < C::NHS; ++h) {
+                if (h >= C::NREAL) {
+                    vf[h] = onesf;
+                } else {
+                    const lds_cptr vb = (lds_cptr)(uintptr_t)vbase[S::SWZ ? h : 0] + (S::SWZ ? 0 : 32 * h);
+                    lds_cptr p0 = vb + (32 * c) * S::ROWB, p1 = vb + (32 * c + 16) * S::ROWB;
+                    if (h == C::NREAL - 1 && ones_lane) { p0 = (lds_cptr)(uintptr_t)(lds0 + ones_rel); p1 = p0; }
+                    const bf16x4_t lo = ld_tr16(p0), hi = ld_tr16(p1);
+                    vf[h] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+            }
+            bf16x8_t pf[NQB];
+#pragma unroll
+            for (int qb = 0; qb < NQB; ++qb) {
+                uint4 p;
+                p.x = pack_bf16x2(sacc[qb][2 * c][0], sacc[qb][2 * c][1]);
+                p.y = pack_bf16x2(sacc[qb][2 * c][2], sacc[qb][2 * c][3]);
+                p.z = pack_bf16x2(sacc[qb][2 * c + 1][0], sacc[qb][2 * c + 1][1]);
+                p.w = pack_bf16x2(sacc[qb][2 * c + 1][2], sacc[qb][2 * c + 1][3]);
+                pf[qb] = __builtin_bit_cast(bf16x8_t, p);
+            }
+#pragma unroll
+            for (int h = 0; h < C::NHS; ++h)
+#pragma unroll
+                for (int qb = 0; qb < NQB; ++qb) oacc[qb][h] = mfma32(vf[h], pf[qb], oacc[qb][h]);
+        }
+    };
+
+    f32x4_t sa[NQB][NKS];
+    const bool active = wq0 < w.slots;
+    // Tiles [from, to) of one kind (tile 0 at row `base` of kv, `rows` of them from there on in all): while a tile is
+    // multiplied the next one lands in the other stage.
+    auto run = [&](auto OWN, const void* kv, int base, int rows, int from, int to, int skip) __attribute__((always_inline)) {
+        if constexpr (!WIDE) from += (wave - skip) & 3;     // the waves go on in turn from one kind to the next
+        if (from >= to) return;     // the whole workgroup, or a wave that waits for no other
+        const int lw = WIDE ? wave : 0;
+        S st;
+        st.init(kv, rows, a.heads, w.kvh, lw, lane);
+        auto stage = [&](int n) { return (uint32_t)((WIDE ? (n & 1) : wave * 2 + (n & 1)) * S::STAGEB); };
+        uint64_t hidden[NQB];
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) hidden[qb] = OWN ? 0ull : sight[qb].fetch(a, from);
+        st.issue(base + from * KT, lw, lds0 + stage(0));
+        int n = 0;
+        for (int t = from; t < to; t += step, ++n) {
+            wait_all();   // tile t has landed, and this wave's reads of the stage refilled below are done
+            if constexpr (WIDE) barrier_only();
+            else asm volatile("" ::: "memory");
+            uint64_t sees[NQB];
+#pragma unroll
+            for (int qb = 0; qb < NQB; ++qb) {
+                sees[qb] = OWN ? sight[qb].own(base + t * KT) : sight[qb].prefix(a, hidden[qb], t);
+                asm volatile("" : "+v"(sees[qb]));      // used before the next loads are under way
+            }
+            if (t + step < to) {
+#pragma unroll
+                for (int qb = 0; qb < NQB; ++qb)
+                    if constexpr (!OWN) hidden[qb] = sight[qb].fetch(a, t + step);
+                st.issue(base + (t + step) * KT, lw, lds0 + stage(n + 1));
+            }
+            if (WIDE && !active) continue;
+            qk(stage(n), sa);
+            hide(sees, sa);
+            softmax(sa);
+            pv(stage(n), sa);
+        }
+        if constexpr (WIDE) {
+            wait_all();
+            barrier_only();   // the stages may be written again
+        } else {
+            wait_all();
+        }
+    };
+    __syncthreads();   // constant LDS
+    const int c0 = min(w.t0, w.ntp), c1 = min(w.t1, w.ntp);
+    run(std::false_type{}, a.kv, 0, a.T, c0, c1, 0);
+    if (w.f1 > w.f0) run(std::true_type{}, a.fresh, w.f0, w.f1, max(w.t0 - w.ntp, 0), max(w.t1 - w.ntp, 0), c1 - c0);
+
+    float l[NQB];
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+        if constexpr (C::SUM_IN_PAD) {
+            // the last 8 rows of the last subtile are the ones rows: lane groups 2-3 hold them
+            const float t0 = grp >= 2 ? oacc[qb][C::NHS - 1][0] : 0.f;
+            auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(t0), __float_as_uint(t0), false, false);
+            l[qb] = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+        } else {
+            l[qb] = oacc[qb][C::NHS - 1][0];
+        }
+    }
+    const long range = (long)w.split * a.M * a.heads * a.group;
+    __syncthreads();   // every wave is past its last read of the stages
+    if constexpr (WIDE) {
+        // through LDS: rows of a slot in 16-byte vectors, chunks swizzled by the slot where rows are a power of two
+        constexpr int CH = HD / 8, CF = HD / 4;
+        constexpr int SWM = (CH & (CH - 1)) == 0 ? (CH >= 16 ? 15 : CH - 1) : 0;
+        constexpr int SWF = (CF & (CF - 1)) == 0 ? (CF >= 16 ? 15 : CF - 1) : 0;
+        uint8_t* const so = smem + wave * 32 * S::ROWB * (a.nsplit == 1 ? 1 : 2);
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+            const float inv_l = l[qb] == 0.f ? 0.f : 1.0f / l[qb];
+            const int rl = qb * 16 + l16;
+            bool fine = finite(l[qb]);
+#pragma unroll
+            for (int h = 0; h < C::NHS; ++h) {
+                const int cidx = h * 16 + grp * 4;
+                if (cidx < HD) {
+                    float v[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        fine = fine && finite(oacc[qb][h][r]);
+                        v[r] = oacc[qb][h][r] * inv_l;
+                    }
+                    if (a.nsplit == 1)
+                        store4<bf16_t>(reinterpret_cast<bf16_t*>(so + rl * S::ROWB + (((cidx / 8) ^ (rl & SWM)) * 16) + (cidx % 8) * 2), v);
+                    else
+                        store4<float>(reinterpret_cast<float*>(so + rl * 2 * S::ROWB) + ((cidx / 4) ^ (rl & SWF)) * 4, v);
+                }
+            }
+            const int slot = wq0 + rl;
+            if (!fine && slot < w.slots) atomicOr(&bad[wave], 1u << rl);
+            if (a.nsplit > 1 && grp == 0 && slot < w.slots)
+                *reinterpret_cast<float2*>(a.part_ml + 2 * (range + slot_row(a, w, slot))) = make_float2(m_run[qb] * cs, l[qb]);
+        }
+        __syncthreads();
+        if (a.nsplit == 1) {
+            for (int k = lane; k < 32 * CH; k += kWave) {
+                const int rl = k / CH, c = k % CH;
+                if (wq0 + rl < w.slots)
+                    st16(static_cast<bf16_t*>(a.o) + slot_row(a, w, wq0 + rl) * HD + c * 8,
+                         ld16(so + rl * S::ROWB + ((c ^ (rl & SWM)) * 16)));
+            }
+        } else {
+            for (int k = lane; k < 32 * CF; k += kWave) {
+                const int rl = k / CF, c = k % CF;
+                if (wq0 + rl < w.slots)
+                    st16(a.part_o + (range + slot_row(a, w, wq0 + rl)) * HD + c * 4,
+                         ld16(so + rl * 2 * S::ROWB + ((c ^ (rl & SWF)) * 16)));
+            }
+        }
+    } else {
+        // the four waves' sums, each relative to its own maximum, joined through LDS 16 slots at a time
+        constexpr int OLD = C::OLD;
+        float* const so = reinterpret_cast<float*>(smem);
+        float2* const sml = reinterpret_cast<float2*>(so + 4 * 16 * OLD);
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+            if (qb > 0) __syncthreads();
+#pragma unroll
+            for (int h = 0; h < C::NREAL; ++h) {
+                const int cidx = h * 16 + grp * 4;
+                if (cidx < HD) {
+                    float v[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = oacc[qb][h][r];
+                    store4<float>(so + (wave * 16 + l16) * OLD + cidx, v);
+                }
+            }
+            if (grp == 0) sml[wave * 16 + l16] = make_float2(m_run[qb] * cs, l[qb]);
+            __syncthreads();
+            join_waves<bf16_t, HD, OLD>(a, w, so, sml, tid, qb * 16, &bad[0]);
+        }
+    }
+    __syncthreads();    // the flags are complete, and the results of flagged slots written
+    recompute_bad<bf16_t, QT, KT>(a, w, tables, bad, wave);
+}
+
+// float32: 16 query slots in every wave, 32-key tiles of its own per wave, staged through registers
+// into padded rows, products on the float32 matrix instructions; joined at the end.
+template <int HD>
+struct TilesF32 {
+    static constexpr int KT = 32;
+    static constexpr int CR = HD / 4;                   // 16-byte chunks per row
+    static constexpr int NCH = 2 * KT * CR / kWave;     // chunks per lane
+    static_assert(2 * KT * CR % kWave == 0, "whole chunks");
+    // words per row: 4 P = 16 or 48 mod 64 keeps the four rows that a transposed V read takes in different banks
+    static constexpr int P = HD + 4;
+    static constexpr int WORDS = 2 * KT * P + 16;       // reads of a last block of eight columns go past the last row
+    __amdgpu_buffer_rsrc_t rsrc;
+    uint32_t row_bytes, col0;
+    int lane, end;
+    vec16 raw[NCH];
+    __device__ __forceinline__ void init(const void* kv, int rows, int heads, int kvh, int lane_) {
+        lane = lane_;
+        row_bytes = 8u * heads * HD;
+        col0 = kvh * HD * 4;
+        rsrc = make_rsrc(kv, (uint32_t)rows * row_bytes);
+        end = rows;
+    }
+    // rows past the last read as zeros
+    __device__ __forceinline__ void issue(int k0) {
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            const int c = i * kWave + lane, r = c / CR, key = k0 + r % KT;
+            const uint32_t o = key < end ? (uint32_t)key * row_bytes + (r >= KT ? row_bytes / 2 : 0u) + col0 + (c % CR) * 16 : 0xfff00000u;
+            raw[i] = buf_ld16(rsrc, o, 0);
+        }
+    }
+    __device__ __forceinline__ void store(float* smem) {
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            const int c = i * kWave + lane;
+            st16(smem + (c / CR) * P + (c % CR) * 4, raw[i]);
+        }
+    }
+};
+
+template <int HD>
+__global__ __launch_bounds__(kThreads, 2) void shared_f32_kernel(SharedAttnDesc a, int qtiles) {
+    using S = TilesF32<HD>;
+    constexpr int KT = S::KT, P = S::P, NJ = (HD + 15) / 16;
+    constexpr int OLD = NJ * 16 + 4;
+    constexpr int JOIN = 4 * 16 * OLD + 4 * 16 * 2;     // words of the waves' sums
+    __shared__ __attribute__((aligned(16))) float smem[4 * S::WORDS > JOIN ? 4 * S::WORDS : JOIN];
+    __shared__ Tables tables;
+    __shared__ uint32_t bad[1];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), grp = lane / 16, l16 = lane % 16;
+    const int i = blockIdx.x / kXcds, pair = i / a.heads * kXcds + blockIdx.x % kXcds;
+    Work w;
+    if (pair >= qtiles * a.nsplit) return;
+    if (!find_work<16, KT>(a, pair / a.nsplit, i % a.heads, pair % a.nsplit, tables, w)) return;
+    if (tid == 0) bad[0] = 0;
+    float* const sw = smem + wave * S::WORDS;
+    if (lane < 16) sw[2 * KT * P + lane] = 0.f;
+
+    // Q^T operand: slot l16, head_dim 16 j + 4 grp + e for the instruction (j, e)
+    float qf[NJ][4];
+    const int slot = w.q0 + l16;
+    Sight<KT> sight;
+    sight.init(a, tables, w, slot);
+    const float* const q = static_cast<const float*>(a.q) + slot_row(a, w, slot) * HD;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (slot < w.slots && j * 16 + grp * 4 < HD) load4<float>(q + j * 16 + grp * 4, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) qf[j][e] = v[e];
+    }
+    f32x4_t oacc[NJ];
+#pragma unroll
+    for (int h = 0; h < NJ; ++h) oacc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, l_run = 0.f;
+
+    auto multiply = [&](uint64_t sees) __attribute__((always_inline)) {
+        // S^T: keys 16 ks + 4 grp + r of slot l16, in the log2 domain
+        float sc[2][4];
+        float mx = -INFINITY;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                float k[4] = {0.f, 0.f, 0.f, 0.f};
+                if (HD % 16 == 0 || j + 1 < NJ || j * 16 + grp * 4 < HD) load4<float>(sw + (ks * 16 + l16) * P + j * 16 + grp * 4, k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc = Elt<float>::mma(k[e], qf[j][e], acc);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool there = (sees >> (ks * 16 + grp * 4 + r)) & 1;
+                sc[ks][r] = there ? acc[r] * a.scale_log2 : -INFINITY;
+                mx = fmaxf(mx, sc[ks][r]);
+            }
+        }
+        const float m_new = fmaxf(m_run, rows_max(mx));
+        const float ref = m_new == -INFINITY ? 0.f : m_new;
+        const float corr = m_run == -INFINITY ? 0.f : fast_exp2(m_run - ref);
+        m_run = m_new;
+        l_run *= corr;
+#pragma unroll
+        for (int h = 0; h < NJ; ++h) oacc[h] *= corr;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                sc[ks][r] = fast_exp2(sc[ks][r] - ref);
+                l_run += sc[ks][r];
+            }
+        // O^T += V^T P^T; a last block of eight columns multiplies what lies behind the row too, into rows that are not used
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int h = 0; h < NJ; ++h)
+                    oacc[h] = Elt<float>::mma(sw[(KT + ks * 16 + grp * 4 + r) * P + h * 16 + l16], sc[ks][r], oacc[h]);
+    };
+    auto run = [&](auto OWN, const void* kv, int base, int rows, int from, int to, int skip) __attribute__((always_inline)) {
+        from += (wave - skip) & 3;   // the waves go on in turn from one kind to the next
+        if (from >= to) return;
+        S st;
+        st.init(kv, rows, a.heads, w.kvh, lane);
+        uint64_t hidden = OWN ? 0ull : sight.fetch(a, from);
+        st.issue(base + from * KT);
+        for (int t = from; t < to; t += 4) {
+            const uint64_t sees = OWN ? sight.own(base + t * KT) : sight.prefix(a, hidden, t);
+            asm volatile("" ::: "memory");      // LDS operations of a wave are done in order
+            st.store(sw);
+            asm volatile("" ::: "memory");
+            if (t + 4 < to) {
+                if constexpr (!OWN) hidden = sight.fetch(a, t + 4);
+                st.issue(base + (t + 4) * KT);
+            }
+            multiply(sees);
+        }
+    };
+    const int c0 = min(w.t0, w.ntp), c1 = min(w.t1, w.ntp);
+    run(std::false_type{}, a.kv, 0, a.T, c0, c1, 0);
+    if (w.f1 > w.f0) run(std::true_type{}, a.fresh, w.f0, w.f1, max(w.t0 - w.ntp, 0), max(w.t1 - w.ntp, 0), c1 - c0);
+
+    const float l = rows_sum(l_run);
+    __syncthreads();
+    float* const so = smem;
+    float2* const sml = reinterpret_cast<float2*>(so + 4 * 16 * OLD);
+#pragma unroll
+    for (int h = 0; h < NJ; ++h) {
+        const float v[4] = {oacc[h][0], oacc[h][1], oacc[h][2], oacc[h][3]};
+        store4<float>(so + (wave * 16 + l16) * OLD + h * 16 + grp * 4, v);
+    }
+    if (grp == 0) sml[wave * 16 + l16] = make_float2(m_run, l);
+    __syncthreads();
+    join_waves<float, HD, OLD>(a, w, so, sml, tid, 0, bad);
+    __syncthreads();    // the flags are complete, and the results of flagged slots written
+    recompute_bad<float, 16, KT>(a, w, tables, bad, wave);
+}
+
+// Join of the key ranges: range s has the weight l_s 2^(m_s - m); rows of no
+// request are left alone, rows of no key get 0. One wave per (row, head): lane s
+// holds range s's maximum and sum, then hd / 4 lanes take four columns each and as
+// many groups of them as the wave holds take the ranges in turn.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedAttnDesc a) {
+    const int HG = a.heads * a.group, hd = a.hd, lane = threadIdx.x % kWave;
+    const int lo = a.seg_start ? min(max(a.seg_start[0], 0), a.M) : 0;
+    const int hi = a.seg_start ? min(max(a.seg_start[a.batch], 0), a.M) : a.M;
+    const long plane = (long)a.M * HG;
+    const long sr = (long)lo * HG + (long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;   // (row, head)
+    if (sr >= (long)hi * HG) return;
+    const int CL = hd / 4, groups = kWave / CL, grp = lane / CL, col = lane % CL;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < a.nsplit) ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (lane * plane + sr));
+    float m = wave_max(ml.x);
+    if (__any(ml.x != ml.x)) m = __uint_as_float(0x7fc00000u);      // maxima drop NaN
+    const float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m) * ml.y;
+    const float L = wave_sum(f);
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    const float* const po = a.part_o + sr * hd + col * 4;
+    for (int s0 = 0; s0 < a.nsplit; s0 += groups) {
+        const int s = s0 + grp;
+        const float fs = __shfl(f, s, kWave);
+        if (grp < groups && s < a.nsplit) {
+            const float4 p = *reinterpret_cast<const float4*>(po + s * plane * hd);
+            acc[0] += fs * p.x; acc[1] += fs * p.y; acc[2] += fs * p.z; acc[3] += fs * p.w;
+        }
+    }
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < groups; ++g)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] += __shfl(acc[r], (g * CL + col) % kWave, kWave);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] *= inv;
+    if (lane < CL) store4<T>(static_cast<T*>(a.o) + sr * hd + col * 4, o);
+}
+
+// One wave per word of 64 tokens.
+__global__ __launch_bounds__(kThreads) void shared_bits_kernel(const uint8_t* __restrict__ mask, int batch, int T, int words, uint64_t* __restrict__ bits) {
+    const int lane = threadIdx.x % kWave;
+    const long i = (long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
+    if (i >= (long)batch * words) return;
+    const int b = (int)(i / words), t = (int)(i - (long)b * words) * 64 + lane;
+    const uint64_t v = __ballot(t >= T || mask[(long)b * T + t] != 0);
+    if (lane == 0) bits[i] = v;
+}
+
+int slot_tiles(const SharedAttnDesc& a, int tile) { return (int)(((long)a.M * a.group + tile - 1) / tile); }
+
+template <int QT>
+void launch_bf16(const SharedAttnDesc& a, hipStream_t s) {
+    const int qtiles = slot_tiles(a, QT);
+    const int pairs = qtiles * a.nsplit;
+    const dim3 grid((unsigned)(QT == 128 ? pairs : (pairs + kXcds - 1) / kXcds * kXcds) * a.heads), block(kThreads);
+    switch (a.hd) {
+#define MS_HD(n) case n: hipLaunchKernelGGL((shared_bf16_kernel<n, QT>), grid, block, 0, s, a, qtiles); break;
+        MS_HD(8) MS_HD(16) MS_HD(24) MS_HD(32) MS_HD(40) MS_HD(48) MS_HD(56) MS_HD(64)
+        MS_HD(72) MS_HD(80) MS_HD(88) MS_HD(96) MS_HD(104) MS_HD(112) MS_HD(120) MS_HD(128)
+#undef MS_HD
+    }
+}
+
+void launch_f32(const SharedAttnDesc& a, hipStream_t s) {
+    const int qtiles = slot_tiles(a, 16);
+    const int pairs = qtiles * a.nsplit;
+    const dim3 grid((unsigned)(pairs + kXcds - 1) / kXcds * kXcds * a.heads), block(kThreads);
+    switch (a.hd) {
+#define MS_HD(n) case n: hipLaunchKernelGGL(shared_f32_kernel<n>, grid, block, 0, s, a, qtiles); break;
+        MS_HD(8) MS_HD(16) MS_HD(24) MS_HD(32) MS_HD(40) MS_HD(48) MS_HD(56) MS_HD(64)
+#undef MS_HD
+    }
+}
+
+// Whether a split into n ranges stays below the 2^32 threads that end a launch.
+bool ranges_fit(const SharedAttnDesc& a, int tile, int n) {
+    constexpr long most = (1l << 32) / kThreads;
+    return ((long)slot_tiles(a, tile) * n + kXcds) * a.heads < most &&
+           (long)a.M * a.heads * a.group / (kThreads / kWave) + 1 < most;
+}
+
+}  // namespace
+
+void plan_shared_attention(int dtype, SharedAttnDesc& a) {
+    a.tile = 16;
+    a.nsplit = 1;
+    if (a.M == 0) return;
+    const long slots = (long)a.M * a.group;
+    if (dtype == kBF16) a.tile = slots <= 16 ? 16 : slots <= 32 ? 32 : 128;
+    const long base = (long)slot_tiles(a, a.tile) * a.heads;
+    const long steps = (a.T + 127) / 128;
+    int n = 1;
+    while (n < kSharedMaxRanges && base * n * 2 <= 512 && n * 2 <= steps && ranges_fit(a, a.tile, n * 2)) n *= 2;
+    a.nsplit = n;
+}
+
+hipError_t launch_shared_bits(const uint8_t* mask, int batch, int T, uint64_t* bits, hipStream_t s) {
+    const int words = (T + 63) / 64;
+    const long n = (long)batch * words;
+    const dim3 grid((unsigned)((n + kThreads / kWave - 1) / (kThreads / kWave))), block(kThreads);
+    hipLaunchKernelGGL(shared_bits_kernel, grid, block, 0, s, mask, batch, T, words, bits);
+    return hipGetLastError();
+}
+
+hipError_t launch_shared_attention(int dtype, const SharedAttnDesc& a, hipStream_t s) {
+    if (a.M == 0) return hipSuccess;
+    if (dtype == kBF16) {
+        if (a.tile == 16) launch_bf16<16>(a, s);
+        else if (a.tile == 32) launch_bf16<32>(a, s);
+        else launch_bf16<128>(a, s);
+    } else {
+        launch_f32(a, s);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_shared_join(int dtype, const SharedAttnDesc& a, hipStream_t s) {
+    if (a.M == 0 || a.nsplit == 1) return hipSuccess;
+    const long n = (long)a.M * a.heads * a.group;
+    const dim3 grid((unsigned)((n + kThreads / kWave - 1) / (kThreads / kWave))), block(kThreads);
+    if (dtype == kBF16) hipLaunchKernelGGL(shared_join_kernel<bf16_t>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(shared_join_kernel<float>, grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace ms

@@ -71,6 +71,24 @@ class Kv8Attn(C.Structure):
                 ("fresh_start", C.c_void_p), ("scale", C.c_float)]
 
 
+class QkNormRopeArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("qkv", C.c_void_p), ("ld", C.c_int64), ("q_gain", C.c_void_p),
+                ("k_gain", C.c_void_p), ("eps", C.c_float), ("table", C.c_void_p), ("n_pos", C.c_int32), ("rot", C.c_int32),
+                ("pairing", C.c_int32), ("pos", C.c_void_p), ("q", C.c_void_p), ("kv", C.c_void_p), ("kv_rows", C.c_int64),
+                ("dst_rows", C.c_void_p)]
+
+
+MS_ROPE_PAIRS, MS_ROPE_HALVES = 0, 1
+
+
+class SharedAttn(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("rows", C.c_int32), ("n_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("kv", C.c_void_p), ("tokens", C.c_int32),
+                ("batch", C.c_int32), ("bits", C.c_void_p), ("seg_start", C.c_void_p), ("fresh", C.c_void_p),
+                ("fresh_rows", C.c_int64), ("fresh_start", C.c_void_p), ("scale", C.c_float)]
+
+
 class CostModel(C.Structure):
     """ms_cost_model: per-block Comp(F) = comp_ms0 + comp_ms_per_gflop * F / 1e9 and
     Load(B) = load_ms0 + load_ms_per_mb * B / 1e6 (Sec. 4.3)."""
@@ -124,6 +142,14 @@ def load() -> C.CDLL:
                                              C.POINTER(C.c_double)]),
             "mask_profiler_start": (i32, [C.c_uint32, i32]),
             "ms_linear": (i32, [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]),
+            "ms_mx4_quantize": (i32, [i32, vp, C.c_int64, i32, C.c_int64, vp, vp, vp]),
+            "ms_mx4_dequantize": (i32, [i32, vp, vp, C.c_int64, i32, vp, C.c_int64, vp]),
+            "ms_mx4_linear_workspace_bytes": (sz, [i32, i32, i32]),
+            "ms_mx4_linear": (i32, [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]),
+            "ms_qk_norm_rope": (i32, [C.POINTER(QkNormRopeArgs), vp]),
+            "ms_shared_bits": (i32, [vp, i32, i32, vp, vp]),
+            "ms_shared_attention_workspace_bytes": (sz, [i32, C.POINTER(SharedAttn)]),
+            "ms_shared_attention": (i32, [i32, C.POINTER(SharedAttn), vp, sz, vp]),
             "ms_kv8_keys": (i32, [vp, i32, i32, vp, i32, vp, vp]),
             "ms_kv8_quantize": (i32, [C.POINTER(Kv8Cache), vp, C.c_int64, C.c_int64, vp, vp]),
             "ms_kv8_dequantize": (i32, [C.POINTER(Kv8Cache), C.POINTER(Kv8Select), vp, C.c_int64, vp]),
@@ -369,6 +395,202 @@ def ms_kv8_attention(q, codes, scales, out, seg_start, *, block, seg_req=None, c
             raise _kv8_bad("workspace must be a contiguous tensor on q's device")
         wp, wb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _kv8_run(load().ms_kv8_attention, q, stream, C.byref(c), C.byref(sel), C.byref(a), wp, wb)
+
+
+def _bad(what):
+    return MaskStepError(MS_EINVAL, what)
+
+
+def _rows_dtype(x, what):
+    dt = _KV8_DTYPES.get(x.dtype)
+    if dt is None:
+        raise _bad(f"{what} must be bfloat16 or float32, not {x.dtype}")
+    if not x.is_cuda:
+        raise _bad(f"{what} must be on a GPU")
+    return dt
+
+
+def _like(t, shape, dtype, dev, name):
+    """Address of a contiguous tensor of that shape, type and device."""
+    if t.shape != shape or t.dtype != dtype or t.device != dev or not t.is_contiguous():
+        raise _bad(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _apart(out, ins, what):
+    """Refuses an output that shares memory with an input: (address, bytes) of each."""
+    o, n = out
+    for p, k in ins:
+        if p and o and p < o + n and o < p + k:
+            raise _bad(f"{what} must not overlap an input")
+
+
+def _span(t):
+    """(address, bytes) from a tensor's first to its last element."""
+    if t is None or t.numel() == 0:
+        return 0, 0
+    return t.data_ptr(), (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * t.element_size()
+
+
+def _mx4_codes(codes, scales, dev, name):
+    """(rows, columns) of codes [rows][cols / 2] with scales [rows][cols / 32]."""
+    if codes.dim() != 2 or codes.element_size() != 1 or not codes.is_contiguous() or codes.device != dev:
+        raise _bad(f"{name} codes must be contiguous bytes [rows][cols / 2] on {dev}, not {codes.dtype} {tuple(codes.shape)} "
+                   f"on {codes.device}")
+    rows, cols = codes.shape[0], 2 * codes.shape[1]
+    if scales.shape != (rows, cols // 32) or cols % 32 or scales.element_size() != 1 or not scales.is_contiguous() or scales.device != dev:
+        raise _bad(f"{name} scales must be contiguous bytes [rows][cols / 32] on {dev} with cols a multiple of 32, not "
+                   f"{scales.dtype} {tuple(scales.shape)} (codes {tuple(codes.shape)}) on {scales.device}")
+    return rows, cols
+
+
+def _mx4_rows(x, codes, scales):
+    """(dtype, rows, cols, row stride) of x [rows][cols] with its codes; rows may lie apart, columns not."""
+    dt = _rows_dtype(x, "x")
+    rows, cols = _mx4_codes(codes, scales, x.device, "the")
+    if x.shape != (rows, cols) or (cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < cols):
+        raise _bad(f"x must be [{rows}][{cols}] with neighbouring columns, not {tuple(x.shape)} strided {x.stride()}")
+    return dt, rows, cols, x.stride(0) if rows > 1 else cols
+
+
+def ms_mx4_quantize(x, codes, scales, *, stream=None):
+    """Rows x [rows][cols] into microscaled 4-bit codes [rows][cols / 2] and scale bytes [rows][cols / 32]. The rows of x
+    may lie apart (whole 16 bytes)."""
+    dt, rows, cols, ld = _mx4_rows(x, codes, scales)
+    for t in (codes, scales):
+        _apart(_span(t), [_span(x), _span(scales if t is codes else codes)], "codes or scales")
+    _kv8_run(load().ms_mx4_quantize, x, stream, dt, x.data_ptr(), rows, cols, ld, codes.data_ptr(), scales.data_ptr())
+
+
+def ms_mx4_dequantize(codes, scales, x, *, stream=None):
+    """The values of such codes into x [rows][cols], whose rows may lie apart."""
+    dt, rows, cols, ld = _mx4_rows(x, codes, scales)
+    _apart(_span(x), [_span(codes), _span(scales)], "x")
+    _kv8_run(load().ms_mx4_dequantize, x, stream, dt, codes.data_ptr(), scales.data_ptr(), rows, cols, x.data_ptr(), ld)
+
+
+def ms_mx4_linear_workspace_bytes(a_codes, w_codes) -> int:
+    """Bytes of workspace with which ms_mx4_linear may split the columns as it sees fit, for codes of these shapes."""
+    n = load().ms_mx4_linear_workspace_bytes(a_codes.shape[0], w_codes.shape[0], 2 * w_codes.shape[1])
+    if n == 0 and load().mask_last_error():
+        raise _bad(load().mask_last_error().decode())
+    return n
+
+
+def _workspace(workspace, dev):
+    if workspace is None:
+        return 0, 0
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise _bad("workspace must be a contiguous tensor on the operands' device")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def ms_mx4_linear(a_codes, a_scales, w_codes, w_scales, bias, out, *, resid=None, gelu=False, workspace=None, stream=None):
+    """out[M][N] = A W^T + bias, with ``gelu`` its GELU, or with ``resid`` [M][N] (which may be out) plus that; A [M][K] and
+    W [N][K] as ms_mx4_quantize writes them."""
+    dev = out.device
+    dt = _rows_dtype(out, "out")
+    M, K = _mx4_codes(a_codes, a_scales, dev, "A's")
+    N, kw = _mx4_codes(w_codes, w_scales, dev, "W's")
+    if kw != K:
+        raise _bad(f"A has {K} columns, W {kw}")
+    if gelu and resid is not None:
+        raise _bad("gelu and resid exclude each other")
+    op = _like(out, (M, N), out.dtype, dev, "out")
+    bp = _like(bias, (N,), out.dtype, dev, "bias")
+    rp = None if resid is None else _like(resid, (M, N), out.dtype, dev, "resid")
+    wp, wb = _workspace(workspace, dev)
+    ins = [_span(t) for t in (a_codes, a_scales, w_codes, w_scales, bias)]
+    _apart(_span(out), ins + ([] if rp == op else [_span(resid)]), "out")
+    _apart((wp, wb), ins + [_span(resid), _span(out)], "workspace")
+    _kv8_run(load().ms_mx4_linear, out, stream, dt, M, N, K, a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(),
+             w_scales.data_ptr(), bp, rp, op, 2 if gelu else 0 if rp is None else 1, wp, wb)
+
+
+def ms_qk_norm_rope(qkv, q, kv, *, q_gain=None, k_gain=None, eps=1e-6, table=None, pos=None, halves=False, rows=None, stream=None):
+    """Per-head norms, rotation and K/V scatter of a projection's packed rows qkv [rows][(heads + 2 kv_heads) head_dim]
+    (rows may lie apart): Q to q [rows][heads][head_dim], K and V to the rows ``rows`` (int32 [rows], None: in order) of kv
+    [kv_rows][2][kv_heads][head_dim]. Gains [head_dim], None: not normalised; ``table`` float32 [positions][rot / 2][2]
+    (cos, sin) with ``pos`` int32 [rows] (None: in order), None: not rotated; ``halves``: pairs (i, i + rot / 2)."""
+    dt, dev = _rows_dtype(qkv, "qkv"), qkv.device
+    if q.dim() != 3 or kv.dim() != 4 or kv.shape[1] != 2 or kv.shape[3] != q.shape[2]:
+        raise _bad(f"q must be [rows][heads][head_dim] and kv [kv_rows][2][kv_heads][head_dim], not {tuple(q.shape)} and {tuple(kv.shape)}")
+    M, H, hd = q.shape
+    G = kv.shape[2]
+    cols = (H + 2 * G) * hd
+    if qkv.shape != (M, cols) or (cols > 1 and qkv.stride(1) != 1) or (M > 1 and qkv.stride(0) < cols):
+        raise _bad(f"qkv must be [{M}][{cols}] with neighbouring columns, not {tuple(qkv.shape)} strided {qkv.stride()}")
+    qp, kp = _like(q, q.shape, qkv.dtype, dev, "q"), _like(kv, kv.shape, qkv.dtype, dev, "kv")
+    gains = [None if g is None else _like(g, (hd,), qkv.dtype, dev, "a gain") for g in (q_gain, k_gain)]
+    tp, n_pos, rot = None, 0, 0
+    if table is not None:
+        if table.dim() != 3 or table.shape[2] != 2:
+            raise _bad(f"table must be [positions][rot / 2][2], not {tuple(table.shape)}")
+        n_pos, rot = table.shape[0], 2 * table.shape[1]
+        tp = _like(table, table.shape, torch.float32, dev, "table") or _KV8_NO_ENTRIES
+    ins = [_span(t) for t in (qkv, q_gain, k_gain, table, pos, rows)]
+    _apart(_span(q), ins + [_span(kv)], "q")
+    _apart(_span(kv), ins, "kv")
+    a = QkNormRopeArgs(dt, M, H, G, hd, qkv.data_ptr(), qkv.stride(0) if M > 1 else cols, gains[0], gains[1], eps, tp, n_pos, rot,
+                       MS_ROPE_HALVES if halves else MS_ROPE_PAIRS, _kv8_table(pos, dev, (M,), "pos"), qp, kp, kv.shape[0],
+                       _kv8_table(rows, dev, (M,), "rows"))
+    _kv8_run(load().ms_qk_norm_rope, qkv, stream, C.byref(a))
+
+
+def ms_shared_bits(mask, bits, *, stream=None):
+    """Hidden tokens as bits: mask uint8 or bool [batch][tokens] -> bits int64 [batch][ceil(tokens / 64)]."""
+    if not mask.is_cuda or mask.dim() != 2 or mask.element_size() != 1 or not mask.is_contiguous():
+        raise _bad("mask must be contiguous bytes [batch][tokens] on a GPU")
+    B, T = mask.shape
+    bp = _like(bits, (B, -(-T // 64)), torch.int64, mask.device, "bits")
+    _apart(_span(bits), [_span(mask)], "bits")
+    _kv8_run(load().ms_shared_bits, mask, stream, mask.data_ptr(), B, T, bp)
+
+
+def ms_shared_attention_workspace_bytes(q, kv, *, fresh=None) -> int:
+    """Bytes of workspace with which ms_shared_attention may split the keys as it sees fit, for tensors of these shapes."""
+    some = _KV8_NO_ENTRIES   # addresses are checked but not read
+    n_own = 0 if fresh is None else fresh.shape[0]
+    a = SharedAttn(some, some, q.shape[0], q.shape[1], kv.shape[2], q.shape[2], some, kv.shape[0], 1, None, some,
+                   some if n_own else None, n_own, some, 0.0)
+    n = load().ms_shared_attention_workspace_bytes(_KV8_DTYPES.get(q.dtype, -1), C.byref(a))
+    if n == 0 and load().mask_last_error():
+        raise _bad(load().mask_last_error().decode())
+    return n
+
+
+def ms_shared_attention(q, kv, out, *, seg_start=None, bits=None, fresh=None, fresh_start=None, scale=None, workspace=None,
+                        stream=None):
+    """out[rows][heads][head_dim] = attention of the packed query rows q of a batch over one shared prefix kv
+    [tokens][2][kv_heads][head_dim], less the tokens that the row's request hides (``bits`` int64 [batch][ceil(tokens / 64)],
+    from ms_shared_bits), and over the request's own rows of ``fresh`` [rows][2][kv_heads][head_dim] (fresh_start int32
+    [batch + 1]). ``seg_start`` int32 [batch + 1]: packed rows of each request, None: one request. ``scale``: of the scores,
+    None: 1 / sqrt(head_dim); one that float32 holds as 0 is refused, since 0 stands for None in the library."""
+    if scale is not None and C.c_float(scale).value == 0.0:
+        raise _bad(f"scale {scale!r} is 0 in float32; None stands for 1 / sqrt(head_dim)")
+    dt, dev = _rows_dtype(q, "q"), q.device
+    if q.dim() != 3 or kv.dim() != 4 or kv.shape[1] != 2 or kv.shape[3] != q.shape[2]:
+        raise _bad(f"q must be [rows][heads][head_dim] and kv [tokens][2][kv_heads][head_dim], not {tuple(q.shape)} and {tuple(kv.shape)}")
+    M, H, hd = q.shape
+    T, G = kv.shape[0], kv.shape[2]
+    qp, kp = _like(q, q.shape, q.dtype, dev, "q"), _like(kv, kv.shape, q.dtype, dev, "kv")
+    op = _like(out, q.shape, q.dtype, dev, "out")
+    B = 1 if seg_start is None else seg_start.numel() - 1
+    sp = _kv8_table(seg_start, dev, (B + 1,), "seg_start")
+    bp = None if bits is None else _like(bits, (B, -(-T // 64)), torch.int64, dev, "bits")
+    fp, f_rows, fs = None, 0, None
+    if fresh is not None:
+        f_rows = fresh.shape[0]
+        fp = _like(fresh, (f_rows, 2, G, hd), q.dtype, dev, "fresh") or None
+        if fresh_start is None:
+            raise _bad("own rows need fresh_start")
+        fs = _kv8_table(fresh_start, dev, (B + 1,), "fresh_start")
+    wp, wb = _workspace(workspace, dev)
+    ins = [_span(t) for t in (kv, bits, seg_start, fresh, fresh_start)]
+    _apart((op, out.numel() * out.element_size()), ins + ([] if qp == op else [_span(q)]), "out")
+    _apart((wp, wb), ins + [_span(q), _span(out)], "workspace")
+    a = SharedAttn(qp, op, M, H, G, hd, kp, T, B, bp, sp, fp, f_rows, fs, 0.0 if scale is None else scale)
+    _kv8_run(load().ms_shared_attention, q, stream, dt, C.byref(a), wp, wb)
 
 
 KERNEL_CLASSES = ("compact", "gather", "layernorm", "gemm_qkv", "attention", "gemm_out", "gemm_up",
