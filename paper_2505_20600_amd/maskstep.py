@@ -397,75 +397,76 @@ def ms_kv8_attention(q, codes, scales, out, seg_start, *, block, seg_req=None, c
     _kv8_run(load().ms_kv8_attention, q, stream, C.byref(c), C.byref(sel), C.byref(a), wp, wb)
 
 
+# The checks below look at each tensor once and in few steps: small calls take the GPU less than ten microseconds.
+
 def _bad(what):
     return MaskStepError(MS_EINVAL, what)
 
 
-def _rows_dtype(x, what):
-    dt = _KV8_DTYPES.get(x.dtype)
+def _on(x, what):
+    """(ms_dtype, device number) of a tensor of rows."""
+    dt, dev = _KV8_DTYPES.get(x.dtype), x.get_device()
     if dt is None:
         raise _bad(f"{what} must be bfloat16 or float32, not {x.dtype}")
-    if not x.is_cuda:
+    if dev < 0:
         raise _bad(f"{what} must be on a GPU")
-    return dt
+    return dt, dev
 
 
 def _like(t, shape, dtype, dev, name):
     """Address of a contiguous tensor of that shape, type and device."""
-    if t.shape != shape or t.dtype != dtype or t.device != dev or not t.is_contiguous():
-        raise _bad(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise _bad(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on GPU {dev}, not {t.dtype} {tuple(t.shape)} "
+                   f"strided {t.stride()} on {t.device}")
     return t.data_ptr()
 
 
-def _apart(out, ins, what):
-    """Refuses an output that shares memory with an input: (address, bytes) of each."""
-    o, n = out
-    for p, k in ins:
-        if p and o and p < o + n and o < p + k:
-            raise _bad(f"{what} must not overlap an input")
+def _ints(t, n, dev, name):
+    """Address of a table of n int32, None where there is none (a table without entries has one too)."""
+    return None if t is None else _like(t, (n,), torch.int32, dev, name) or _KV8_NO_ENTRIES
 
 
-def _span(t):
-    """(address, bytes) from a tensor's first to its last element."""
-    if t is None or t.numel() == 0:
-        return 0, 0
-    return t.data_ptr(), (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * t.element_size()
-
-
-def _mx4_codes(codes, scales, dev, name):
+def _codes(codes, scales, dev, name):
     """(rows, columns) of codes [rows][cols / 2] with scales [rows][cols / 32]."""
-    if codes.dim() != 2 or codes.element_size() != 1 or not codes.is_contiguous() or codes.device != dev:
-        raise _bad(f"{name} codes must be contiguous bytes [rows][cols / 2] on {dev}, not {codes.dtype} {tuple(codes.shape)} "
-                   f"on {codes.device}")
-    rows, cols = codes.shape[0], 2 * codes.shape[1]
-    if scales.shape != (rows, cols // 32) or cols % 32 or scales.element_size() != 1 or not scales.is_contiguous() or scales.device != dev:
-        raise _bad(f"{name} scales must be contiguous bytes [rows][cols / 32] on {dev} with cols a multiple of 32, not "
-                   f"{scales.dtype} {tuple(scales.shape)} (codes {tuple(codes.shape)}) on {scales.device}")
-    return rows, cols
+    shape = codes.shape
+    if len(shape) != 2 or codes.dtype is not torch.uint8 or codes.get_device() != dev or not codes.is_contiguous():
+        raise _bad(f"{name} codes must be contiguous uint8 [rows][cols / 2] on GPU {dev}, not {codes.dtype} {tuple(shape)} "
+                   f"strided {codes.stride()} on {codes.device}")
+    rows, half = shape
+    if half % 16 or scales.shape != (rows, half // 16) or scales.dtype is not torch.uint8 or scales.get_device() != dev or not scales.is_contiguous():
+        raise _bad(f"{name} scales must be contiguous uint8 [rows][cols / 32] on GPU {dev} with cols a multiple of 32, not "
+                   f"{scales.dtype} {tuple(scales.shape)} (codes {tuple(shape)}) on {scales.device}")
+    return rows, 2 * half
 
 
-def _mx4_rows(x, codes, scales):
-    """(dtype, rows, cols, row stride) of x [rows][cols] with its codes; rows may lie apart, columns not."""
-    dt = _rows_dtype(x, "x")
-    rows, cols = _mx4_codes(codes, scales, x.device, "the")
-    if x.shape != (rows, cols) or (cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < cols):
-        raise _bad(f"x must be [{rows}][{cols}] with neighbouring columns, not {tuple(x.shape)} strided {x.stride()}")
-    return dt, rows, cols, x.stride(0) if rows > 1 else cols
+def _apart_rows(x, rows, cols, name):
+    """Elements between the rows of x [rows][cols], which may lie apart, its columns not."""
+    if x.shape != (rows, cols):
+        raise _bad(f"{name} must be [{rows}][{cols}], not {tuple(x.shape)}")
+    if rows < 2 or x.is_contiguous():
+        if cols > 1 and x.stride(1) != 1:
+            raise _bad(f"{name} must have neighbouring columns, not be strided {x.stride()}")
+        return cols
+    ld, one = x.stride()
+    if one != 1 and cols > 1 or ld < cols:
+        raise _bad(f"{name} must have neighbouring columns and rows that do not overlap, not be strided {x.stride()}")
+    return ld
 
 
 def ms_mx4_quantize(x, codes, scales, *, stream=None):
     """Rows x [rows][cols] into microscaled 4-bit codes [rows][cols / 2] and scale bytes [rows][cols / 32]. The rows of x
     may lie apart (whole 16 bytes)."""
-    dt, rows, cols, ld = _mx4_rows(x, codes, scales)
-    for t in (codes, scales):
-        _apart(_span(t), [_span(x), _span(scales if t is codes else codes)], "codes or scales")
+    dt, dev = _on(x, "x")
+    rows, cols = _codes(codes, scales, dev, "the")
+    ld = _apart_rows(x, rows, cols, "x")
     _kv8_run(load().ms_mx4_quantize, x, stream, dt, x.data_ptr(), rows, cols, ld, codes.data_ptr(), scales.data_ptr())
 
 
 def ms_mx4_dequantize(codes, scales, x, *, stream=None):
     """The values of such codes into x [rows][cols], whose rows may lie apart."""
-    dt, rows, cols, ld = _mx4_rows(x, codes, scales)
-    _apart(_span(x), [_span(codes), _span(scales)], "x")
+    dt, dev = _on(x, "x")
+    rows, cols = _codes(codes, scales, dev, "the")
+    ld = _apart_rows(x, rows, cols, "x")
     _kv8_run(load().ms_mx4_dequantize, x, stream, dt, codes.data_ptr(), scales.data_ptr(), rows, cols, x.data_ptr(), ld)
 
 
@@ -480,29 +481,25 @@ def ms_mx4_linear_workspace_bytes(a_codes, w_codes) -> int:
 def _workspace(workspace, dev):
     if workspace is None:
         return 0, 0
-    if workspace.device != dev or not workspace.is_contiguous():
+    if workspace.get_device() != dev or not workspace.is_contiguous():
         raise _bad("workspace must be a contiguous tensor on the operands' device")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def ms_mx4_linear(a_codes, a_scales, w_codes, w_scales, bias, out, *, resid=None, gelu=False, workspace=None, stream=None):
     """out[M][N] = A W^T + bias, with ``gelu`` its GELU, or with ``resid`` [M][N] (which may be out) plus that; A [M][K] and
     W [N][K] as ms_mx4_quantize writes them."""
-    dev = out.device
-    dt = _rows_dtype(out, "out")
-    M, K = _mx4_codes(a_codes, a_scales, dev, "A's")
-    N, kw = _mx4_codes(w_codes, w_scales, dev, "W's")
+    dt, dev = _on(out, "out")
+    M, K = _codes(a_codes, a_scales, dev, "A's")
+    N, kw = _codes(w_codes, w_scales, dev, "W's")
     if kw != K:
         raise _bad(f"A has {K} columns, W {kw}")
     if gelu and resid is not None:
         raise _bad("gelu and resid exclude each other")
-    op = _like(out, (M, N), out.dtype, dev, "out")
-    bp = _like(bias, (N,), out.dtype, dev, "bias")
-    rp = None if resid is None else _like(resid, (M, N), out.dtype, dev, "resid")
+    t = out.dtype
+    op, bp = _like(out, (M, N), t, dev, "out"), _like(bias, (N,), t, dev, "bias")
+    rp = None if resid is None else _like(resid, (M, N), t, dev, "resid")
     wp, wb = _workspace(workspace, dev)
-    ins = [_span(t) for t in (a_codes, a_scales, w_codes, w_scales, bias)]
-    _apart(_span(out), ins + ([] if rp == op else [_span(resid)]), "out")
-    _apart((wp, wb), ins + [_span(resid), _span(out)], "workspace")
     _kv8_run(load().ms_mx4_linear, out, stream, dt, M, N, K, a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(),
              w_scales.data_ptr(), bp, rp, op, 2 if gelu else 0 if rp is None else 1, wp, wb)
 
@@ -512,28 +509,24 @@ def ms_qk_norm_rope(qkv, q, kv, *, q_gain=None, k_gain=None, eps=1e-6, table=Non
     (rows may lie apart): Q to q [rows][heads][head_dim], K and V to the rows ``rows`` (int32 [rows], None: in order) of kv
     [kv_rows][2][kv_heads][head_dim]. Gains [head_dim], None: not normalised; ``table`` float32 [positions][rot / 2][2]
     (cos, sin) with ``pos`` int32 [rows] (None: in order), None: not rotated; ``halves``: pairs (i, i + rot / 2)."""
-    dt, dev = _rows_dtype(qkv, "qkv"), qkv.device
-    if q.dim() != 3 or kv.dim() != 4 or kv.shape[1] != 2 or kv.shape[3] != q.shape[2]:
-        raise _bad(f"q must be [rows][heads][head_dim] and kv [kv_rows][2][kv_heads][head_dim], not {tuple(q.shape)} and {tuple(kv.shape)}")
-    M, H, hd = q.shape
-    G = kv.shape[2]
-    cols = (H + 2 * G) * hd
-    if qkv.shape != (M, cols) or (cols > 1 and qkv.stride(1) != 1) or (M > 1 and qkv.stride(0) < cols):
-        raise _bad(f"qkv must be [{M}][{cols}] with neighbouring columns, not {tuple(qkv.shape)} strided {qkv.stride()}")
-    qp, kp = _like(q, q.shape, qkv.dtype, dev, "q"), _like(kv, kv.shape, qkv.dtype, dev, "kv")
-    gains = [None if g is None else _like(g, (hd,), qkv.dtype, dev, "a gain") for g in (q_gain, k_gain)]
+    dt, dev = _on(qkv, "qkv")
+    qs, ks, t = q.shape, kv.shape, qkv.dtype
+    if len(qs) != 3 or len(ks) != 4 or ks[1] != 2 or ks[3] != qs[2]:
+        raise _bad(f"q must be [rows][heads][head_dim] and kv [kv_rows][2][kv_heads][head_dim], not {tuple(qs)} and {tuple(ks)}")
+    M, H, hd = qs
+    G = ks[2]
+    ld = _apart_rows(qkv, M, (H + 2 * G) * hd, "qkv")
     tp, n_pos, rot = None, 0, 0
     if table is not None:
-        if table.dim() != 3 or table.shape[2] != 2:
-            raise _bad(f"table must be [positions][rot / 2][2], not {tuple(table.shape)}")
-        n_pos, rot = table.shape[0], 2 * table.shape[1]
-        tp = _like(table, table.shape, torch.float32, dev, "table") or _KV8_NO_ENTRIES
-    ins = [_span(t) for t in (qkv, q_gain, k_gain, table, pos, rows)]
-    _apart(_span(q), ins + [_span(kv)], "q")
-    _apart(_span(kv), ins, "kv")
-    a = QkNormRopeArgs(dt, M, H, G, hd, qkv.data_ptr(), qkv.stride(0) if M > 1 else cols, gains[0], gains[1], eps, tp, n_pos, rot,
-                       MS_ROPE_HALVES if halves else MS_ROPE_PAIRS, _kv8_table(pos, dev, (M,), "pos"), qp, kp, kv.shape[0],
-                       _kv8_table(rows, dev, (M,), "rows"))
+        shape = table.shape
+        if len(shape) != 3 or shape[2] != 2:
+            raise _bad(f"table must be [positions][rot / 2][2], not {tuple(shape)}")
+        n_pos, rot = shape[0], 2 * shape[1]
+        tp = _like(table, shape, torch.float32, dev, "table") or _KV8_NO_ENTRIES
+    a = QkNormRopeArgs(dt, M, H, G, hd, qkv.data_ptr(), ld, None if q_gain is None else _like(q_gain, (hd,), t, dev, "q_gain"),
+                       None if k_gain is None else _like(k_gain, (hd,), t, dev, "k_gain"), eps, tp, n_pos, rot,
+                       MS_ROPE_HALVES if halves else MS_ROPE_PAIRS, _ints(pos, M, dev, "pos"), _like(q, qs, t, dev, "q"),
+                       _like(kv, ks, t, dev, "kv"), ks[0], _ints(rows, M, dev, "rows"))
     _kv8_run(load().ms_qk_norm_rope, qkv, stream, C.byref(a))
 
 
@@ -542,8 +535,7 @@ def ms_shared_bits(mask, bits, *, stream=None):
     if not mask.is_cuda or mask.dim() != 2 or mask.element_size() != 1 or not mask.is_contiguous():
         raise _bad("mask must be contiguous bytes [batch][tokens] on a GPU")
     B, T = mask.shape
-    bp = _like(bits, (B, -(-T // 64)), torch.int64, mask.device, "bits")
-    _apart(_span(bits), [_span(mask)], "bits")
+    bp = _like(bits, (B, -(-T // 64)), torch.int64, mask.get_device(), "bits")
     _kv8_run(load().ms_shared_bits, mask, stream, mask.data_ptr(), B, T, bp)
 
 
@@ -568,28 +560,24 @@ def ms_shared_attention(q, kv, out, *, seg_start=None, bits=None, fresh=None, fr
     None: 1 / sqrt(head_dim); one that float32 holds as 0 is refused, since 0 stands for None in the library."""
     if scale is not None and C.c_float(scale).value == 0.0:
         raise _bad(f"scale {scale!r} is 0 in float32; None stands for 1 / sqrt(head_dim)")
-    dt, dev = _rows_dtype(q, "q"), q.device
-    if q.dim() != 3 or kv.dim() != 4 or kv.shape[1] != 2 or kv.shape[3] != q.shape[2]:
-        raise _bad(f"q must be [rows][heads][head_dim] and kv [tokens][2][kv_heads][head_dim], not {tuple(q.shape)} and {tuple(kv.shape)}")
-    M, H, hd = q.shape
-    T, G = kv.shape[0], kv.shape[2]
-    qp, kp = _like(q, q.shape, q.dtype, dev, "q"), _like(kv, kv.shape, q.dtype, dev, "kv")
-    op = _like(out, q.shape, q.dtype, dev, "out")
+    dt, dev = _on(q, "q")
+    qs, ks, t = q.shape, kv.shape, q.dtype
+    if len(qs) != 3 or len(ks) != 4 or ks[1] != 2 or ks[3] != qs[2]:
+        raise _bad(f"q must be [rows][heads][head_dim] and kv [tokens][2][kv_heads][head_dim], not {tuple(qs)} and {tuple(ks)}")
+    M, H, hd = qs
+    T, _, G, _ = ks
     B = 1 if seg_start is None else seg_start.numel() - 1
-    sp = _kv8_table(seg_start, dev, (B + 1,), "seg_start")
-    bp = None if bits is None else _like(bits, (B, -(-T // 64)), torch.int64, dev, "bits")
     fp, f_rows, fs = None, 0, None
     if fresh is not None:
         f_rows = fresh.shape[0]
-        fp = _like(fresh, (f_rows, 2, G, hd), q.dtype, dev, "fresh") or None
+        fp = _like(fresh, (f_rows, 2, G, hd), t, dev, "fresh") or None
         if fresh_start is None:
             raise _bad("own rows need fresh_start")
-        fs = _kv8_table(fresh_start, dev, (B + 1,), "fresh_start")
+        fs = _ints(fresh_start, B + 1, dev, "fresh_start")
+    a = SharedAttn(_like(q, qs, t, dev, "q"), _like(out, qs, t, dev, "out"), M, H, G, hd, _like(kv, ks, t, dev, "kv"), T, B,
+                   None if bits is None else _like(bits, (B, -(-T // 64)), torch.int64, dev, "bits"),
+                   _ints(seg_start, B + 1, dev, "seg_start"), fp, f_rows, fs, 0.0 if scale is None else scale)
     wp, wb = _workspace(workspace, dev)
-    ins = [_span(t) for t in (kv, bits, seg_start, fresh, fresh_start)]
-    _apart((op, out.numel() * out.element_size()), ins + ([] if qp == op else [_span(q)]), "out")
-    _apart((wp, wb), ins + [_span(q), _span(out)], "workspace")
-    a = SharedAttn(qp, op, M, H, G, hd, kp, T, B, bp, sp, fp, f_rows, fs, 0.0 if scale is None else scale)
     _kv8_run(load().ms_shared_attention, q, stream, dt, C.byref(a), wp, wb)
 
 
