@@ -54,7 +54,11 @@ struct Mx4LinearDesc {
     const uint8_t *w, *ws;      // codes [N][K / 2], exponent bytes [N][K / 32]
     GemmDesc g;                 // shape, bias, residual, output, epilogue, ksplit and part; kchunk in 256-element steps
     int form;                   // set by plan_mx4_linear
+    int waves;                  // of a workgroup of the forms for few rows
 };
+
+// Outputs of a workgroup: 16, 32 or 64 rows by 16 columns, or square tiles.
+enum { kMx4Rows16 = 0, kMx4Rows32 = 1, kMx4Rows64 = 2, kMx4Tile64 = 3, kMx4Tile128 = 4, kMx4Tile256 = 5 };
 
 hipError_t launch_mx4_quantize(int dtype, const void* x, long rows, int cols, long ld, uint8_t* codes, uint8_t* scales,
                                hipStream_t s);

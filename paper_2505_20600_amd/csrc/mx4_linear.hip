@@ -6,19 +6,24 @@
 // bytes) of row l % 16, columns 32 (l / 16) on, and their exponent byte. W is the
 // first operand, so that a lane's four results are four neighbouring columns of
 // one output row.
+#include <algorithm>
+#include <cstdlib>
+
 #include "gelu.h"
 #include "mx4.h"
 
 namespace ms {
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kStep = 256;              // K elements per step
 constexpr int kRowB = kStep / 2;        // bytes of a staged row
+constexpr int kStepBlocks = kStep / kMxBlock;
 constexpr uint32_t kAbsent = 0xfff00000u;
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
+// w's scale in byte OW of sw, a's in byte OA of sa.
+template <int OW, int OA>
 __device__ __forceinline__ f32x4_t mfma_mx4(const vec16& w, const vec16& a, f32x4_t c, int sw, int sa) {
     i32x8_t x = {}, y = {};
 #pragma unroll
@@ -26,7 +31,25 @@ __device__ __forceinline__ f32x4_t mfma_mx4(const vec16& w, const vec16& a, f32x
         x[i] = (int)w.w[i];
         y[i] = (int)a.w[i];
     }
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, sw, 0, sa);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, OW, sw, OA, sa);
+}
+// The same with byte numbers that are constants once loops are unrolled.
+template <int OW>
+__device__ __forceinline__ f32x4_t mfma_mx4_a(const vec16& w, const vec16& a, f32x4_t c, int sw, int sa, int oa) {
+    switch (oa) {
+        case 0: return mfma_mx4<OW, 0>(w, a, c, sw, sa);
+        case 1: return mfma_mx4<OW, 1>(w, a, c, sw, sa);
+        case 2: return mfma_mx4<OW, 2>(w, a, c, sw, sa);
+        default: return mfma_mx4<OW, 3>(w, a, c, sw, sa);
+    }
+}
+__device__ __forceinline__ f32x4_t mfma_mx4_b(const vec16& w, const vec16& a, f32x4_t c, int sw, int ow, int sa, int oa) {
+    switch (ow) {
+        case 0: return mfma_mx4_a<0>(w, a, c, sw, sa, oa);
+        case 1: return mfma_mx4_a<1>(w, a, c, sw, sa, oa);
+        case 2: return mfma_mx4_a<2>(w, a, c, sw, sa, oa);
+        default: return mfma_mx4_a<3>(w, a, c, sw, sa, oa);
+    }
 }
 
 // Permutation of a staged row's eight 16-byte chunks: 16 rows' reads of one chunk take every bank in turn.
@@ -34,8 +57,7 @@ __device__ __forceinline__ int k_chunk(int r) { return (r >> 1) & 7; }
 
 // Four columns n.. of row m: to the output with the epilogue, or to the K range's part.
 template <typename T, int EPI>
-__device__ __forceinline__ void finish(const GemmDesc& g, int m, int n, int split, const f32x4_t& acc) {
-    float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+__device__ __forceinline__ void finish(const GemmDesc& g, int m, int n, int split, float v[4]) {
     if (g.ksplit > 1) {
         store4<float>(g.part + ((long)split * g.M + m) * g.N + n, v);
         return;
@@ -56,119 +78,552 @@ __device__ __forceinline__ void finish(const GemmDesc& g, int m, int n, int spli
     store4<T>(static_cast<T*>(g.C) + (long)m * g.N + n, v);
 }
 
-template <typename T, int EPI>
-__global__ __launch_bounds__(kThreads) void mx4_linear_kernel(Mx4LinearDesc d) {
-    constexpr int BM = 128, BN = 128, STAGEB = (BM + BN) * kRowB;
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGEB];
+// First row, first column and K range of a workgroup's tile.
+template <int BM, int BN>
+__device__ __forceinline__ void tile_of(const GemmDesc& g, int& m0, int& n0, int& split) {
+    const int mt = (g.M + BM - 1) / BM, nt = (g.N + BN - 1) / BN;
+    const int lb = xcd_logical_block(blockIdx.x, mt * nt * g.ksplit);
+    split = lb / (mt * nt);
+    // groups of group_m row tiles, the column tiles of a group side by side: what an XCD works on stays in its L2
+    const int in = lb % (mt * nt), per = g.group_m * nt, first = in / per * g.group_m;
+    const int gm = min(g.group_m, mt - first), at = in % per;
+    m0 = (first + at % gm) * BM;
+    n0 = at / gm * BN;
+}
+
+// A wave's MI x NI blocks of 16 x 16 outputs from (m0, n0) on: 16 rows at a time through LDS, so that it loads and
+// stores whole lines of a row. A barrier for the workgroup; `smem` is the stages' memory.
+template <typename T, int EPI, int MI, int NI>
+__device__ __forceinline__ void write_tile(const GemmDesc& g, int m0, int n0, int split, const f32x4_t (&acc)[NI][MI], uint8_t* smem,
+                                           int wave, int lane) {
+    constexpr int OLD = NI * 16 + 4;                    // floats of a row in LDS
+    constexpr int COLS = NI * 4, ROWS = kWave / COLS;   // lanes of four columns per row, rows at a time
+    static_assert(kWave % COLS == 0, "output lanes");
+    __syncthreads();    // every wave is past its last read of the stages
+    float* const so = reinterpret_cast<float*>(smem) + wave * 16 * OLD;
+    const int grp = lane / 16, l16 = lane % 16, col = lane % COLS * 4, n = n0 + col, row0 = lane / COLS;
+    const bool whole = g.ksplit == 1, in = n < g.N;
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};
+    if (whole && in) load4<T>(static_cast<const T*>(g.bias) + n, bias);
+#pragma unroll
+    for (int j = 0; j < MI; ++j) {
+        const int m = m0 + j * 16 + row0;
+        float res[16 / ROWS][4];
+        if constexpr (EPI == kEpiBiasResid) {       // on their way while the sums pass through LDS
+#pragma unroll
+            for (int r = 0; r < 16 / ROWS; ++r) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) res[r][e] = 0.f;
+                if (whole && in && m + r * ROWS < g.M) load4<T>(static_cast<const T*>(g.R) + (long)(m + r * ROWS) * g.N + n, res[r]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+            store4<float>(so + l16 * OLD + i * 16 + grp * 4, v);
+        }
+        asm volatile("" ::: "memory");      // LDS operations of a wave are done in order
+        float v[16 / ROWS][4];
+#pragma unroll
+        for (int r = 0; r < 16 / ROWS; ++r) load4<float>(so + (row0 + r * ROWS) * OLD + col, v[r]);
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int r = 0; r < 16 / ROWS; ++r) {
+            if (!in || m + r * ROWS >= g.M) continue;
+            if (!whole) {
+                store4<float>(g.part + ((long)split * g.M + m + r * ROWS) * g.N + n, v[r]);
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[r][e] += bias[e];
+                if constexpr (EPI == kEpiBiasGelu) v[r][e] = gelu(v[r][e]);
+                if constexpr (EPI == kEpiBiasResid) v[r][e] += res[r][e];
+            }
+            store4<T>(static_cast<T*>(g.C) + (long)(m + r * ROWS) * g.N + n, v[r]);
+        }
+    }
+}
+
+// Tiles of BM x BN outputs by WM x WN waves, steps of 256 elements of K in two stages of LDS. Codes land
+// there by direct loads; a step's scales (8 bytes a row) come through registers, a thread to a row, and are laid
+// out so that a lane finds those of its row and columns for two fragments and both halves of the step in one word.
+template <int BM, int BN, int WM, int WN>
+struct Tile {
+    static constexpr int NT = WM * WN * kWave;
+    static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;      // 16 x 16 outputs of a wave
+    static constexpr int CODEB = (BM + BN) * kRowB, SCALEB = (BM + BN) * kStepBlocks;
+    static constexpr int STAGEB = CODEB + SCALEB;
+    static constexpr int OUTB = WM * WN * 16 * (NI * 16 + 4) * 4;
+    static constexpr int LDSB = 2 * STAGEB > OUTB ? 2 * STAGEB : OUTB;
+    static constexpr int COPIES = (BM + BN) / 8;                    // of 1 KB
+    static_assert(COPIES % (WM * WN) == 0 && BM % 64 == 0 && BN % 64 == 0 && BM + BN <= NT && MI % 2 == 0 && NI % 2 == 0, "tile");
+};
+
+template <typename T, int EPI, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * kWave) void mx4_linear_kernel(Mx4LinearDesc d) {
+    using C = Tile<BM, BN, WM, WN>;
+    constexpr int MI = C::MI, NI = C::NI;
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDSB];
     const GemmDesc& g = d.g;
     const uint32_t lds0 = lds_addr(smem);
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int grp = lane / 16, l16 = lane % 16;
-    const int mt = (g.M + BM - 1) / BM, nt = (g.N + BN - 1) / BN;
-    const int lb = xcd_logical_block(blockIdx.x, mt * nt * g.ksplit);
-    const int m0 = lb % mt * BM, n0 = lb / mt % nt * BN, split = lb / (mt * nt);
-    const uint32_t rowb = (uint32_t)g.K / 2, blocks = (uint32_t)g.K / kMxBlock;
+    int m0, n0, split;
+    tile_of<BM, BN>(g, m0, n0, split);
+    const uint32_t rowb = (uint32_t)g.K / 2;
+    const int blocks = g.K / kMxBlock;
     const int rows_a = min(BM, g.M - m0), rows_w = min(BN, g.N - n0);
     const u32x4_t ra = raw_rsrc(d.a + (long)m0 * rowb, (uint32_t)rows_a * rowb), rw = raw_rsrc(d.w + (long)n0 * rowb, (uint32_t)rows_w * rowb);
-    const __amdgpu_buffer_rsrc_t sa = make_rsrc(d.as + (long)m0 * blocks, (uint32_t)rows_a * blocks), sw = make_rsrc(d.ws + (long)n0 * blocks, (uint32_t)rows_w * blocks);
     const int steps = (g.K + kStep - 1) / kStep;
     const int t0 = split * g.kchunk, t1 = min(steps, t0 + g.kchunk);
 
-    // stage: BM rows of A, then BN of W, a row's 16-byte chunks permuted by the row
-    auto issue = [&](int t, int st) {
+    // stage: BM rows of A, then BN of W, a row's 16-byte chunks permuted by the row; then the scales
+    constexpr int PER = C::COPIES / (WM * WN);
+    uint32_t voff[PER];
+    int chunk[PER];
 #pragma unroll
-        for (int i = 0; i < (BM + BN) / 8 / 4; ++i) {
-            const int q = i * 4 + wave, r = (q * 8 + lane / 8) % BM;
-            const int c = t * 8 + ((lane % 8) ^ k_chunk(r));
-            const uint32_t off = c < (int)blocks ? (uint32_t)r * rowb + c * 16 : kAbsent;
-            dma_buf16(q < BM / 8 ? ra : rw, off, 0, lds0 + st * STAGEB + q * 1024);
+    for (int i = 0; i < PER; ++i) {
+        const int q = i * WM * WN + wave, r = (q < BM / 8 ? q : q - BM / 8) * 8 + lane / 8;
+        chunk[i] = (lane % 8) ^ k_chunk(r);
+        voff[i] = (uint32_t)r * rowb + chunk[i] * 16;
+    }
+    auto issue = [&](int t, int st) {
+        const bool whole = (t + 1) * kStepBlocks <= blocks;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int q = i * WM * WN + wave;
+            const uint32_t off = whole || t * kStepBlocks + chunk[i] < blocks ? voff[i] + (uint32_t)t * kRowB : kAbsent;
+            dma_buf16(q < BM / 8 ? ra : rw, off, 0, lds0 + st * C::STAGEB + q * 1024);
         }
     };
-    const int wm = wave % 2 * 64, wn = wave / 2 * 64;
-    int xa[2][4], xw[2][4];
-    auto scales = [&](int t) {
+    // this thread's row of scales: eight bytes of step t, zeros past K and past the last row
+    const bool row_of_a = tid < BM;
+    const int srow = row_of_a ? tid : tid - BM;
+    const bool has_row = tid < BM + BN && srow < (row_of_a ? rows_a : rows_w);
+    const uint8_t* const sp = (row_of_a ? d.as + (long)(m0 + (has_row ? srow : 0)) * blocks : d.ws + (long)(n0 + (has_row ? srow : 0)) * blocks);
+    const bool words = (((uintptr_t)d.as | (uintptr_t)d.ws | (uintptr_t)blocks) & 3) == 0;
+    auto load_scales = [&](int t, uint32_t (&v)[2]) {
+        v[0] = v[1] = 0;
+        if (!has_row || t >= t1) return;
+        const uint8_t* const p = sp + t * kStepBlocks;
+        const int n = min(kStepBlocks, blocks - t * kStepBlocks);
+        if (words) {
+            v[0] = reinterpret_cast<const uint32_t*>(p)[0];
+            if (n > 4) v[1] = reinterpret_cast<const uint32_t*>(p)[1];
+        } else {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = t * 8 + k * 4 + grp;
-                const bool in = c < (int)blocks;
-                xa[k][i] = __builtin_amdgcn_raw_buffer_load_b8(sa, in ? (wm + i * 16 + l16) * blocks + c : kAbsent, 0, 0);
-                xw[k][i] = __builtin_amdgcn_raw_buffer_load_b8(sw, in ? (wn + i * 16 + l16) * blocks + c : kAbsent, 0, 0);
-            }
+            for (int i = 0; i < kStepBlocks; ++i)
+                if (i < n) v[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
+        }
     };
-    f32x4_t acc[4][4];
+    // [64 rows][lane group][row % 16][row / 16][half of the step]
+    const uint32_t sdst = (uint32_t)(tid / 64 * 512 + tid % 16 * 8 + tid % 64 / 16 * 2);
+    auto store_scales = [&](const uint32_t (&v)[2], int st) {
+        if (tid >= BM + BN) return;
+        uint8_t* const p = smem + st * C::STAGEB + C::CODEB + sdst;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<uint16_t*>(p + k * 128) = (uint16_t)((v[0] >> (8 * k) & 0xff) | (v[1] >> (8 * k) & 0xff) << 8);
+    };
+    const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
+    auto scale_at = [&](int row) { return (uint32_t)(row / 64 * 512 + grp * 128 + l16 * 8 + row % 64 / 32 * 4); };
+
+    f32x4_t acc[NI][MI];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < MI; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    uint32_t next[2];
     if (t0 < t1) {
-        scales(t0);
+        load_scales(t0, next);
         issue(t0, 0);
+        store_scales(next, 0);
+        load_scales(t0 + 1, next);
     }
     for (int t = t0; t < t1; ++t) {
-        int ca[2][4], cw[2][4];
+        wait_all();     // step t has landed, and this wave's reads of the stage refilled below are done
+        barrier_only();
+        const int st = (t - t0) & 1;
+        if (t + 1 < t1) {
+            store_scales(next, st ^ 1);
+            issue(t + 1, st ^ 1);
+            load_scales(t + 2, next);
+        }
+        const uint8_t* const s = smem + st * C::STAGEB;
+        uint32_t sa[MI / 2], sw[NI / 2];
+#pragma unroll
+        for (int j = 0; j < MI / 2; ++j) sa[j] = *reinterpret_cast<const uint32_t*>(s + C::CODEB + scale_at(wm + j * 32));
+#pragma unroll
+        for (int i = 0; i < NI / 2; ++i) sw[i] = *reinterpret_cast<const uint32_t*>(s + C::CODEB + scale_at(BM + wn + i * 32));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            vec16 fa[MI], fw[NI];
+            const int c = ((k * 4 + grp) ^ k_chunk(l16)) * 16;
+#pragma unroll
+            for (int j = 0; j < MI; ++j) fa[j] = ld16(s + (wm + j * 16 + l16) * kRowB + c);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) fw[i] = ld16(s + (BM + wn + i * 16 + l16) * kRowB + c);
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int j = 0; j < MI; ++j)
+                    acc[i][j] = mfma_mx4_b(fw[i], fa[j], acc[i][j], (int)sw[i / 2], i % 2 * 2 + k, (int)sa[j / 2], j % 2 * 2 + k);
+        }
+    }
+    write_tile<T, EPI, MI, NI>(g, m0 + wm, n0 + wn, split, acc, smem, wave, lane);
+}
+
+// Lane (group g of 16, l) holds the four scale bytes of row 16 g + l, one per 32 columns; returns, in byte i, that
+// of row 16 i + l and columns 32 g on: a transpose of 4 x 4 bytes across the lane groups in two exchanges.
+__device__ __forceinline__ uint32_t scale_bytes(uint32_t v, uint32_t pick2, uint32_t pick1) {
+    const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);       // of group g % 2, of group g % 2 + 2
+    const uint32_t e = __builtin_amdgcn_perm(a[1], a[0], pick2);               // their columns 2 (g / 2) and 2 (g / 2) + 1
+    const auto b = __builtin_amdgcn_permlane16_swap(e, e, false, false);       // the same of even and odd groups
+    return __builtin_amdgcn_perm(b[1], b[0], pick1);
+}
+
+// The same where K is a multiple of 128 and the scales are 4-byte aligned: everything lands in LDS by direct loads. Such a
+// load costs a CU about four cycles per 128-byte line that it touches, however little of it, so a row's codes come
+// as 128 bytes (a step) and its scales as 32 (four steps). A stage is three regions: the rows of A, and the first and the
+// second half of every wave's rows of W. Halfway through step t all waves have A's fragments in registers and are done
+// with the first half of W: there, at the only barrier of a step, these regions take step t + 2 and the second half's other
+// stage step t + 1, so that a whole step's copies are under way all the time; the fragments that step t + 1 starts with
+// are read under the last products of step t.
+template <int BM, int BN, int WM, int WN>
+struct Stream {
+    static constexpr int NW = WM * WN;
+    static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
+    static constexpr int ROWB = kRowB, HALFN = BN / WN / 2;         // rows of W of a wave in each of its regions
+    static constexpr int AT_W = BM * ROWB, REGW = BN / 2 * ROWB, STAGEB = AT_W + 2 * REGW;
+    static constexpr int SCALES = 2 * STAGEB, SCALEB = (BM + BN) * 32;  // two blocks of four steps' scales behind the stages
+    static constexpr int OUTB = NW * 16 * (NI * 16 + 4) * 4;
+    static constexpr int END = SCALES + 2 * SCALEB, LDSB = END > OUTB ? END : OUTB;
+    static constexpr int PA = BM / 8 / NW, PW = BN / 16 / NW;       // 1 KB copies of a wave: A, half of W
+    static constexpr int SC = (BM + BN) / 32, PS = (SC + NW - 1) / NW;  // 1 KB copies of scales, those of a wave
+    static_assert(BM / 8 % NW == 0 && BN / 16 % NW == 0 && BM % 64 == 0 && BN % 64 == 0 && NI % 2 == 0 && MI <= 4, "tile");
+};
+
+template <typename T, int EPI, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * kWave) void mx4_stream_kernel(Mx4LinearDesc d) {
+    using C = Stream<BM, BN, WM, WN>;
+    constexpr int MI = C::MI, NI = C::NI, NS = (NI + 3) / 4;
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDSB];
+    const GemmDesc& g = d.g;
+    const uint32_t lds0 = lds_addr(smem);
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int grp = lane / 16, l16 = lane % 16;
+    int m0, n0, split;
+    tile_of<BM, BN>(g, m0, n0, split);
+    const uint32_t rowb = (uint32_t)g.K / 2, blocks = (uint32_t)g.K / kMxBlock;
+    const int rows_a = min(BM, g.M - m0), rows_w = min(BN, g.N - n0);
+    const u32x4_t ra = raw_rsrc(d.a + (long)m0 * rowb, (uint32_t)rows_a * rowb), rw = raw_rsrc(d.w + (long)n0 * rowb, (uint32_t)rows_w * rowb);
+    const u32x4_t qa = raw_rsrc(d.as + (long)m0 * blocks, (uint32_t)rows_a * blocks), qw = raw_rsrc(d.ws + (long)n0 * blocks, (uint32_t)rows_w * blocks);
+    const int steps = (g.K + kStep - 1) / kStep;
+    const int t0 = split * g.kchunk, t1 = min(steps, t0 + g.kchunk);
+    const int half_step = g.K % kStep ? steps - 1 : -1;     // its second half lies past K
+
+    // rows past the last lie past the buffers and read as zeros; a row's 16-byte chunks are permuted by the row
+    uint32_t va[C::PA], vw[C::PW], vs[C::PS];
+    const int c8 = (lane % 8) ^ k_chunk(lane / 8), c8b = (lane % 8) ^ k_chunk(lane / 8 + 8);    // of a copy's rows: even, odd copies
+#pragma unroll
+    for (int i = 0; i < C::PA; ++i) {
+        const int q = i * C::NW + wave;
+        va[i] = (uint32_t)(q * 8 + lane / 8) * rowb + (q % 2 ? c8b : c8) * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < C::PW; ++i) {
+        const int q = i * C::NW + wave, r = q * 8 + lane / 8;
+        vw[i] = (uint32_t)(r / C::HALFN * 2 * C::HALFN + r % C::HALFN) * rowb + (q % 2 ? c8b : c8) * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < C::PS; ++i) {       // copies past the last repeat earlier ones
+        const int c = (i * C::NW + wave) % C::SC;
+        vs[i] = (uint32_t)((c < BM / 32 ? c : c - BM / 32) * 32 + lane / 2) * blocks + lane % 2 * 16;
+    }
+    const bool past0 = c8 >= 4, past1 = c8b >= 4;           // chunks that the half step lacks
+    auto issue_a = [&](int t, int i) {
+        const int q = i * C::NW + wave;
+        const bool absent = t == half_step && (q % 2 ? past1 : past0);
+        dma_buf16(ra, absent ? kAbsent : va[i], (uint32_t)t * C::ROWB, lds0 + (t & 1) * C::STAGEB + q * 1024);
+    };
+    auto issue_w = [&](int t, int part, int i) {
+        const int q = i * C::NW + wave;
+        const bool absent = t == half_step && (q % 2 ? past1 : past0);
+        dma_buf16(rw, absent ? kAbsent : vw[i], (uint32_t)t * C::ROWB + (uint32_t)part * C::HALFN * rowb,
+                  lds0 + (t & 1) * C::STAGEB + C::AT_W + part * C::REGW + q * 1024);
+    };
+    // scales of steps 4 b to 4 b + 3; what lies past a row's end is not used
+    auto issue_scales = [&](int b, int i) {
+        const int c = (i * C::NW + wave) % C::SC;
+        dma_buf16(c < BM / 32 ? qa : qw, vs[i], (uint32_t)b * 32u, lds0 + C::SCALES + (b & 1) * C::SCALEB + c * 1024);
+    };
+    const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
+
+    f32x4_t acc[NI][MI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < MI; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // selectors of the scales' transpose
+    const uint32_t pick2 = grp < 2 ? 0x05040100u : 0x07060302u, pick1 = grp % 2 ? 0x07030501u : 0x06020400u;
+    // scales of up to 64 staged rows from `row` on, both halves of step t as they lie
+    auto read_scales = [&](int t, int row, int rows) {
+        const uint8_t* const p = smem + C::SCALES + (t / 4 & 1) * C::SCALEB + t % 4 * 8;
+        return *reinterpret_cast<const uint2*>(p + (row + lane % (rows < 64 ? rows : 64)) * 32);
+    };
+    const uint32_t at_k[2] = {(uint32_t)((grp ^ k_chunk(l16)) * 16), (uint32_t)(((4 + grp) ^ k_chunk(l16)) * 16)};
+    const uint32_t at_a = (uint32_t)(wm + l16) * C::ROWB;
+    const uint32_t at_w = (uint32_t)(C::AT_W + (wn / 2 + l16) * C::ROWB);
+    // what a step starts with; A's other half is read under its first products
+    struct Start {
+        vec16 a[MI], w[2];
+        uint32_t sa[2], sw[2][NS];
+    };
+    auto read_a = [&](int t, int k, int j) { return ld16(smem + (t & 1) * C::STAGEB + at_a + j * 16 * C::ROWB + at_k[k]); };
+    auto read_w = [&](int t, int i, int k) {
+        return ld16(smem + (t & 1) * C::STAGEB + at_w + (i < NI / 2 ? i * 16 * C::ROWB : C::REGW + (i - NI / 2) * 16 * C::ROWB) + at_k[k]);
+    };
+    // A step is 2 MI NI slots of one product each; what has to be done besides is dealt out to them in a fixed order, so that
+    // it is issued while the matrix cores work. After the barrier (slot MID): the copies, the next step's first
+    // operands, and the transposes of its scales.
+    constexpr int SLOTS = 2 * MI * NI, MID = (NI / 2 - 1) * 2 * MI;
+    constexpr int A0 = C::PW, A1 = A0 + C::PA, A2 = A1 + C::PW, A3 = A2 + C::PS, A4 = A3 + 1 + NS, A5 = A4 + MI, A6 = A5 + 2 * (1 + NS), AUX = A6 + 2;
+    auto step = [&](const Start& c, Start& n, int t) __attribute__((always_inline)) {
+        vec16 w[NI][2], a1[MI];
+        uint2 raw[1 + NS];
+        w[0][0] = c.w[0];
+        w[0][1] = c.w[1];
+        const uint32_t upper = t + 1 == half_step ? 0u : ~0u;       // a row's end may have any bytes behind it
+        auto other = [&](int x) __attribute__((always_inline)) {
+            if (x < A0) {
+                if (t + 1 < t1) issue_w(t + 1, 1, x);
+            } else if (x < A1) {
+                if (t + 2 < t1) issue_a(t + 2, x - A0);
+            } else if (x < A2) {
+                if (t + 2 < t1) issue_w(t + 2, 0, x - A1);
+            } else if (x < A3) {
+                if (t + 2 < t1 && (t + 2) % 4 == 0) issue_scales((t + 2) / 4, x - A2);
+            } else if (x < A4) {
+                raw[x - A3] = x == A3 ? read_scales(t + 1, wm, MI * 16) : read_scales(t + 1, BM + wn + (x - A3 - 1) * 64, NI * 16);
+            } else if (x < A5) {
+                n.a[x - A4] = read_a(t + 1, 0, x - A4);
+            } else if (x < A6) {
+                const int y = (x - A5) / 2, k = (x - A5) % 2;
+                const uint32_t v = scale_bytes(k ? raw[y].y & upper : raw[y].x, pick2, pick1);
+                if (y == 0) n.sa[k] = v;
+                else n.sw[k][y - 1] = v;
+            } else {
+                n.w[x - A6] = read_w(t + 1, 0, x - A6);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < MI; ++j) {
+                    const int slot = (i * 2 + k) * MI + j;
+                    if (MID >= MI ? slot < MI : slot == 0) {    // before the barrier
+#pragma unroll
+                        for (int x = 0; x < MI; ++x)
+                            if (MID < MI || x == slot) a1[x] = read_a(t, 1, x);
+                    }
+                    if (slot == MID) {
+                        wait_all();     // what the last step's middle sent for has landed; A and the first half of W are read
+                        barrier_only();
+                    }
+                    if (i + 1 < NI && k == 0 && j < 2) w[i + 1][j] = read_w(t, i + 1, j);
+#pragma unroll
+                    for (int x = 0; x < AUX; ++x)
+                        if (MID + 1 + x * (SLOTS - MID - 1) / AUX == slot) other(x);
+                    __builtin_amdgcn_sched_barrier(0);
+                    acc[i][j] = mfma_mx4_b(w[i][k], k ? a1[j] : c.a[j], acc[i][j], (int)c.sw[k][i / 4], i % 4, (int)c.sa[k], j);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+    };
+    if (t0 < t1) {
+        auto issue_step = [&](int t, bool scales, int parts) {
+#pragma unroll
+            for (int i = 0; i < C::PS; ++i)
+                if (scales) issue_scales(t / 4, i);
+#pragma unroll
+            for (int i = 0; i < C::PA; ++i) issue_a(t, i);
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int i = 0; i < C::PW; ++i)
+                    if (p < parts) issue_w(t, p, i);
+        };
+        issue_step(t0, true, 2);
+        if (t0 + 1 < t1) {
+            issue_step(t0 + 1, (t0 + 1) % 4 == 0, 1);
+            wait_vmcnt<C::PA + C::PW>();
+        } else {
+            wait_all();
+        }
+        barrier_only();
+        Start f0, f1;
+        const uint32_t upper = t0 == half_step ? 0u : ~0u;
+        const uint2 v = read_scales(t0, wm, MI * 16);
+        f0.sa[0] = scale_bytes(v.x, pick2, pick1);
+        f0.sa[1] = scale_bytes(v.y & upper, pick2, pick1);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            const uint2 u = read_scales(t0, BM + wn + i * 64, NI * 16);
+            f0.sw[0][i] = scale_bytes(u.x, pick2, pick1);
+            f0.sw[1][i] = scale_bytes(u.y & upper, pick2, pick1);
+        }
+#pragma unroll
+        for (int j = 0; j < MI; ++j) f0.a[j] = read_a(t0, 0, j);
+        f0.w[0] = read_w(t0, 0, 0);
+        f0.w[1] = read_w(t0, 0, 1);
+        for (int t = t0; t < t1; ++t) {
+            step(f0, f1, t);
+            f0 = f1;
+        }
+    }
+    wait_all();
+    write_tile<T, EPI, MI, NI>(g, m0 + wm, n0 + wn, split, acc, smem, wave, lane);
+}
+
+// Few rows: 16 columns of the output and MI x 16 rows per workgroup; every wave has 256-element steps of its own (step
+// wave + waves i) and loads its fragments from global memory, the weights' rows once in all; the waves' sums meet in LDS.
+template <typename T, int EPI, int MI>
+__global__ __launch_bounds__(1024) void mx4_rows_kernel(Mx4LinearDesc d) {
+    constexpr int OLD = 20;
+    __shared__ __attribute__((aligned(16))) float smem[16 * MI * 16 * OLD];
+    const GemmDesc& g = d.g;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), waves = blockDim.x / kWave;
+    const int grp = lane / 16, l16 = lane % 16;
+    const int nt = (g.N + 15) / 16;
+    const int n0 = (int)(blockIdx.x % nt) * 16, m0 = (int)(blockIdx.x / nt) * MI * 16;
+    const uint32_t rowb = (uint32_t)g.K / 2;
+    const int blocks = g.K / kMxBlock, steps = (g.K + kStep - 1) / kStep;
+    const int rows_a = min(MI * 16, g.M - m0), rows_w = min(16, g.N - n0);
+    const __amdgpu_buffer_rsrc_t ra = make_rsrc(d.a + (long)m0 * rowb, (uint32_t)rows_a * rowb), rw = make_rsrc(d.w + (long)n0 * rowb, (uint32_t)rows_w * rowb);
+    const __amdgpu_buffer_rsrc_t qa = make_rsrc(d.as + (long)m0 * blocks, (uint32_t)(rows_a * blocks)), qw = make_rsrc(d.ws + (long)n0 * blocks, (uint32_t)(rows_w * blocks));
+    f32x4_t acc[MI];
+#pragma unroll
+    for (int j = 0; j < MI; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    struct Frag {
+        vec16 w[2], a[2][MI];
+        int sw[2], sa[2][MI];
+    };
+    auto load = [&](int t, Frag& f) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int b = t * kStepBlocks + k * 4 + grp;
+            const bool in = t < steps && b < blocks;
+            f.w[k] = buf_ld16(rw, in ? (uint32_t)l16 * rowb + b * 16 : kAbsent, 0);
+            f.sw[k] = __builtin_amdgcn_raw_buffer_load_b8(qw, in ? l16 * blocks + b : (int)kAbsent, 0, 0);
+#pragma unroll
+            for (int j = 0; j < MI; ++j) {
+                f.a[k][j] = buf_ld16(ra, in ? (uint32_t)(j * 16 + l16) * rowb + b * 16 : kAbsent, 0);
+                f.sa[k][j] = __builtin_amdgcn_raw_buffer_load_b8(qa, in ? (j * 16 + l16) * blocks + b : (int)kAbsent, 0, 0);
+            }
+        }
+    };
+    auto multiply = [&](const Frag& f) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                ca[k][i] = xa[k][i];
-                cw[k][i] = xw[k][i];
-            }
-        wait_all();
-        barrier_only();
-        if (t + 1 < t1) {
-            scales(t + 1);
-            issue(t + 1, (t + 1 - t0) & 1);
-        }
-        const uint8_t* const s = smem + ((t - t0) & 1) * STAGEB;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            vec16 fa[4], fw[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = ((k * 4 + grp) ^ k_chunk(l16)) * 16;
-                fa[i] = ld16(s + (wm + i * 16 + l16) * kRowB + c);
-                fw[i] = ld16(s + (BM + wn + i * 16 + l16) * kRowB + c);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = mfma_mx4(fw[i], fa[j], acc[i][j], cw[k][i], ca[k][j]);
-        }
+            for (int j = 0; j < MI; ++j) acc[j] = mfma_mx4<0, 0>(f.w[k], f.a[k][j], acc[j], f.sw[k], f.sa[k][j]);
+    };
+    Frag f0, f1;
+    load(wave, f0);
+    for (int t = wave; t < steps; t += 2 * waves) {
+        load(t + waves, f1);        // past the last step: zeros
+        multiply(f0);
+        load(t + 2 * waves, f0);
+        multiply(f1);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int n = n0 + wn + i * 16 + grp * 4;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int m = m0 + wm + j * 16 + l16;
-            if (m < g.M && n < g.N) finish<T, EPI>(g, m, n, split, acc[i][j]);
-        }
+    for (int j = 0; j < MI; ++j) {
+        const float v[4] = {acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
+        store4<float>(smem + ((wave * MI + j) * 16 + l16) * OLD + grp * 4, v);
     }
+    __syncthreads();
+    for (int i = tid; i < MI * 64; i += blockDim.x) {       // a thread per row and four columns
+        const int row = i / 4, n = n0 + i % 4 * 4, m = m0 + row;
+        if (m >= g.M || n >= g.N) continue;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < waves; ++w) {
+            float p[4];
+            load4<float>(smem + ((w * MI) * 16 + row) * OLD + i % 4 * 4, p);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] += p[r];
+        }
+        finish<T, EPI>(g, m, n, 0, v);
+    }
+}
+
+template <typename T, int EPI>
+hipError_t launch(const Mx4LinearDesc& d, hipStream_t s) {
+    const GemmDesc& g = d.g;
+#define MS_TILE(form_, BM, BN, WM, WN)                                                                                            \
+    case form_:                                                                                                                   \
+        hipLaunchKernelGGL((mx4_linear_kernel<T, EPI, BM, BN, WM, WN>),                                                           \
+                           dim3((unsigned)(((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN) * g.ksplit)), dim3(WM * WN * kWave), 0, s, d); \
+        break;
+#define MS_STREAM(form_, BM, BN, WM, WN)                                                                                       \
+    case form_:                                                                                                                   \
+        hipLaunchKernelGGL((mx4_stream_kernel<T, EPI, BM, BN, WM, WN>),                                                        \
+                           dim3((unsigned)(((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN) * g.ksplit)), dim3(WM * WN * kWave), 0, s, d); \
+        break;
+#define MS_ROWS(form_, MI)                                                                                                        \
+    case form_:                                                                                                                   \
+        hipLaunchKernelGGL((mx4_rows_kernel<T, EPI, MI>), dim3((unsigned)(((g.N + 15) / 16) * ((g.M + MI * 16 - 1) / (MI * 16)))),   \
+                           dim3(d.waves * kWave), 0, s, d);                                                                       \
+        break;
+    switch (d.form) {
+        MS_ROWS(kMx4Rows16, 1)
+        MS_ROWS(kMx4Rows32, 2)
+        MS_ROWS(kMx4Rows64, 4)
+        MS_TILE(kMx4Tile64, 64, 64, 2, 2)
+        MS_TILE(kMx4Tile128, 128, 128, 2, 2)
+        MS_TILE(kMx4Tile256, 256, 256, 4, 2)
+        MS_STREAM(6, 64, 64, 2, 2)
+        MS_STREAM(7, 128, 128, 2, 2)
+        MS_STREAM(8, 256, 256, 4, 2)
+        MS_STREAM(9, 256, 128, 4, 2)
+        MS_STREAM(10, 64, 128, 2, 2)
+        default: return hipErrorInvalidValue;
+    }
+#undef MS_TILE
+#undef MS_ROWS
+    return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch(const Mx4LinearDesc& d, hipStream_t s) {
-    const GemmDesc& g = d.g;
-    const dim3 grid((unsigned)(((g.M + 127) / 128) * ((g.N + 127) / 128) * g.ksplit)), block(kThreads);
-    switch (g.epilogue) {
-        case kEpiBias: hipLaunchKernelGGL((mx4_linear_kernel<T, kEpiBias>), grid, block, 0, s, d); break;
-        case kEpiBiasResid: hipLaunchKernelGGL((mx4_linear_kernel<T, kEpiBiasResid>), grid, block, 0, s, d); break;
-        case kEpiBiasGelu: hipLaunchKernelGGL((mx4_linear_kernel<T, kEpiBiasGelu>), grid, block, 0, s, d); break;
+    switch (d.g.epilogue) {
+        case kEpiBias: return launch<T, kEpiBias>(d, s);
+        case kEpiBiasResid: return launch<T, kEpiBiasResid>(d, s);
+        case kEpiBiasGelu: return launch<T, kEpiBiasGelu>(d, s);
         default: return hipErrorInvalidValue;
     }
-    return hipGetLastError();
 }
+
+int tile_side(int form) { return form == kMx4Tile64 ? 64 : form == kMx4Tile128 ? 128 : 256; }
 
 }  // namespace
 
 void plan_mx4_linear(Mx4LinearDesc& d, size_t part_floats) {
     GemmDesc& g = d.g;
     const int steps = (g.K + kStep - 1) / kStep;
-    d.form = 0;
+    auto tiles = [&](int side) { return (long)((g.M + side - 1) / side) * ((g.N + side - 1) / side); };
+    if (const char* v = std::getenv("MS_MX4_FORM")) d.form = std::atoi(v);
+    else d.form = g.M <= 16 ? kMx4Rows16 : g.M <= 32 ? kMx4Rows32 : g.M <= 64 ? kMx4Rows64 : tiles(256) >= 256 ? kMx4Tile256 : tiles(128) >= 256 ? kMx4Tile128 : kMx4Tile64;
+    d.waves = std::min(16, steps);
     g.ksplit = 1;
     g.kchunk = steps;
+    g.group_m = 4;
+    if (const char* v = std::getenv("MS_MX4_SPLIT")) {
+        g.ksplit = d.form < 3 ? 1 : std::max(1, std::min<int>(std::min<long>(std::atoi(v), steps), (long)std::min<size_t>(1000, part_floats / ((size_t)g.M * g.N))));
+        g.kchunk = (steps + g.ksplit - 1) / g.ksplit;
+        g.ksplit = (steps + g.kchunk - 1) / g.kchunk;
+    }
 }
 
 hipError_t launch_mx4_linear(int dtype, const Mx4LinearDesc& d, hipStream_t s) {
