@@ -54,17 +54,17 @@ struct Mx4LinearDesc {
     const uint8_t *w, *ws;      // codes [N][K / 2], exponent bytes [N][K / 32]
     GemmDesc g;                 // shape, bias, residual, output, epilogue, ksplit and part; kchunk in 256-element steps
     int form;                   // set by plan_mx4_linear
-    int waves;                  // of a workgroup of the forms for few rows
+    int waves;                  // of a workgroup of the form for few rows
 };
 
-// Outputs of a workgroup: 16, 32 or 64 rows by 16 columns, or square tiles.
-enum { kMx4Rows16 = 0, kMx4Rows32 = 1, kMx4Rows64 = 2, kMx4Tile64 = 3, kMx4Tile128 = 4, kMx4Tile256 = 5 };
+// Outputs of a workgroup: 16 x 16, or tiles of 64, 128 or 256 rows and columns, of any K or (Stream) a multiple of 128.
+enum { kMx4Rows = 0, kMx4Any64, kMx4Any256, kMx4Stream64, kMx4Stream128, kMx4Stream256 };
 
 hipError_t launch_mx4_quantize(int dtype, const void* x, long rows, int cols, long ld, uint8_t* codes, uint8_t* scales,
                                hipStream_t s);
 hipError_t launch_mx4_dequantize(int dtype, const uint8_t* codes, const uint8_t* scales, long rows, int cols, void* x,
                                  long ld, hipStream_t s);
-// Sets the form and the K split from the shape.
+// Sets the form and the K split from the shape, the scales' alignment and what the caller's buffer for parts holds.
 void plan_mx4_linear(Mx4LinearDesc& d, size_t part_floats);
 hipError_t launch_mx4_linear(int dtype, const Mx4LinearDesc& d, hipStream_t s);
 

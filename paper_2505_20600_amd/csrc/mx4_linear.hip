@@ -7,7 +7,7 @@
 // first operand, so that a lane's four results are four neighbouring columns of
 // one output row.
 #include <algorithm>
-#include <cstdlib>
+#include <cmath>
 
 #include "gelu.h"
 #include "mx4.h"
@@ -55,13 +55,9 @@ __device__ __forceinline__ f32x4_t mfma_mx4_b(const vec16& w, const vec16& a, f3
 // Permutation of a staged row's eight 16-byte chunks: 16 rows' reads of one chunk take every bank in turn.
 __device__ __forceinline__ int k_chunk(int r) { return (r >> 1) & 7; }
 
-// Four columns n.. of row m: to the output with the epilogue, or to the K range's part.
+// Four columns n.. of row m to the output, with the epilogue.
 template <typename T, int EPI>
-__device__ __forceinline__ void finish(const GemmDesc& g, int m, int n, int split, float v[4]) {
-    if (g.ksplit > 1) {
-        store4<float>(g.part + ((long)split * g.M + m) * g.N + n, v);
-        return;
-    }
+__device__ __forceinline__ void finish(const GemmDesc& g, int m, int n, float v[4]) {
     float b[4];
     load4<T>(static_cast<const T*>(g.bias) + n, b);
 #pragma unroll
@@ -202,15 +198,13 @@ __global__ __launch_bounds__(WM * WN * kWave) void mx4_linear_kernel(Mx4LinearDe
     const int srow = row_of_a ? tid : tid - BM;
     const bool has_row = tid < BM + BN && srow < (row_of_a ? rows_a : rows_w);
     const uint8_t* const sp = (row_of_a ? d.as + (long)(m0 + (has_row ? srow : 0)) * blocks : d.ws + (long)(n0 + (has_row ? srow : 0)) * blocks);
-    const bool words = (((uintptr_t)d.as | (uintptr_t)d.ws | (uintptr_t)blocks) & 3) == 0;
     auto load_scales = [&](int t, uint32_t (&v)[2]) {
         v[0] = v[1] = 0;
         if (!has_row || t >= t1) return;
         const uint8_t* const p = sp + t * kStepBlocks;
         const int n = min(kStepBlocks, blocks - t * kStepBlocks);
-        if (words) {
-            v[0] = reinterpret_cast<const uint32_t*>(p)[0];
-            if (n > 4) v[1] = reinterpret_cast<const uint32_t*>(p)[1];
+        if (n == kStepBlocks) {
+            __builtin_memcpy(v, p, 8);      // of any alignment
         } else {
 #pragma unroll
             for (int i = 0; i < kStepBlocks; ++i)
@@ -487,48 +481,44 @@ __global__ __launch_bounds__(WM * WN * kWave) void mx4_stream_kernel(Mx4LinearDe
     write_tile<T, EPI, MI, NI>(g, m0 + wm, n0 + wn, split, acc, smem, wave, lane);
 }
 
-// Few rows: 16 columns of the output and MI x 16 rows per workgroup; every wave has 256-element steps of its own (step
-// wave + waves i) and loads its fragments from global memory, the weights' rows once in all; the waves' sums meet in LDS.
-template <typename T, int EPI, int MI>
+// Few rows: 16 x 16 outputs per workgroup of up to 16 waves; every wave has 256-element steps of its own (step wave +
+// waves i) and loads its fragments from global memory, so that the weights' rows are on their way at once; the waves'
+// sums meet in LDS. Bound by latency: one row of 3456 x 1152 3.9 us, of 4096 x 16384 13 us (34 MB of weights, 2.7 TB/s).
+template <typename T, int EPI>
 __global__ __launch_bounds__(1024) void mx4_rows_kernel(Mx4LinearDesc d) {
     constexpr int OLD = 20;
-    __shared__ __attribute__((aligned(16))) float smem[16 * MI * 16 * OLD];
+    __shared__ __attribute__((aligned(16))) float smem[16 * 16 * OLD];
     const GemmDesc& g = d.g;
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), waves = blockDim.x / kWave;
     const int grp = lane / 16, l16 = lane % 16;
     const int nt = (g.N + 15) / 16;
-    const int n0 = (int)(blockIdx.x % nt) * 16, m0 = (int)(blockIdx.x / nt) * MI * 16;
+    const int n0 = (int)(blockIdx.x % nt) * 16, m0 = (int)(blockIdx.x / nt) * 16;
     const uint32_t rowb = (uint32_t)g.K / 2;
     const int blocks = g.K / kMxBlock, steps = (g.K + kStep - 1) / kStep;
-    const int rows_a = min(MI * 16, g.M - m0), rows_w = min(16, g.N - n0);
+    const int rows_a = min(16, g.M - m0), rows_w = min(16, g.N - n0);
     const __amdgpu_buffer_rsrc_t ra = make_rsrc(d.a + (long)m0 * rowb, (uint32_t)rows_a * rowb), rw = make_rsrc(d.w + (long)n0 * rowb, (uint32_t)rows_w * rowb);
     const __amdgpu_buffer_rsrc_t qa = make_rsrc(d.as + (long)m0 * blocks, (uint32_t)(rows_a * blocks)), qw = make_rsrc(d.ws + (long)n0 * blocks, (uint32_t)(rows_w * blocks));
-    f32x4_t acc[MI];
-#pragma unroll
-    for (int j = 0; j < MI; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
     struct Frag {
-        vec16 w[2], a[2][MI];
-        int sw[2], sa[2][MI];
+        vec16 w[2], a[2];
+        int sw[2], sa[2];
     };
     auto load = [&](int t, Frag& f) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int b = t * kStepBlocks + k * 4 + grp;
-            const bool in = t < steps && b < blocks;
-            f.w[k] = buf_ld16(rw, in ? (uint32_t)l16 * rowb + b * 16 : kAbsent, 0);
-            f.sw[k] = __builtin_amdgcn_raw_buffer_load_b8(qw, in ? l16 * blocks + b : (int)kAbsent, 0, 0);
-#pragma unroll
-            for (int j = 0; j < MI; ++j) {
-                f.a[k][j] = buf_ld16(ra, in ? (uint32_t)(j * 16 + l16) * rowb + b * 16 : kAbsent, 0);
-                f.sa[k][j] = __builtin_amdgcn_raw_buffer_load_b8(qa, in ? (j * 16 + l16) * blocks + b : (int)kAbsent, 0, 0);
-            }
+            const bool in = t < steps && b < blocks;        // else zeros
+            const uint32_t at = in ? (uint32_t)l16 * rowb + b * 16 : kAbsent;
+            const int sat = in ? l16 * blocks + b : (int)kAbsent;
+            f.w[k] = buf_ld16(rw, at, 0);
+            f.a[k] = buf_ld16(ra, at, 0);
+            f.sw[k] = __builtin_amdgcn_raw_buffer_load_b8(qw, sat, 0, 0);
+            f.sa[k] = __builtin_amdgcn_raw_buffer_load_b8(qa, sat, 0, 0);
         }
     };
     auto multiply = [&](const Frag& f) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int j = 0; j < MI; ++j) acc[j] = mfma_mx4<0, 0>(f.w[k], f.a[k][j], acc[j], f.sw[k], f.sa[k][j]);
+        for (int k = 0; k < 2; ++k) acc = mfma_mx4<0, 0>(f.w[k], f.a[k], acc, f.sw[k], f.sa[k]);
     };
     Frag f0, f1;
     load(wave, f0);
@@ -538,60 +528,37 @@ __global__ __launch_bounds__(1024) void mx4_rows_kernel(Mx4LinearDesc d) {
         load(t + 2 * waves, f0);
         multiply(f1);
     }
-#pragma unroll
-    for (int j = 0; j < MI; ++j) {
-        const float v[4] = {acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
-        store4<float>(smem + ((wave * MI + j) * 16 + l16) * OLD + grp * 4, v);
-    }
+    const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+    store4<float>(smem + (wave * 16 + l16) * OLD + grp * 4, v);
     __syncthreads();
-    for (int i = tid; i < MI * 64; i += blockDim.x) {       // a thread per row and four columns
-        const int row = i / 4, n = n0 + i % 4 * 4, m = m0 + row;
-        if (m >= g.M || n >= g.N) continue;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int w = 0; w < waves; ++w) {
-            float p[4];
-            load4<float>(smem + ((w * MI) * 16 + row) * OLD + i % 4 * 4, p);
+    if (tid < 64) {         // a thread per row and four columns
+        const int row = tid / 4, n = n0 + tid % 4 * 4, m = m0 + row;
+        if (m < g.M && n < g.N) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int w = 0; w < waves; ++w) {
+                float p[4];
+                load4<float>(smem + (w * 16 + row) * OLD + tid % 4 * 4, p);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] += p[r];
+                for (int r = 0; r < 4; ++r) v[r] += p[r];
+            }
+            finish<T, EPI>(g, m, n, v);
         }
-        finish<T, EPI>(g, m, n, 0, v);
     }
 }
 
 template <typename T, int EPI>
 hipError_t launch(const Mx4LinearDesc& d, hipStream_t s) {
     const GemmDesc& g = d.g;
-#define MS_TILE(form_, BM, BN, WM, WN)                                                                                            \
-    case form_:                                                                                                                   \
-        hipLaunchKernelGGL((mx4_linear_kernel<T, EPI, BM, BN, WM, WN>),                                                           \
-                           dim3((unsigned)(((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN) * g.ksplit)), dim3(WM * WN * kWave), 0, s, d); \
-        break;
-#define MS_STREAM(form_, BM, BN, WM, WN)                                                                                       \
-    case form_:                                                                                                                   \
-        hipLaunchKernelGGL((mx4_stream_kernel<T, EPI, BM, BN, WM, WN>),                                                        \
-                           dim3((unsigned)(((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN) * g.ksplit)), dim3(WM * WN * kWave), 0, s, d); \
-        break;
-#define MS_ROWS(form_, MI)                                                                                                        \
-    case form_:                                                                                                                   \
-        hipLaunchKernelGGL((mx4_rows_kernel<T, EPI, MI>), dim3((unsigned)(((g.N + 15) / 16) * ((g.M + MI * 16 - 1) / (MI * 16)))),   \
-                           dim3(d.waves * kWave), 0, s, d);                                                                       \
-        break;
+    auto tiles = [&](int bm, int bn) { return dim3((unsigned)((long)((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn) * g.ksplit)); };
     switch (d.form) {
-        MS_ROWS(kMx4Rows16, 1)
-        MS_ROWS(kMx4Rows32, 2)
-        MS_ROWS(kMx4Rows64, 4)
-        MS_TILE(kMx4Tile64, 64, 64, 2, 2)
-        MS_TILE(kMx4Tile128, 128, 128, 2, 2)
-        MS_TILE(kMx4Tile256, 256, 256, 4, 2)
-        MS_STREAM(6, 64, 64, 2, 2)
-        MS_STREAM(7, 128, 128, 2, 2)
-        MS_STREAM(8, 256, 256, 4, 2)
-        MS_STREAM(9, 256, 128, 4, 2)
-        MS_STREAM(10, 64, 128, 2, 2)
+        case kMx4Rows: hipLaunchKernelGGL((mx4_rows_kernel<T, EPI>), tiles(16, 16), dim3(d.waves * kWave), 0, s, d); break;
+        case kMx4Any64: hipLaunchKernelGGL((mx4_linear_kernel<T, EPI, 64, 64, 2, 2>), tiles(64, 64), dim3(256), 0, s, d); break;
+        case kMx4Any256: hipLaunchKernelGGL((mx4_linear_kernel<T, EPI, 256, 256, 4, 2>), tiles(256, 256), dim3(512), 0, s, d); break;
+        case kMx4Stream64: hipLaunchKernelGGL((mx4_stream_kernel<T, EPI, 64, 64, 2, 2>), tiles(64, 64), dim3(256), 0, s, d); break;
+        case kMx4Stream128: hipLaunchKernelGGL((mx4_stream_kernel<T, EPI, 128, 128, 2, 2>), tiles(128, 128), dim3(256), 0, s, d); break;
+        case kMx4Stream256: hipLaunchKernelGGL((mx4_stream_kernel<T, EPI, 256, 256, 4, 2>), tiles(256, 256), dim3(512), 0, s, d); break;
         default: return hipErrorInvalidValue;
     }
-#undef MS_TILE
-#undef MS_ROWS
     return hipGetLastError();
 }
 
@@ -605,24 +572,59 @@ hipError_t launch(const Mx4LinearDesc& d, hipStream_t s) {
     }
 }
 
-int tile_side(int form) { return form == kMx4Tile64 ? 64 : form == kMx4Tile128 ? 128 : 256; }
-
 }  // namespace
 
+// Form and K split: the least modelled time. A form with tiles of its side takes, with k workgroups on the fullest of 256
+// CUs (at most as many as fit) and `full` of the CUs busy, in us
+//   a + rounds (steps (s0 + s1 k + s2 full) + o0 + o1 k)
+// for `steps` of 256 columns in its K range, and a K split 2.3 + 1.36e-6 per range and output more. The form for few
+// rows takes its steps in up to 16 waves at once. Fitted to 9600 measured times (17 widths and depths, 128 to 16384, by 20 row counts,
+// 1 to 8192, each form, 1 to 32 ranges); the chosen pair takes 1.017 times the fastest on average, 1.40 times at most. In
+// us, rows / 64 / 128 / 256: 16 x 1152 x 1152 4.0 / 5.7 / 8.3 / 15, 410 x 4608 x 1152 31 / 7.4 / 9.4 / 16, 1024 x 16384 x 4096
+// - / 69 / 51 / 42, 8192 x 4096 x 16384 - / 510 / 328 / 267; 64 x 4096 x 16384 in 1 / 2 / 4 / 8 / 16 ranges 34 / 22 / 16 / 15 / 18.
 void plan_mx4_linear(Mx4LinearDesc& d, size_t part_floats) {
     GemmDesc& g = d.g;
     const int steps = (g.K + kStep - 1) / kStep;
-    auto tiles = [&](int side) { return (long)((g.M + side - 1) / side) * ((g.N + side - 1) / side); };
-    if (const char* v = std::getenv("MS_MX4_FORM")) d.form = std::atoi(v);
-    else d.form = g.M <= 16 ? kMx4Rows16 : g.M <= 32 ? kMx4Rows32 : g.M <= 64 ? kMx4Rows64 : tiles(256) >= 256 ? kMx4Tile256 : tiles(128) >= 256 ? kMx4Tile128 : kMx4Tile64;
+    d.form = kMx4Rows;
     d.waves = std::min(16, steps);
     g.ksplit = 1;
     g.kchunk = steps;
     g.group_m = 4;
-    if (const char* v = std::getenv("MS_MX4_SPLIT")) {
-        g.ksplit = d.form < 3 ? 1 : std::max(1, std::min<int>(std::min<long>(std::atoi(v), steps), (long)std::min<size_t>(1000, part_floats / ((size_t)g.M * g.N))));
-        g.kchunk = (steps + g.ksplit - 1) / g.ksplit;
-        g.ksplit = (steps + g.kchunk - 1) / g.kchunk;
+    if (g.M == 0) return;
+    struct Form {
+        int form, side, most;
+        double a, s0, s1, s2, o0, o1;
+    };
+    static const Form forms[] = {{kMx4Any64, 64, 4, 3.2, 0.39, 0.16, 0.16, 0.0, 0.45},      {kMx4Any256, 256, 1, 5.1, 0.71, 1.14, 1.03, 1.25, 0.66},
+                                 {kMx4Stream64, 64, 4, 3.8, 0.26, 0.13, 0.08, 0.0, 0.56},   {kMx4Stream128, 128, 2, 4.0, 0.47, 0.22, 0.2, 0.0, 1.71},
+                                 {kMx4Stream256, 256, 1, 2.4, 0.83, 0.63, 0.45, 1.1, 5.1}};
+    const bool stream = g.K % 128 == 0 && ((reinterpret_cast<uintptr_t>(d.as) | reinterpret_cast<uintptr_t>(d.ws)) & 3) == 0;
+    const double mn = (double)g.M * g.N;
+    double least = 1e30;
+    if (g.M <= 256) {
+        const double tiles = (double)((g.M + 15) / 16) * ((g.N + 15) / 16);
+        least = 2.2 + 1.25 * ((steps + d.waves - 1) / d.waves) + 2.36e-6 * tiles * g.K + 0.085 * std::ceil(tiles / 256) * d.waves + 0.53e-6 * g.M * g.K;
+    }
+    for (const Form& f : forms) {
+        if ((f.form >= kMx4Stream64) != stream) continue;
+        const long tiles = (long)((g.M + f.side - 1) / f.side) * ((g.N + f.side - 1) / f.side);
+        int before = 0;
+        for (int want : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            const int chunk = (steps + want - 1) / want, n = (steps + chunk - 1) / chunk;
+            if (n == before || want > steps) continue;
+            before = n;
+            if (n > 1 && ((size_t)n > part_floats / ((size_t)g.M * g.N) || tiles * n >= (1l << 22))) break;
+            const double q = std::ceil(tiles * n / 256.0), k = std::min(q, (double)f.most), rounds = std::max(1.0, q / f.most);
+            const double full = std::min(1.0, tiles * n / 256.0);
+            double us = f.a + rounds * (chunk * (f.s0 + f.s1 * k + f.s2 * full) + f.o0 + f.o1 * k);
+            if (n > 1) us += 2.3 + 1.36e-6 * n * mn;
+            if (us < least) {
+                least = us;
+                d.form = f.form;
+                g.ksplit = n;
+                g.kchunk = chunk;
+            }
+        }
     }
 }
 
