@@ -6,8 +6,8 @@
 //
 // Bound by the rows' bytes, in and out once. hd / VEC lanes of 16 bytes have a head,
 // as many heads side by side as a wave holds, and walk over the row's heads: their
-// columns stay the same, so gains and (cos, sin) are loaded once per row and live in
-// registers. Sums of squares, norms and rotations are float32; the result is rounded once.
+// columns stay the same, so the products of gains and (cos, sin) are formed once per row and
+// live in registers. Sums of squares, norms and rotations are float32; the result is rounded once.
 #include <algorithm>
 
 #include "kernels.h"
@@ -19,7 +19,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 
-enum { kPairs = 0, kHalves = 1 };
+// Pairs (2 p, 2 p + 1), in one lane; (p, p + rot / 2) where that is whole lanes away; or anywhere, through LDS.
+enum { kPairs = 0, kLanes = 1, kAny = 2 };
 
 template <typename T>
 __device__ __forceinline__ void load_vec(const T* p, float* v) {
@@ -49,80 +50,214 @@ __device__ __forceinline__ void store_vec(T* p, const float* v) {
 
 // One wave per (packed row, part of its heads).
 template <typename T, int PAIRING>
-__global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(QkNormRopeDesc d) {
+__global__ __launch_bounds__(kThreads, 4) void qk_norm_rope_kernel(QkNormRopeDesc d) {
     constexpr int VEC = 16 / sizeof(T);
-    const int lane = threadIdx.x % kWave;
-    const long unit = (long)blockIdx.x * kWaves + threadIdx.x / kWave;
-    const long m = unit / d.parts;
-    if (m >= d.M) return;
-    const int part = (int)(unit - m * d.parts);
+    constexpr int kAtOnce = PAIRING == kAny ? 2 : 4;        // passes whose rows are loaded before the first is used, as many as the registers hold
+    __shared__ __attribute__((aligned(16))) uint8_t smem[PAIRING == kAny ? kWaves * kAtOnce * 1024 : 16];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int lph = d.hd / VEC, side = kWave / lph;         // lanes per head, heads side by side
-    const int sub = lane / lph, at = lane - sub * lph, col = at * VEC;
-    const int heads = d.H + 2 * d.G;
-    const T* const src = static_cast<const T*>(d.qkv) + m * d.ld;
-
-    float cs[VEC], sn[VEC];
-    int other[VEC];         // column that each of this lane's columns is rotated with
-    const int pos = d.pos ? d.pos[m] : (int)m;
-    const bool turn = d.table && pos >= 0 && pos < d.n_pos;
+    const int sub = min(lane / lph, side - 1), at = min(lane - sub * lph, lph - 1), col = at * VEC;     // lanes past the last head repeat its last
+    const bool idle = lane >= side * lph;
     const int half = d.rot / 2;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
+    // passes over `side` heads of one kind: Q, K, V
+    const int nq = (d.H + side - 1) / side, nk = (d.G + side - 1) / side, passes = nq + 2 * nk;
+    const bool whole_heads = d.rot == d.hd;
+    const float per = 1.0f / (float)d.hd;
+    const bool in_rot = col < d.rot, all_in = col + VEC <= d.rot;
+    // with kLanes, the columns that this lane's are turned with and the lane that holds them
+    const int away = PAIRING == kLanes && in_rot ? (col < half ? half : -half) : 0;
+    const int from = lane + away / VEC;
+    auto partner = [&](int e) {         // the column that column col + e, below rot, is turned with
         const int c = col + e;
-        const bool first = PAIRING == kPairs ? (c & 1) == 0 : c < half;
-        const int pair = PAIRING == kPairs ? c >> 1 : first ? c : c - half;
-        other[e] = PAIRING == kPairs ? c ^ 1 : first ? c + half : c - half;
-        cs[e] = 1.f;
-        sn[e] = 0.f;
-        if (turn && c < d.rot) {
-            const float2 t = *reinterpret_cast<const float2*>(d.table + ((long)pos * half + pair) * 2);
-            cs[e] = t.x;
-            sn[e] = first ? -t.y : t.y;
+        return PAIRING == kPairs ? c ^ 1 : c < half ? c + half : c - half;
+    };
+    // gains of this lane's columns and of those they are turned with, as they lie
+    vec16 ga[2], gb[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const T* const gain = static_cast<const T*>(k ? d.k_gain : d.q_gain);
+        const uint32_t one = sizeof(T) == 2 ? 0x3f803f80u : 0x3f800000u;
+        ga[k] = gb[k] = vec16{{one, one, one, one}};
+        if (!gain) continue;
+        ga[k] = ld16(gain + col);
+        if constexpr (PAIRING == kLanes) {
+            gb[k] = ld16(gain + col + away);
         } else {
-            other[e] = c;
+            T x[VEC];
+            __builtin_memcpy(x, &ga[k], 16);
+            T y[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) y[e] = PAIRING == kPairs ? x[e ^ 1] : gain[col + e < d.rot ? partner(e) : 0];
+            __builtin_memcpy(&gb[k], y, 16);
         }
     }
-    const int row = d.rows ? d.rows[m] : (int)m;
-    const bool keep = row >= 0 && row < d.kv_rows;
-    T* const q = static_cast<T*>(d.q) + m * d.H * d.hd;
-    T* const kv = static_cast<T*>(d.kv) + (long)(keep ? row : 0) * 2 * d.G * d.hd;
-    // the heads of one pass share their lanes' columns; a head past the last is loaded as head 0 and not written
-    for (int h0 = part * side; h0 < heads; h0 += d.parts * side) {
-        const int h = h0 + sub;
-        const bool mine = sub < side && h < heads;
-        const bool is_q = h < d.H, is_v = h >= d.H + d.G;
-        const T* const x = src + (mine ? h : 0) * d.hd;
-        const int c0 = sub < side ? col : 0;
-        const vec16 raw = ld16(x + c0);
-        float v[VEC], y[VEC];
-        load_vec<T>(reinterpret_cast<const T*>(&raw), v);
-        float ss = 0.f;
+
+    const long units = (long)d.M * d.parts;
+    for (long unit = (long)blockIdx.x * kWaves + wave; unit < units; unit += (long)gridDim.x * kWaves) {
+        const long m = d.parts == 1 ? unit : unit / d.parts;
+        const int p0 = (int)(unit - m * d.parts);
+        const T* const src = static_cast<const T*>(d.qkv) + m * d.ld;
+        vec16 raw[kAtOnce];
+        int kind[kAtOnce], head[kAtOnce];       // 0 Q, 1 K, 2 V, 3 past the last pass; this lane's head of that kind
+        auto fetch = [&](int first) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) ss = fmaf(v[e], v[e], ss);
-        for (int o = 1; o < lph; o <<= 1) {     // sums of what lies behind within the head; the first lane has them all
-            const float t = __shfl_down(ss, o, kWave);
-            if (at + o < lph) ss += t;
-        }
-        ss = __shfl(ss, min(lane - at, kWave - 1), kWave);
-        const T* const gain = static_cast<const T*>(is_q ? d.q_gain : d.k_gain);
-        const float inv = gain ? 1.0f / sqrtf(ss / (float)d.hd + d.eps) : 1.0f;
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int p = first + u * d.parts;
+                kind[u] = p < nq ? 0 : p < nq + nk ? 1 : p < passes ? 2 : 3;
+                head[u] = (kind[u] == 0 ? p : kind[u] == 1 ? p - nq : p - nq - nk) * side + sub;
+                const int n = kind[u] == 0 ? d.H : d.G, before = kind[u] == 0 ? 0 : kind[u] == 1 ? d.H : d.H + d.G;
+                raw[u] = ld16(src + (kind[u] == 3 ? 0 : before + min(head[u], n - 1)) * d.hd + col);   // past the last head: not written
+            }
+        };
+        const int pos = d.pos ? d.pos[m] : (int)m;
+        const int row = d.rows ? d.rows[m] : (int)m;
+        fetch(p0);
+        // y_c = (x_c fc + x_c' fs) / rms: gain and cos of column c, gain of the column c' that it is turned with and signed sin
+        const bool turn = d.table && pos >= 0 && pos < d.n_pos;
+        float cs[VEC], sn[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const int oc = sub < side ? other[e] : 0;
-            const float p = PAIRING == kPairs ? (oc == col + e ? v[e] : v[e ^ 1]) : Elt<T>::to_f32(x[oc]);
-            const float ga = gain ? Elt<T>::to_f32(gain[c0 + e]) : 1.f, gb = gain ? Elt<T>::to_f32(gain[oc]) : 1.f;
-            const float a = v[e] * inv * ga, b = p * inv * gb;
-            y[e] = sn[e] == 0.f && oc == c0 + e ? a : fmaf(a, cs[e], b * sn[e]);
+            cs[e] = 1.f;
+            sn[e] = 0.f;
         }
-        if (!mine) continue;
-        if (is_q) {
-            store_vec<T>(q + h * d.hd + col, y);
-        } else if (keep) {
-            T* const to = kv + (h - d.H) * d.hd + col;      // K heads, then V heads
-            if (is_v) st16(to, raw);
-            else store_vec<T>(to, y);
+        if (turn && in_rot) {
+            const float* const t = d.table + (long)pos * half * 2;
+            if (PAIRING == kPairs && all_in && half % 2 == 0) {
+#pragma unroll
+                for (int e = 0; e < VEC; e += 4) {
+                    const float4 v = *reinterpret_cast<const float4*>(t + col + e);
+                    cs[e] = cs[e + 1] = v.x;
+                    sn[e] = -v.y;
+                    sn[e + 1] = v.y;
+                    cs[e + 2] = cs[e + 3] = v.z;
+                    sn[e + 2] = -v.w;
+                    sn[e + 3] = v.w;
+                }
+            } else if (PAIRING == kLanes) {
+                const float* const p = t + (col < half ? col : col - half) * 2;
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) {
+                    const float4 v = *reinterpret_cast<const float4*>(p + 2 * e);
+                    cs[e] = v.x;
+                    sn[e] = col < half ? -v.y : v.y;
+                    cs[e + 1] = v.z;
+                    sn[e + 1] = col < half ? -v.w : v.w;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int c = col + e;
+                    if (c >= d.rot) continue;
+                    const bool first = PAIRING == kPairs ? (c & 1) == 0 : c < half;
+                    const int pair = PAIRING == kPairs ? c >> 1 : first ? c : c - half;
+                    const float2 v = *reinterpret_cast<const float2*>(t + pair * 2);
+                    cs[e] = v.x;
+                    sn[e] = first ? -v.y : v.y;
+                }
+            }
+        }
+        float fc[2][VEC], fs[2][VEC];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float x[VEC], y[VEC];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) asm volatile("" : "+v"(ga[k].w[w]), "+v"(gb[k].w[w]));     // not unpacked before the loop
+            load_vec<T>(reinterpret_cast<const T*>(&ga[k]), x);
+            load_vec<T>(reinterpret_cast<const T*>(&gb[k]), y);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                fc[k][e] = x[e] * cs[e];
+                fs[k][e] = y[e] * sn[e];
+            }
+        }
+        const bool keep = row >= 0 && row < d.kv_rows;
+        T* const q = static_cast<T*>(d.q) + m * d.H * d.hd;
+        T* const kv = static_cast<T*>(d.kv) + (long)(keep ? row : 0) * 2 * d.G * d.hd;
+
+        for (int first = p0;;) {
+            if constexpr (PAIRING == kAny) {
+                asm volatile("" ::: "memory");      // LDS operations of a wave are done in order
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+                    if (!idle) st16(smem + (wave * kAtOnce + u) * 1024 + lane * 16, raw[u]);     // a head's rows lie in order
+                asm volatile("" ::: "memory");
+            }
+            float ss[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                float v[VEC];
+                load_vec<T>(reinterpret_cast<const T*>(&raw[u]), v);
+                ss[u] = 0.f;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) ss[u] = fmaf(v[e], v[e], ss[u]);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) asm volatile("" : "+v"(raw[u].w[w]));      // unpacked again below, not kept
+            }
+            for (int o = 1; o < lph; o <<= 1) {     // sums of what lies behind within the head; the first lane has them all
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const float t = __shfl_down(ss[u], o, kWave);
+                    if (at + o < lph) ss[u] += t;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) ss[u] = __shfl(ss[u], sub * lph, kWave);
+            auto turned = [&](int u, const float (&fc_)[VEC], const float (&fs_)[VEC], bool norm) {
+                float v[VEC], p[VEC], y[VEC];
+                load_vec<T>(reinterpret_cast<const T*>(&raw[u]), v);
+                if constexpr (PAIRING == kPairs) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) p[e] = v[e ^ 1];
+                } else if constexpr (PAIRING == kLanes) {
+                    vec16 o;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) o.w[k] = (uint32_t)__shfl((int)raw[u].w[k], from, kWave);
+                    load_vec<T>(reinterpret_cast<const T*>(&o), p);
+                } else {
+                    const T* const x = reinterpret_cast<const T*>(smem + (wave * kAtOnce + u) * 1024) + sub * d.hd;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) p[e] = Elt<T>::to_f32(x[col + e < d.rot ? partner(e) : 0]);
+                }
+                const float inv = norm ? __builtin_amdgcn_rsqf(fmaf(ss[u], per, d.eps)) : 1.0f;
+                if (turn && whole_heads) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) y[e] = fmaf(p[e], fs_[e], v[e] * fc_[e]) * inv;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float x = v[e] * fc_[e];
+                        y[e] = (turn && col + e < d.rot ? fmaf(p[e], fs_[e], x) : x) * inv;     // not 0 times an infinity
+                    }
+                }
+                vec16 o;
+                store_vec<T>(reinterpret_cast<T*>(&o), y);
+                return o;
+            };
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                if (kind[u] == 0) {
+                    const vec16 y = turned(u, fc[0], fs[0], d.q_gain != nullptr);
+                    if (!idle && head[u] < d.H) st16(q + head[u] * d.hd + col, y);
+                } else if (kind[u] == 1) {
+                    const vec16 y = turned(u, fc[1], fs[1], d.k_gain != nullptr);
+                    if (!idle && head[u] < d.G && keep) st16(kv + head[u] * d.hd + col, y);
+                } else if (kind[u] == 2) {
+                    if (!idle && head[u] < d.G && keep) st16(kv + (d.G + head[u]) * d.hd + col, raw[u]);
+                }
+            }
+            first += kAtOnce * d.parts;
+            if (first >= passes) break;
+            fetch(first);
         }
     }
+}
+
+template <typename T>
+void launch(const QkNormRopeDesc& d, dim3 grid, hipStream_t s) {
+    const dim3 block(kThreads);
+    if (!d.halves) hipLaunchKernelGGL((qk_norm_rope_kernel<T, kPairs>), grid, block, 0, s, d);
+    else if (d.rot / 2 % (16 / sizeof(T)) == 0) hipLaunchKernelGGL((qk_norm_rope_kernel<T, kLanes>), grid, block, 0, s, d);
+    else hipLaunchKernelGGL((qk_norm_rope_kernel<T, kAny>), grid, block, 0, s, d);
 }
 
 }  // namespace
@@ -131,17 +266,13 @@ hipError_t launch_qk_norm_rope(int dtype, const QkNormRopeDesc& desc, hipStream_
     if (desc.M == 0) return hipSuccess;
     QkNormRopeDesc d = desc;
     const int vec = dtype == kBF16 ? 8 : 4, side = kWave / (d.hd / vec);
-    const int passes = (d.H + 2 * d.G + side - 1) / side;
+    const int passes = (d.H + side - 1) / side + 2 * ((d.G + side - 1) / side);
     // few rows: their heads spread over more waves
-    d.parts = (int)std::max(1l, std::min<long>(passes, 2048 / std::max(1, d.M)));
-    const dim3 grid((unsigned)(((long)d.M * d.parts + kWaves - 1) / kWaves)), block(kThreads);
-    if (dtype == kBF16) {
-        if (d.halves) hipLaunchKernelGGL((qk_norm_rope_kernel<bf16_t, kHalves>), grid, block, 0, s, d);
-        else hipLaunchKernelGGL((qk_norm_rope_kernel<bf16_t, kPairs>), grid, block, 0, s, d);
-    } else {
-        if (d.halves) hipLaunchKernelGGL((qk_norm_rope_kernel<float, kHalves>), grid, block, 0, s, d);
-        else hipLaunchKernelGGL((qk_norm_rope_kernel<float, kPairs>), grid, block, 0, s, d);
-    }
+    d.parts = (int)std::max(1l, std::min<long>(passes, 4096 / std::max(1, d.M)));
+    // as many waves as the CUs hold take the rows in turn
+    const dim3 grid((unsigned)std::min<long>(((long)d.M * d.parts + kWaves - 1) / kWaves, 256 * 4));
+    if (dtype == kBF16) launch<bf16_t>(d, grid, s);
+    else launch<float>(d, grid, s);
     return hipGetLastError();
 }
 
