@@ -23,6 +23,7 @@
 // wave at a slot (recompute). Finite inputs never come there.
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <type_traits>
 
 #include "attn_tiles.h"
@@ -47,7 +48,8 @@ struct Work {
     int split;
     int t0, t1;     // key tiles: those of the prefix, then the own ones
     int ntp;        // prefix tiles
-    int f0, f1;     // own rows of the tile's requests
+    int first, last;    // requests of the tile
+    int f0, f1;     // their own rows
 };
 
 // The tables of a workgroup's requests in LDS: where each one's rows start, and its own rows.
@@ -88,10 +90,10 @@ __device__ __forceinline__ bool find_work(const SharedAttnDesc& a, int tile, int
     w.kvh = kvh;
     w.split = split;
     if (w.q0 >= w.slots) return false;
-    const int first = request_of(a, t, w.row0 + w.q0 / a.group);
-    const int last = request_of(a, t, w.row0 + (min(w.q0 + QT, w.slots) - 1) / a.group);
-    w.f0 = uniform(t.own[first]);
-    w.f1 = max(uniform(t.own[last + 1]), w.f0);
+    w.first = uniform(request_of(a, t, w.row0 + w.q0 / a.group));
+    w.last = uniform(request_of(a, t, w.row0 + (min(w.q0 + QT, w.slots) - 1) / a.group));
+    w.f0 = uniform(t.own[w.first]);
+    w.f1 = max(uniform(t.own[w.last + 1]), w.f0);
     w.ntp = (a.T + KT - 1) / KT;
     const uint32_t nt = w.ntp + (w.f1 - w.f0 + KT - 1) / KT;    // below 2^24; times 64 ranges below 2^32
     w.t0 = uniform((int)(nt * split / a.nsplit));
@@ -103,6 +105,12 @@ __device__ __forceinline__ bool find_work(const SharedAttnDesc& a, int tile, int
 template <int KT>
 __device__ __forceinline__ uint64_t below(int n) {
     return n >= KT ? (KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1) : n <= 0 ? 0ull : (1ull << n) - 1;
+}
+
+// x where bit `at` of w is set, else -infinity, without a condition register per score.
+__device__ __forceinline__ float seen_or_none(uint32_t w, int at, float x) {
+    const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)w, at, 1);
+    return __uint_as_float((__float_as_uint(x) & m) | (0xff800000u & ~m));
 }
 
 // Which keys of the tiles one slot sees.
@@ -235,44 +243,79 @@ __device__ __forceinline__ void join_waves(const SharedAttnDesc& a, const Work& 
     if (!fine) atomicOr(bad, 1u << (first + s));
 }
 
-// Tiles of KT K rows and V rows by direct-to-LDS loads of NW waves, [K rows][V rows][zeros].
+// Tiles of KT K rows and as many V rows by direct-to-LDS loads of NW waves, K and V apart.
 template <int HD, int KT, int NW>
 struct Tiles {
     static constexpr int ROWB = HD * 2, TILEB = KT * ROWB, PAD = 64;
-    static constexpr int STAGEB = 2 * TILEB + PAD;
-    static constexpr int NQ = 2 * TILEB / 1024;             // 1 KB copies per tile
+    static constexpr int NQ = (TILEB + 1023) / 1024;        // 1 KB copies of the K or V rows, the last may be half of one
     static constexpr int IPW = (NQ + NW - 1) / NW;          // per wave, most
-    static_assert(2 * TILEB % 1024 == 0, "tile copies");
+    static constexpr int PARTB = TILEB;
+    static_assert(TILEB % 512 == 0, "tile copies");
     static constexpr bool SWZ = ROWB == 128 || ROWB == 256 || ROWB % 128 == 64;
     static constexpr uint32_t kAbsent = 0xfff00000u;
-    u32x4_t rsrc;
-    uint32_t row_bytes, voff[IPW];
-    int rl[IPW], end;
+    uint32_t row_bytes, vk[IPW], vv[IPW];
+    int rl[IPW];
 
-    // rows [0, rows) of kv
-    __device__ __forceinline__ void init(const void* kv, int rows, int heads, int kvh, int wave, int lane) {
+    __device__ __forceinline__ void init(int heads, int kvh, int wave, int lane) {
         row_bytes = 4u * heads * HD;
-        rsrc = raw_rsrc(kv, (uint32_t)rows * row_bytes);
-        end = rows;
 #pragma unroll
         for (int i = 0; i < IPW; ++i) {
-            const int pos = min(i * NW + wave, NQ - 1) * 1024 + lane * 16;
-            const bool isv = pos >= TILEB;
-            const int p = isv ? pos - TILEB : pos, r = p / ROWB;
+            const int pos = min(i * NW + wave, NQ - 1) * 1024 + lane * 16, r = pos / ROWB;
             rl[i] = r;
-            voff[i] = (uint32_t)r * row_bytes + (isv ? row_bytes / 2 : 0u) + kvh * ROWB +
-                      (((p % ROWB) / 16) ^ (isv ? v_swz<ROWB>(r) : k_swz<ROWB>(r))) * 16;
+            const uint32_t row = (uint32_t)r * row_bytes + kvh * ROWB, c = pos % ROWB / 16;
+            vk[i] = row + (c ^ k_swz<ROWB>(r)) * 16;
+            vv[i] = row + row_bytes / 2 + (c ^ v_swz<ROWB>(r)) * 16;
         }
     }
-    // rows k0 on into the stage at LDS address `lds`; rows past the last read as zeros
-    __device__ __forceinline__ void issue(int k0, int wave, uint32_t lds) {
+    // K (or V) rows k0 on, of `end` in all, to LDS address `lds`; rows past the last read as zeros
+    __device__ __forceinline__ void issue(u32x4_t rsrc, const uint32_t (&off)[IPW], int k0, int end, int wave, uint32_t lds) {
         const uint32_t base = (uint32_t)k0 * row_bytes;
         const bool whole = k0 + KT <= end;
 #pragma unroll
         for (int i = 0; i < IPW; ++i) {
-            const uint32_t o = whole || k0 + rl[i] < end ? voff[i] + base : kAbsent;
-            if (NQ % NW == 0 || i * NW + wave < NQ) dma_buf16(rsrc, o, 0, lds + (uint32_t)(i * NW + wave) * 1024u);
+            const uint32_t o = whole || k0 + rl[i] < end ? off[i] + base : kAbsent;
+            const int q = i * NW + wave;
+            if (NQ % NW != 0 && q >= NQ) continue;
+            if (TILEB % 1024 != 0 && q == NQ - 1) {
+                if (threadIdx.x % kWave < 32) dma_buf16(rsrc, o, 0, lds + (uint32_t)q * 1024u);     // half a copy
+            } else {
+                dma_buf16(rsrc, o, 0, lds + (uint32_t)q * 1024u);
+            }
         }
+    }
+};
+
+// The prefix tiles of 64 tokens that some request of the workgroup sees, 64 tiles at a time: every wave finds the same.
+struct Live {
+    uint64_t seen;
+    int base, to;
+    bool some;      // whether tiles are left out at all
+    __device__ __forceinline__ void look(const SharedAttnDesc& a, const Work& w, int lane) {
+        const int t = base + lane;
+        uint64_t hidden = ~0ull;
+        for (int b = w.first; b <= w.last; ++b) hidden &= a.bits[(long)b * a.words + min(t, a.words - 1)];
+        seen = __ballot(t < to && hidden != ~0ull);
+    }
+    // of tiles [from, to); a few tiles, or those of many requests, are all taken
+    __device__ __forceinline__ void init(const SharedAttnDesc& a, const Work& w, int lane, int from, int end) {
+        base = from;
+        to = end;
+        some = a.bits && end - from >= 8 && w.last >= w.first && w.last - w.first < 8;
+        if (some) look(a, w, lane);
+    }
+    // the first tile from t on, `to` where there is none
+    __device__ __forceinline__ int next(const SharedAttnDesc& a, const Work& w, int lane, int t) {
+        if (!some) return t;
+        while (t < to) {
+            if (t >= base + kWave) {
+                base = t;
+                look(a, w, lane);
+            }
+            const uint64_t m = seen >> (t - base);
+            if (m) return t + __builtin_ctzll(m);
+            t = base + kWave;
+        }
+        return to;
     }
 };
 
@@ -292,12 +335,14 @@ struct Cfg {
     static constexpr int NHS = NREAL + (SUM_IN_PAD ? 0 : 1);
     static constexpr int OLD = HD + 4;
     static constexpr int STAGES = 2;
-    static constexpr int TILES = (WIDE ? STAGES : 4 * STAGES) * S::STAGEB;
+    static constexpr int V0 = STAGES * S::PARTB;            // a wave's (or the workgroup's) stages: K parts, then V parts, then zeros
+    static constexpr int ZERO = 2 * STAGES * S::PARTB, RINGB = ZERO + S::PAD;
+    static constexpr int TILES = (WIDE ? 1 : 4) * RINGB;
     static constexpr int JOIN = WIDE ? 4 * 32 * 2 * S::ROWB : (4 * 16 * OLD + 4 * 16 * 2) * 4;
     static constexpr int LDSB = ((TILES > JOIN ? TILES : JOIN) + 63) / 64 * 64;
 };
 
-constexpr int wide_per_cu(int hd) { return hd <= 48 ? 4 : hd <= 64 ? 3 : 2; }
+constexpr int wide_per_cu(int hd) { return hd <= 32 ? 4 : hd <= 80 ? 3 : 2; }
 constexpr int few_per_cu(int hd) { return hd <= 32 ? 4 : hd <= 48 ? 3 : hd <= 72 ? 2 : 1; }
 
 // bf16. WIDE: 128 slots, 32 per wave; the four waves share 64-key tiles in two stages.
@@ -329,10 +374,10 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
     }
     constexpr int step = WIDE ? 1 : 4;
 
-    // constant LDS: zeros behind the tiles, the ones block
-    constexpr int NSTG = (WIDE ? 1 : 4) * C::STAGES;
-    if (tid < 4 * NSTG) *reinterpret_cast<uint4*>(smem + (tid / 4) * S::STAGEB + 2 * S::TILEB + (tid % 4) * 16) = make_uint4(0u, 0u, 0u, 0u);
-    if (tid == 4 * NSTG) *reinterpret_cast<uint2*>(smem + C::LDSB) = make_uint2(0x3f803f80u, 0x3f803f80u);
+    // constant LDS: zeros behind the rings, the ones block
+    constexpr int RINGS = WIDE ? 1 : 4;
+    if (tid < 4 * RINGS) *reinterpret_cast<uint4*>(smem + (tid / 4) * C::RINGB + C::ZERO + (tid % 4) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == 4 * RINGS) *reinterpret_cast<uint2*>(smem + C::LDSB) = make_uint2(0x3f803f80u, 0x3f803f80u);
     if (tid < QT / 32 + 1) bad[tid] = 0;
 
     // Q^T fragments (B operand), their sign that of the score scale
@@ -370,7 +415,7 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
 #pragma unroll
     for (int h = 0; h < C::NREAL; ++h) {
         const int hd = 16 * h + 4 * (l16 & 3);
-        voffh[h] = S::TILEB + rowA * S::ROWB + (((hd / 8) ^ fV) * 16) + (hd % 8) * 2;
+        voffh[h] = rowA * S::ROWB + (((hd / 8) ^ fV) * 16) + (hd % 8) * 2;
     }
     const bool ones_lane = C::SUM_IN_PAD && (16 * (C::NREAL - 1) + 4 * (l16 & 3)) >= HD;
 
@@ -391,22 +436,23 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
     const bf16x8_t onesf = __builtin_bit_cast(bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
     constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
 
-    auto qk = [&](uint32_t sbase, f32x4_t (&sacc)[NQB][NKS]) {
+    const uint32_t ring = WIDE ? 0u : (uint32_t)(wave * C::RINGB);
+    const uint32_t zero = ring + C::ZERO;
+    // K fragment (16 keys, 32 columns) of the tile at `base`
+    auto k_frag = [&](uint32_t base, int ks, int kc) {
+        uint32_t at = base + koff[kc] + ks * 16 * S::ROWB;
+        if (C::KTAIL && kc == C::NK32 - 1) at = in_row ? at : zero;
+        return *reinterpret_cast<const bf16x8_t*>(smem + at);
+    };
+    auto qk = [&](uint32_t base, f32x4_t (&sacc)[NQB][NKS]) {
 #pragma unroll
-        for (int qb = 0; qb < NQB; ++qb)
-#pragma unroll
-            for (int ks = 0; ks < NKS; ++ks) sacc[qb][ks] = negm[qb];
-#pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) {
+        for (int ks = 0; ks < NKS; ++ks)
 #pragma unroll
             for (int kc = 0; kc < C::NK32; ++kc) {
-                uint32_t at = koff[kc] + ks * 16 * S::ROWB;
-                if (C::KTAIL && kc == C::NK32 - 1) at = in_row ? at : (uint32_t)(2 * S::TILEB);
-                const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(smem + sbase + at);
+                const bf16x8_t kf = k_frag(base, ks, kc);
 #pragma unroll
-                for (int qb = 0; qb < NQB; ++qb) sacc[qb][ks] = mfma32(kf, qf[qb][kc], sacc[qb][ks]);
+                for (int qb = 0; qb < NQB; ++qb) sacc[qb][ks] = mfma32(kf, qf[qb][kc], kc == 0 ? negm[qb] : sacc[qb][ks]);
             }
-        }
     };
     // scores of keys that a slot does not see become -infinity, whatever they were
     auto hide = [&](const uint64_t (&sees)[NQB], f32x4_t (&sacc)[NQB][NKS]) {
@@ -417,16 +463,16 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb) {
             const uint64_t mine = sees[qb] >> (grp * 4);
+            const uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (!((mine >> (ks * 16 + r)) & 1)) sacc[qb][ks][r] = -INFINITY;
+                for (int r = 0; r < 4; ++r) sacc[qb][ks][r] = seen_or_none(half[ks / 2], ks % 2 * 16 + r, sacc[qb][ks][r]);
         }
     };
-    // online softmax in place: sacc becomes the weights; running maxima and accumulators
-    // updated, a rescale only where a score exceeds its slot's maximum by more than 2^8
-    auto softmax = [&](f32x4_t (&sacc)[NQB][NKS]) {
+    // online softmax: running maxima and accumulators updated, a rescale only where a score exceeds its slot's
+    // maximum by more than 2^8; after it the weights are 2^(cs score)
+    auto raise = [&](f32x4_t (&sacc)[NQB][NKS]) {
         float mx[NQB];
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb) {
@@ -461,6 +507,8 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
             }
             beyond = __any(far);
         }
+    };
+    auto weights = [&](f32x4_t (&sacc)[NQB][NKS]) {
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb)
 #pragma unroll
@@ -509,24 +557,39 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
         }
     };
 
-    f32x4_t sa[NQB][NKS];
     const bool active = wq0 < w.slots;
-    // Tiles [from, to) of one kind (tile 0 at row `base` of kv, `rows` of them from there on in all): while a tile is
-    // multiplied the next one lands in the other stage.
+    __syncthreads();   // constant LDS
+    f32x4_t sa[NQB][NKS];
+    // Tiles [from, to) of one kind (tile 0 at row `base` of kv, which has `rows`): while a tile is multiplied the next one lands.
     auto run = [&](auto OWN, const void* kv, int base, int rows, int from, int to, int skip) __attribute__((always_inline)) {
         if constexpr (!WIDE) from += (wave - skip) & 3;     // the waves go on in turn from one kind to the next
         if (from >= to) return;     // the whole workgroup, or a wave that waits for no other
+        Live live;
+        auto after = [&](int t) {
+            if constexpr (WIDE && !OWN) return live.next(a, w, lane, t);
+            else return t;
+        };
+        if constexpr (WIDE && !OWN) {
+            live.init(a, w, lane, from, to);
+            from = after(from);
+            if (from >= to) return;
+        }
         const int lw = WIDE ? wave : 0;
+        const u32x4_t rsrc = raw_rsrc(kv, (uint32_t)rows * 4u * a.heads * HD);
         S st;
-        st.init(kv, rows, a.heads, w.kvh, lw, lane);
-        auto stage = [&](int n) { return (uint32_t)((WIDE ? (n & 1) : wave * 2 + (n & 1)) * S::STAGEB); };
+        st.init(a.heads, w.kvh, lw, lane);
+        auto issue = [&](int t, int n) {
+            st.issue(rsrc, st.vk, base + t * KT, rows, lw, lds0 + ring + (n & 1) * S::PARTB);
+            st.issue(rsrc, st.vv, base + t * KT, rows, lw, lds0 + ring + C::V0 + (n & 1) * S::PARTB);
+        };
         uint64_t hidden[NQB];
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb) hidden[qb] = OWN ? 0ull : sight[qb].fetch(a, from);
-        st.issue(base + from * KT, lw, lds0 + stage(0));
+        issue(from, 0);
         int n = 0;
-        for (int t = from; t < to; t += step, ++n) {
-            wait_all();   // tile t has landed, and this wave's reads of the stage refilled below are done
+        for (int t = from, then; t < to; t = then, ++n) {
+            then = after(t + step);
+            wait_all();   // tile t has landed, and this wave's reads of the parts refilled below are done
             if constexpr (WIDE) barrier_only();
             else asm volatile("" ::: "memory");
             uint64_t sees[NQB];
@@ -535,26 +598,22 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
                 sees[qb] = OWN ? sight[qb].own(base + t * KT) : sight[qb].prefix(a, hidden[qb], t);
                 asm volatile("" : "+v"(sees[qb]));      // used before the next loads are under way
             }
-            if (t + step < to) {
+            if (then < to) {
 #pragma unroll
                 for (int qb = 0; qb < NQB; ++qb)
-                    if constexpr (!OWN) hidden[qb] = sight[qb].fetch(a, t + step);
-                st.issue(base + (t + step) * KT, lw, lds0 + stage(n + 1));
+                    if constexpr (!OWN) hidden[qb] = sight[qb].fetch(a, then);
+                issue(then, n + 1);
             }
             if (WIDE && !active) continue;
-            qk(stage(n), sa);
+            qk(ring + (n & 1) * S::PARTB, sa);
             hide(sees, sa);
-            softmax(sa);
-            pv(stage(n), sa);
+            raise(sa);
+            weights(sa);
+            pv(ring + C::V0 + (n & 1) * S::PARTB, sa);
         }
-        if constexpr (WIDE) {
-            wait_all();
-            barrier_only();   // the stages may be written again
-        } else {
-            wait_all();
-        }
+        wait_all();
+        if constexpr (WIDE) barrier_only();   // the parts may be written again
     };
-    __syncthreads();   // constant LDS
     const int c0 = min(w.t0, w.ntp), c1 = min(w.t1, w.ntp);
     run(std::false_type{}, a.kv, 0, a.T, c0, c1, 0);
     if (w.f1 > w.f0) run(std::true_type{}, a.fresh, w.f0, w.f1, max(w.t0 - w.ntp, 0), max(w.t1 - w.ntp, 0), c1 - c0);
@@ -829,12 +888,22 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedAttnDesc a)
     const float inv = L == 0.f ? 0.f : 1.0f / L;
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
     const float* const po = a.part_o + sr * hd + col * 4;
-    for (int s0 = 0; s0 < a.nsplit; s0 += groups) {
-        const int s = s0 + grp;
-        const float fs = __shfl(f, s, kWave);
-        if (grp < groups && s < a.nsplit) {
-            const float4 p = *reinterpret_cast<const float4*>(po + s * plane * hd);
-            acc[0] += fs * p.x; acc[1] += fs * p.y; acc[2] += fs * p.z; acc[3] += fs * p.w;
+    constexpr int kRounds = 8;      // rounds of loads on their way at once
+    for (int s0 = 0; s0 < a.nsplit; s0 += kRounds * groups) {
+        float4 p[kRounds];
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            const int s = s0 + i * groups + grp;
+            p[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (grp < groups && s < a.nsplit) p[i] = *reinterpret_cast<const float4*>(po + s * plane * hd);
+        }
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            const int s = s0 + i * groups + grp;
+            const float fs = __shfl(f, min(s, kWave - 1), kWave);
+            if (grp < groups && s < a.nsplit) {
+                acc[0] += fs * p[i].x; acc[1] += fs * p[i].y; acc[2] += fs * p[i].z; acc[3] += fs * p[i].w;
+            }
         }
     }
     float o[4] = {0.f, 0.f, 0.f, 0.f};
@@ -902,6 +971,8 @@ void plan_shared_attention(int dtype, SharedAttnDesc& a) {
     int n = 1;
     while (n < kSharedMaxRanges && base * n * 2 <= 512 && n * 2 <= steps && ranges_fit(a, a.tile, n * 2)) n *= 2;
     a.nsplit = n;
+    if (const char* v = std::getenv("MS_SH_TILE")) if (dtype == kBF16) a.tile = std::atoi(v);
+    if (const char* v = std::getenv("MS_SH_SPLIT")) a.nsplit = std::atoi(v);
 }
 
 hipError_t launch_shared_bits(const uint8_t* mask, int batch, int T, uint64_t* bits, hipStream_t s) {
