@@ -7,7 +7,6 @@
 namespace ms {
 
 constexpr int kSharedMaxBatch = 128;
-constexpr int kSharedMaxRanges = 64;
 
 struct SharedAttnDesc {
     const void* q;              // [M][heads * group * hd]

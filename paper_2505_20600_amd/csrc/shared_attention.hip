@@ -23,7 +23,6 @@
 // wave at a slot (recompute). Finite inputs never come there.
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 #include <type_traits>
 
 #include "attn_tiles.h"
@@ -463,7 +462,8 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb) {
             const uint64_t mine = sees[qb] >> (grp * 4);
-            const uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
+            uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
+            asm volatile("" : "+v"(half[0]), "+v"(half[1]));    // what follows stays behind the branch
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks)
 #pragma unroll
@@ -960,19 +960,49 @@ bool ranges_fit(const SharedAttnDesc& a, int tile, int n) {
 
 }  // namespace
 
+// Query slots per workgroup and key ranges: the pair with the least modelled time. A form whose workgroups take steps of
+// `keys` keys takes, with k workgroups on the fullest of 256 CUs (at most as many as fit), in us
+//   a + rounds (steps (s0 + s1 hd/64 + (s2 + s3 hd/64) k) + o0 + o1 hd/64)
+// and more than one range r0 + r1 n MB + r2 MB more, MB the size of one range's parts. A tile's own rows are taken
+// as its slots' rows and an eighth of all: the requests' number plays no part, so that a workspace is planned for the call's shapes.
+// Fitted to 4437 measured times (285 shapes: 16 to 128 columns, 1 to 24 K/V heads, groups of 1 to 8, 64 to 11000 tokens, 1 to 5700
+// rows of 1 to 32 requests, every form, 1 to 48 ranges); among powers of two the chosen pair takes 1.02 times the fastest on
+// average, 1.40 times at most. In us at the best count of ranges, 16 / 32 / 128 slots: 8 requests over 4096 tokens of 16 heads of
+// 64, one row each 11 / 13 / 17, 16 rows 21 / 19 / 24, 32 rows 31 / 25 / 30, 128 rows 94 / 54 / 50, 500 rows 390 / 237 / 133.
 void plan_shared_attention(int dtype, SharedAttnDesc& a) {
     a.tile = 16;
     a.nsplit = 1;
     if (a.M == 0) return;
+    struct Form {
+        int tile, keys;
+        double a, s0, s1, s2, s3, o0, o1, r0, r1, r2;
+    };
+    static const Form bf16[] = {{16, 128, 2.98, 0.101, 0.237, 0.208, 0.201, 2.16, 0.345, 3.21, 0.85, 1.92},
+                                {32, 128, 3.23, 0.044, 0.528, 0.378, 0.023, 2.96, 0.581, 2.92, 0.533, 2.83},
+                                {128, 64, 5.25, 0.051, 0.356, 0.563, 0.0, 1.99, 1.21, 3.4, 0.248, 2.37}};
+    static const Form f32[] = {{16, 128, 4.8, 0.236, 0.211, 0.039, 1.64, 0.0, 0.99, 3.4, 1.07, 1.0}};
     const long slots = (long)a.M * a.group;
-    if (dtype == kBF16) a.tile = slots <= 16 ? 16 : slots <= 32 ? 32 : 128;
-    const long base = (long)slot_tiles(a, a.tile) * a.heads;
-    const long steps = (a.T + 127) / 128;
-    int n = 1;
-    while (n < kSharedMaxRanges && base * n * 2 <= 512 && n * 2 <= steps && ranges_fit(a, a.tile, n * 2)) n *= 2;
-    a.nsplit = n;
-    if (const char* v = std::getenv("MS_SH_TILE")) if (dtype == kBF16) a.tile = std::atoi(v);
-    if (const char* v = std::getenv("MS_SH_SPLIT")) a.nsplit = std::atoi(v);
+    const double h = a.hd / 64.0, mb = (double)slots * a.heads * (a.hd + 2) * 4e-6;
+    double least = 1e30;
+    for (int i = 0; i < (dtype == kBF16 ? 3 : 1); ++i) {
+        const Form& f = dtype == kBF16 ? bf16[i] : f32[i];
+        // few slots: not where a larger tile is full several times over
+        if (dtype == kBF16 && f.tile < 128 && slots > 16 * f.tile + 16 * (f.tile - 16)) continue;
+        const int most = dtype != kBF16 ? 2 : f.tile == 128 ? wide_per_cu(a.hd) : few_per_cu(a.hd);
+        const long keys = a.T + std::min<long>(a.fresh_rows, a.fresh_rows / 8 + f.tile / a.group);
+        const long steps = std::max(1l, (keys + f.keys - 1) / f.keys);
+        for (int n = 1; n <= 32 && (n == 1 || (n <= (keys + 63) / 64 && ranges_fit(a, f.tile, n))); n *= 2) {
+            const double groups = (double)slot_tiles(a, f.tile) * a.heads * n;
+            const double k = std::min(std::ceil(groups / 256), (double)most), rounds = std::max(1.0, groups / (256.0 * most));
+            double us = f.a + rounds * ((steps + n - 1) / n * (f.s0 + f.s1 * h + (f.s2 + f.s3 * h) * k) + f.o0 + f.o1 * h);
+            if (n > 1) us += f.r0 + (f.r1 * n + f.r2) * mb;
+            if (us < least) {
+                least = us;
+                a.tile = f.tile;
+                a.nsplit = n;
+            }
+        }
+    }
 }
 
 hipError_t launch_shared_bits(const uint8_t* mask, int batch, int T, uint64_t* bits, hipStream_t s) {
