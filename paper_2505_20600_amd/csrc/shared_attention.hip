@@ -115,20 +115,23 @@ __device__ __forceinline__ float seen_or_none(uint32_t w, int at, float x) {
 // Which keys of the tiles one slot sees.
 template <int KT>
 struct Sight {
-    const uint64_t* bits;       // its request's hidden tokens, NULL: it sees every one
+    uint32_t at;                // byte offset of its request's hidden tokens in the table
     int lo, hi;                 // its request's own rows
     __device__ __forceinline__ void init(const SharedAttnDesc& a, const Tables& t, const Work& w, int slot) {
         const int s = min(slot, w.slots - 1);
         const int b = request_of(a, t, w.row0 + s / a.group);
-        bits = a.bits ? a.bits + (long)b * a.words : nullptr;
+        at = (uint32_t)b * a.words * 8u;
         lo = t.own[b];
         hi = max(t.own[b + 1], lo);
     }
-    // hidden ones among prefix tile t's keys, as loaded
-    __device__ __forceinline__ uint64_t fetch(const SharedAttnDesc& a, int t) const {
-        if (!bits) return 0ull;
-        if constexpr (KT == 64) return bits[min(t, a.words - 1)];
-        else return reinterpret_cast<const uint32_t*>(bits)[min(t, 2 * a.words - 1)];
+    // hidden ones among prefix tile t's keys, as loaded; `table`: the bits, without an entry where none is hidden
+    __device__ __forceinline__ uint64_t fetch(__amdgpu_buffer_rsrc_t table, int t) const {
+        if constexpr (KT == 64) {
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(table, (int)at, t * 8, 0);
+            return (uint64_t)v[1] << 32 | v[0];
+        } else {
+            return __builtin_amdgcn_raw_buffer_load_b32(table, (int)at, t * 4, 0);
+        }
     }
     __device__ __forceinline__ uint64_t prefix(const SharedAttnDesc& a, uint64_t hidden, int t) const {
         return ~hidden & below<KT>(a.T - t * KT);
@@ -136,6 +139,11 @@ struct Sight {
     // of the own tile of rows k0 on
     __device__ __forceinline__ uint64_t own(int k0) const { return below<KT>(hi - k0) & ~below<KT>(lo - k0); }
 };
+
+// The hidden tokens' words; reads past the last word, or without a table, are zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t hidden_table(const SharedAttnDesc& a) {
+    return make_rsrc(a.bits, a.bits ? (uint32_t)a.batch * a.words * 8u : 0u);
+}
 
 // One slot's result over the keys [t0, t1) that it sees, by a wave: 64 keys at a time, a
 // lane's key's score, then the lanes as columns of the weighted sum.
@@ -154,7 +162,7 @@ __device__ __forceinline__ void recompute(const SharedAttnDesc& a, const Work& w
         for (int k = k0; k < k1; k += kWave) {
             const int key = k + lane;
             bool sees = key < k1;
-            if (sees && !part && sight.bits) sees = !((sight.bits[key / 64] >> (key % 64)) & 1);
+            if (sees && !part && a.bits) sees = !((a.bits[sight.at / 8 + key / 64] >> (key % 64)) & 1);
             float s = -INFINITY;
             if (sees) {
                 const T* const row = kv + (long)key * 2 * dkv;
@@ -272,13 +280,14 @@ struct Tiles {
         const bool whole = k0 + KT <= end;
 #pragma unroll
         for (int i = 0; i < IPW; ++i) {
-            const uint32_t o = whole || k0 + rl[i] < end ? off[i] + base : kAbsent;
             const int q = i * NW + wave;
             if (NQ % NW != 0 && q >= NQ) continue;
-            if (TILEB % 1024 != 0 && q == NQ - 1) {
-                if (threadIdx.x % kWave < 32) dma_buf16(rsrc, o, 0, lds + (uint32_t)q * 1024u);     // half a copy
+            if (TILEB % 1024 != 0 && q == NQ - 1) {     // half a copy
+                if (threadIdx.x % kWave < 32) dma_buf16(rsrc, whole || k0 + rl[i] < end ? off[i] + base : kAbsent, 0, lds + (uint32_t)q * 1024u);
+            } else if (whole) {
+                dma_buf16(rsrc, off[i], base, lds + (uint32_t)q * 1024u);
             } else {
-                dma_buf16(rsrc, o, 0, lds + (uint32_t)q * 1024u);
+                dma_buf16(rsrc, k0 + rl[i] < end ? off[i] + base : kAbsent, 0, lds + (uint32_t)q * 1024u);
             }
         }
     }
@@ -382,6 +391,7 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
     // Q^T fragments (B operand), their sign that of the score scale
     bf16x8_t qf[NQB][C::NK32];
     Sight<KT> sight[NQB];
+    const __amdgpu_buffer_rsrc_t table = hidden_table(a);
     const bf16_t* __restrict__ q = static_cast<const bf16_t*>(a.q);
     const int wq0 = w.q0 + (WIDE ? wave * 32 : 0);
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
@@ -423,15 +433,14 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
     for (int qb = 0; qb < NQB; ++qb)
 #pragma unroll
         for (int h = 0; h < C::NHS; ++h) oacc[qb][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // scores are as multiplied, weights 2^(cs score + neg): neg is minus cs times the running maximum
     const float cs = fabsf(a.scale_log2), rescale_at = kRescaleLog2 / cs;
-    float m_run[NQB];
-    f32x4_t negm[NQB];
+    float m_run[NQB], neg[NQB];
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {
         m_run[qb] = -INFINITY;
-        negm[qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        neg[qb] = 0.f;
     }
-    bool beyond = true;
     const bf16x8_t onesf = __builtin_bit_cast(bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
     constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
 
@@ -450,7 +459,7 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
             for (int kc = 0; kc < C::NK32; ++kc) {
                 const bf16x8_t kf = k_frag(base, ks, kc);
 #pragma unroll
-                for (int qb = 0; qb < NQB; ++qb) sacc[qb][ks] = mfma32(kf, qf[qb][kc], kc == 0 ? negm[qb] : sacc[qb][ks]);
+                for (int qb = 0; qb < NQB; ++qb) sacc[qb][ks] = mfma32(kf, qf[qb][kc], kc == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sacc[qb][ks]);
             }
     };
     // scores of keys that a slot does not see become -infinity, whatever they were
@@ -471,41 +480,28 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
         }
     };
     // online softmax: running maxima and accumulators updated, a rescale only where a score exceeds its slot's
-    // maximum by more than 2^8; after it the weights are 2^(cs score)
-    auto raise = [&](f32x4_t (&sacc)[NQB][NKS]) {
+    // maximum by more than 2^8
+    auto raise = [&](const f32x4_t (&sacc)[NQB][NKS]) {
         float mx[NQB];
+        bool above = false;
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb) {
             mx[qb] = sacc[qb][0][0];
 #pragma unroll
             for (int i = 1; i < 4 * NKS; ++i) mx[qb] = fmaxf(mx[qb], sacc[qb][i / 4][i % 4]);
+            above = above || mx[qb] > m_run[qb] + rescale_at;
         }
-        float most = mx[0];
-#pragma unroll
-        for (int qb = 1; qb < NQB; ++qb) most = fmaxf(most, mx[qb]);
-        if (beyond || __any(most > rescale_at)) {
-            bool far = false;
+        if (__any(above)) {
 #pragma unroll
             for (int qb = 0; qb < NQB; ++qb) {
-                const float rm = rows_max(mx[qb]);
-                const bool none = m_run[qb] == -INFINITY;
-                const float was = none ? -INFINITY : m_run[qb] + negm[qb][0];
-                const float up = fmaxf(rm, was);
-                const bool still = up == -INFINITY;
-                const float corr = none ? 0.f : fast_exp2((was - up) * cs);
+                const float up = fmaxf(m_run[qb], rows_max(mx[qb]));
+                const float corr = m_run[qb] == -INFINITY ? 0.f : fast_exp2((m_run[qb] - up) * cs);
 #pragma unroll
                 for (int h = 0; h < C::NHS; ++h) oacc[qb][h] *= corr;
-                m_run[qb] = fmaxf(m_run[qb], rm - negm[qb][0]);
-                const float n = m_run[qb] == -INFINITY ? 0.f : -fminf(fmaxf(m_run[qb], -kStartMax), kStartMax);
-                negm[qb] = f32x4_t{n, n, n, n};
-                far |= fabsf(m_run[qb]) > kStartMax;
-                const float off = still ? 0.f : up;
-#pragma unroll
-                for (int ks = 0; ks < NKS; ++ks)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) sacc[qb][ks][r] -= off;
+                m_run[qb] = up;
+                // a maximum beyond float32 after scaling is infinite, and so its row NaN
+                neg[qb] = up == -INFINITY ? 0.f : up * cs == INFINITY ? __uint_as_float(0x7fc00000u) : -up * cs;
             }
-            beyond = __any(far);
         }
     };
     auto weights = [&](f32x4_t (&sacc)[NQB][NKS]) {
@@ -514,7 +510,7 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sacc[qb][ks][r] = fast_exp2(sacc[qb][ks][r] * cs);
+                for (int r = 0; r < 4; ++r) sacc[qb][ks][r] = fast_exp2(fmaf(sacc[qb][ks][r], cs, neg[qb]));
     };
     auto pv = [&](uint32_t sbase, f32x4_t (&sacc)[NQB][NKS]) {
         // without a swizzle the blocks of 16 columns lie 32 bytes apart, an offset of the reads
@@ -584,7 +580,7 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
         };
         uint64_t hidden[NQB];
 #pragma unroll
-        for (int qb = 0; qb < NQB; ++qb) hidden[qb] = OWN ? 0ull : sight[qb].fetch(a, from);
+        for (int qb = 0; qb < NQB; ++qb) hidden[qb] = OWN ? 0ull : sight[qb].fetch(table, from);
         issue(from, 0);
         int n = 0;
         for (int t = from, then; t < to; t = then, ++n) {
@@ -601,7 +597,7 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
             if (then < to) {
 #pragma unroll
                 for (int qb = 0; qb < NQB; ++qb)
-                    if constexpr (!OWN) hidden[qb] = sight[qb].fetch(a, then);
+                    if constexpr (!OWN) hidden[qb] = sight[qb].fetch(table, then);
                 issue(then, n + 1);
             }
             if (WIDE && !active) continue;
@@ -770,6 +766,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_f32_kernel(SharedAttnDesc 
     const int slot = w.q0 + l16;
     Sight<KT> sight;
     sight.init(a, tables, w, slot);
+    const __amdgpu_buffer_rsrc_t table = hidden_table(a);
     const float* const q = static_cast<const float*>(a.q) + slot_row(a, w, slot) * HD;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
@@ -832,7 +829,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_f32_kernel(SharedAttnDesc 
         if (from >= to) return;
         S st;
         st.init(kv, rows, a.heads, w.kvh, lane);
-        uint64_t hidden = OWN ? 0ull : sight.fetch(a, from);
+        uint64_t hidden = OWN ? 0ull : sight.fetch(table, from);
         st.issue(base + from * KT);
         for (int t = from; t < to; t += 4) {
             const uint64_t sees = OWN ? sight.own(base + t * KT) : sight.prefix(a, hidden, t);
@@ -840,7 +837,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_f32_kernel(SharedAttnDesc 
             st.store(sw);
             asm volatile("" ::: "memory");
             if (t + 4 < to) {
-                if constexpr (!OWN) hidden = sight.fetch(a, t + 4);
+                if constexpr (!OWN) hidden = sight.fetch(table, t + 4);
                 st.issue(base + (t + 4) * KT);
             }
             multiply(sees);
