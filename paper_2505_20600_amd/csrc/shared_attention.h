@@ -18,7 +18,7 @@ struct SharedAttnDesc {
     const int32_t* fresh_start; // [batch + 1] own rows of each request
     int fresh_rows, batch, T, words, M, heads, group, hd;
     float scale_log2;           // log2(e) times the score scale
-    int tile;                   // query slots per workgroup: 16, or in bf16 32 or 128
+    int tile;                   // query slots per workgroup: 16 or 32, or in bf16 128
     int nsplit;                 // key ranges; > 1: partials in part_o / part_ml
     float* part_o;              // [nsplit][M][heads * group * hd], each range's output over its own sum
     float* part_ml;             // [nsplit][M][heads * group][2]: its maximum (log2 domain) and sum

@@ -94,7 +94,7 @@ __device__ __forceinline__ bool find_work(const SharedAttnDesc& a, int tile, int
     w.f0 = uniform(t.own[w.first]);
     w.f1 = max(uniform(t.own[w.last + 1]), w.f0);
     w.ntp = (a.T + KT - 1) / KT;
-    const uint32_t nt = w.ntp + (w.f1 - w.f0 + KT - 1) / KT;    // below 2^24; times 64 ranges below 2^32
+    const uint32_t nt = w.ntp + (w.f1 - w.f0 + KT - 1) / KT;    // below 2^24; times 32 ranges below 2^32
     w.t0 = uniform((int)(nt * split / a.nsplit));
     w.t1 = uniform((int)(nt * (split + 1) / a.nsplit));
     return true;
@@ -127,10 +127,10 @@ struct Sight {
     // hidden ones among prefix tile t's keys, as loaded; `table`: the bits, without an entry where none is hidden
     __device__ __forceinline__ uint64_t fetch(__amdgpu_buffer_rsrc_t table, int t) const {
         if constexpr (KT == 64) {
-            const auto v = __builtin_amdgcn_raw_buffer_load_b64(table, (int)at, t * 8, 0);
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(table, (int)at + t * 8, 0, 0);
             return (uint64_t)v[1] << 32 | v[0];
         } else {
-            return __builtin_amdgcn_raw_buffer_load_b32(table, (int)at, t * 4, 0);
+            return __builtin_amdgcn_raw_buffer_load_b32(table, (int)at + t * 4, 0, 0);
         }
     }
     __device__ __forceinline__ uint64_t prefix(const SharedAttnDesc& a, uint64_t hidden, int t) const {
@@ -213,7 +213,8 @@ __device__ __forceinline__ void recompute_bad(const SharedAttnDesc& a, const Wor
 }
 
 // The four waves' sums of 16 slots, from slot `first` of the tile on, each relative to its own maximum (so
-// [wave][slot][OLD] and sml [wave][slot]), to the output or the key range's part; slots without a finite result are flagged.
+// [wave][slot][OLD] and sml [wave][slot]), to the output or the key range's part; slots without a finite result are flagged and left: the output may be the
+// queries, which the second computation reads.
 template <typename T, int HD, int OLD>
 __device__ __forceinline__ void join_waves(const SharedAttnDesc& a, const Work& w, const float* so, const float2* sml, int tid,
                                            int first, uint32_t* bad) {
@@ -231,23 +232,39 @@ __device__ __forceinline__ void join_waves(const SharedAttnDesc& a, const Work& 
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
     bool fine = finite(sum);
     const long row = slot_row(a, w, slot), part = (long)w.split * a.M * a.heads * a.group + row;
-    for (int c = (tid % 16) * 4; c < HD; c += 64) {
-        float o[4] = {0.f, 0.f, 0.f, 0.f};
+    constexpr int NC = (HD + 63) / 64;
+    const int c0 = tid % 16 * 4;
+    float o[NC][4];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = c0 + i * 64;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[i][r] = 0.f;
+        if (c >= HD) continue;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const float4 x = *reinterpret_cast<const float4*>(so + (v * 16 + s) * OLD + c);
-            o[0] += f[v] * x.x; o[1] += f[v] * x.y; o[2] += f[v] * x.z; o[3] += f[v] * x.w;
+            o[i][0] += f[v] * x.x; o[i][1] += f[v] * x.y; o[i][2] += f[v] * x.z; o[i][3] += f[v] * x.w;
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            fine = fine && finite(o[r]);
-            o[r] *= inv;
+            fine = fine && finite(o[i][r]);
+            o[i][r] *= inv;
         }
-        if (a.nsplit == 1) store4<T>(static_cast<T*>(a.o) + row * HD + c, o);
-        else store4<float>(a.part_o + part * HD + c, o);
+    }
+    // of the 16 lanes that have the slot
+    if (__ballot(!fine) >> (tid % kWave / 16 * 16) & 0xffff) {
+        if (tid % 16 == 0) atomicOr(bad, 1u << (first + s));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = c0 + i * 64;
+        if (c >= HD) continue;
+        if (a.nsplit == 1) store4<T>(static_cast<T*>(a.o) + row * HD + c, o[i]);
+        else store4<float>(a.part_o + part * HD + c, o[i]);
     }
     if (a.nsplit > 1 && tid % 16 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * part) = make_float2(m, sum);
-    if (!fine) atomicOr(bad, 1u << (first + s));
 }
 
 // Tiles of KT K rows and as many V rows by direct-to-LDS loads of NW waves, K and V apart.
@@ -657,21 +674,22 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
             }
             const int slot = wq0 + rl;
             if (!fine && slot < w.slots) atomicOr(&bad[wave], 1u << rl);
-            if (a.nsplit > 1 && grp == 0 && slot < w.slots)
+            if (a.nsplit > 1 && fine && grp == 0 && slot < w.slots)
                 *reinterpret_cast<float2*>(a.part_ml + 2 * (range + slot_row(a, w, slot))) = make_float2(m_run[qb] * cs, l[qb]);
         }
         __syncthreads();
+        const uint32_t again = bad[wave];       // flagged slots are left: the output may be the queries, which the second computation reads
         if (a.nsplit == 1) {
             for (int k = lane; k < 32 * CH; k += kWave) {
                 const int rl = k / CH, c = k % CH;
-                if (wq0 + rl < w.slots)
+                if (wq0 + rl < w.slots && !(again >> rl & 1))
                     st16(static_cast<bf16_t*>(a.o) + slot_row(a, w, wq0 + rl) * HD + c * 8,
                          ld16(so + rl * S::ROWB + ((c ^ (rl & SWM)) * 16)));
             }
         } else {
             for (int k = lane; k < 32 * CF; k += kWave) {
                 const int rl = k / CF, c = k % CF;
-                if (wq0 + rl < w.slots)
+                if (wq0 + rl < w.slots && !(again >> rl & 1))
                     st16(a.part_o + (range + slot_row(a, w, wq0 + rl)) * HD + c * 4,
                          ld16(so + rl * 2 * S::ROWB + ((c ^ (rl & SWF)) * 16)));
             }
@@ -699,11 +717,11 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
             join_waves<bf16_t, HD, OLD>(a, w, so, sml, tid, qb * 16, &bad[0]);
         }
     }
-    __syncthreads();    // the flags are complete, and the results of flagged slots written
+    __syncthreads();    // the flags are complete
     recompute_bad<bf16_t, QT, KT>(a, w, tables, bad, wave);
 }
 
-// float32: 16 query slots in every wave, 32-key tiles of its own per wave, staged through registers
+// float32: 16 or 32 query slots in every wave, 32-key tiles of its own per wave, staged through registers
 // into padded rows, products on the float32 matrix instructions; joined at the end.
 template <int HD>
 struct TilesF32 {
@@ -743,10 +761,11 @@ struct TilesF32 {
     }
 };
 
-template <int HD>
+// One staged tile serves NQB blocks of 16 slots.
+template <int HD, int NQB>
 __global__ __launch_bounds__(kThreads, 2) void shared_f32_kernel(SharedAttnDesc a, int qtiles) {
     using S = TilesF32<HD>;
-    constexpr int KT = S::KT, P = S::P, NJ = (HD + 15) / 16;
+    constexpr int KT = S::KT, P = S::P, NJ = (HD + 15) / 16, QT = 16 * NQB;
     constexpr int OLD = NJ * 16 + 4;
     constexpr int JOIN = 4 * 16 * OLD + 4 * 16 * 2;     // words of the waves' sums
     __shared__ __attribute__((aligned(16))) float smem[4 * S::WORDS > JOIN ? 4 * S::WORDS : JOIN];
@@ -756,88 +775,113 @@ __global__ __launch_bounds__(kThreads, 2) void shared_f32_kernel(SharedAttnDesc 
     const int i = blockIdx.x / kXcds, pair = i / a.heads * kXcds + blockIdx.x % kXcds;
     Work w;
     if (pair >= qtiles * a.nsplit) return;
-    if (!find_work<16, KT>(a, pair / a.nsplit, i % a.heads, pair % a.nsplit, tables, w)) return;
+    if (!find_work<QT, KT>(a, pair / a.nsplit, i % a.heads, pair % a.nsplit, tables, w)) return;
     if (tid == 0) bad[0] = 0;
     float* const sw = smem + wave * S::WORDS;
     if (lane < 16) sw[2 * KT * P + lane] = 0.f;
 
-    // Q^T operand: slot l16, head_dim 16 j + 4 grp + e for the instruction (j, e)
-    float qf[NJ][4];
-    const int slot = w.q0 + l16;
-    Sight<KT> sight;
-    sight.init(a, tables, w, slot);
+    // Q^T operand: slot l16 of a block, head_dim 16 j + 4 grp + e for the instruction (j, e)
+    float qf[NQB][NJ][4];
+    Sight<KT> sight[NQB];
     const __amdgpu_buffer_rsrc_t table = hidden_table(a);
-    const float* const q = static_cast<const float*>(a.q) + slot_row(a, w, slot) * HD;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (slot < w.slots && j * 16 + grp * 4 < HD) load4<float>(q + j * 16 + grp * 4, v);
+    for (int qb = 0; qb < NQB; ++qb) {
+        const int slot = w.q0 + qb * 16 + l16;
+        sight[qb].init(a, tables, w, slot);
+        const float* const q = static_cast<const float*>(a.q) + slot_row(a, w, slot) * HD;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) qf[j][e] = v[e];
-    }
-    f32x4_t oacc[NJ];
+        for (int j = 0; j < NJ; ++j) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (slot < w.slots && j * 16 + grp * 4 < HD) load4<float>(q + j * 16 + grp * 4, v);
 #pragma unroll
-    for (int h = 0; h < NJ; ++h) oacc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float m_run = -INFINITY, l_run = 0.f;
-
-    auto multiply = [&](uint64_t sees) __attribute__((always_inline)) {
-        // S^T: keys 16 ks + 4 grp + r of slot l16, in the log2 domain
-        float sc[2][4];
-        float mx = -INFINITY;
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                float k[4] = {0.f, 0.f, 0.f, 0.f};
-                if (HD % 16 == 0 || j + 1 < NJ || j * 16 + grp * 4 < HD) load4<float>(sw + (ks * 16 + l16) * P + j * 16 + grp * 4, k);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc = Elt<float>::mma(k[e], qf[j][e], acc);
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const bool there = (sees >> (ks * 16 + grp * 4 + r)) & 1;
-                sc[ks][r] = there ? acc[r] * a.scale_log2 : -INFINITY;
-                mx = fmaxf(mx, sc[ks][r]);
-            }
+            for (int e = 0; e < 4; ++e) qf[qb][j][e] = v[e];
         }
-        const float m_new = fmaxf(m_run, rows_max(mx));
-        const float ref = m_new == -INFINITY ? 0.f : m_new;
-        const float corr = m_run == -INFINITY ? 0.f : fast_exp2(m_run - ref);
-        m_run = m_new;
-        l_run *= corr;
+    }
+    f32x4_t oacc[NQB][NJ];
+    float m_run[NQB], l_run[NQB];
 #pragma unroll
-        for (int h = 0; h < NJ; ++h) oacc[h] *= corr;
+    for (int qb = 0; qb < NQB; ++qb) {
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+        for (int h = 0; h < NJ; ++h) oacc[qb][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        m_run[qb] = -INFINITY;
+        l_run[qb] = 0.f;
+    }
+
+    auto multiply = [&](const uint64_t (&sees)[NQB]) __attribute__((always_inline)) {
+        // S^T: keys 16 ks + 4 grp + r of a slot, in the log2 domain
+        f32x4_t acc[NQB][2];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                sc[ks][r] = fast_exp2(sc[ks][r] - ref);
-                l_run += sc[ks][r];
-            }
+        for (int qb = 0; qb < NQB; ++qb) acc[qb][0] = acc[qb][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            float k[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+                if (HD % 16 == 0 || j + 1 < NJ || j * 16 + grp * 4 < HD) load4<float>(sw + (ks * 16 + l16) * P + j * 16 + grp * 4, k[ks]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                    for (int qb = 0; qb < NQB; ++qb) acc[qb][ks] = Elt<float>::mma(k[ks][e], qf[qb][j][e], acc[qb][ks]);
+        }
+        float sc[NQB][2][4];
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    sc[qb][ks][r] = seen_or_none((uint32_t)(sees[qb] >> (grp * 4)), ks * 16 + r, acc[qb][ks][r] * a.scale_log2);
+                    mx = fmaxf(mx, sc[qb][ks][r]);
+                }
+            const float m_new = fmaxf(m_run[qb], rows_max(mx));
+            const float ref = m_new == -INFINITY ? 0.f : m_new;
+            const float corr = m_run[qb] == -INFINITY ? 0.f : fast_exp2(m_run[qb] - ref);
+            m_run[qb] = m_new;
+            l_run[qb] *= corr;
+#pragma unroll
+            for (int h = 0; h < NJ; ++h) oacc[qb][h] *= corr;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    sc[qb][ks][r] = fast_exp2(sc[qb][ks][r] - ref);
+                    l_run[qb] += sc[qb][ks][r];
+                }
+        }
         // O^T += V^T P^T; a last block of eight columns multiplies what lies behind the row too, into rows that are not used
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int h = 0; h < NJ; ++h)
-                    oacc[h] = Elt<float>::mma(sw[(KT + ks * 16 + grp * 4 + r) * P + h * 16 + l16], sc[ks][r], oacc[h]);
+                for (int h = 0; h < NJ; ++h) {
+                    const float v = sw[(KT + ks * 16 + grp * 4 + r) * P + h * 16 + l16];
+#pragma unroll
+                    for (int qb = 0; qb < NQB; ++qb) oacc[qb][h] = Elt<float>::mma(v, sc[qb][ks][r], oacc[qb][h]);
+                }
     };
     auto run = [&](auto OWN, const void* kv, int base, int rows, int from, int to, int skip) __attribute__((always_inline)) {
         from += (wave - skip) & 3;   // the waves go on in turn from one kind to the next
         if (from >= to) return;
         S st;
         st.init(kv, rows, a.heads, w.kvh, lane);
-        uint64_t hidden = OWN ? 0ull : sight.fetch(table, from);
+        uint64_t hidden[NQB], sees[NQB];
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) hidden[qb] = OWN ? 0ull : sight[qb].fetch(table, from);
         st.issue(base + from * KT);
         for (int t = from; t < to; t += 4) {
-            const uint64_t sees = OWN ? sight.own(base + t * KT) : sight.prefix(a, hidden, t);
+#pragma unroll
+            for (int qb = 0; qb < NQB; ++qb) sees[qb] = OWN ? sight[qb].own(base + t * KT) : sight[qb].prefix(a, hidden[qb], t);
             asm volatile("" ::: "memory");      // LDS operations of a wave are done in order
             st.store(sw);
             asm volatile("" ::: "memory");
             if (t + 4 < to) {
-                if constexpr (!OWN) hidden = sight.fetch(table, t + 4);
+#pragma unroll
+                for (int qb = 0; qb < NQB; ++qb)
+                    if constexpr (!OWN) hidden[qb] = sight[qb].fetch(table, t + 4);
                 st.issue(base + (t + 4) * KT);
             }
             multiply(sees);
@@ -847,20 +891,23 @@ __global__ __launch_bounds__(kThreads, 2) void shared_f32_kernel(SharedAttnDesc 
     run(std::false_type{}, a.kv, 0, a.T, c0, c1, 0);
     if (w.f1 > w.f0) run(std::true_type{}, a.fresh, w.f0, w.f1, max(w.t0 - w.ntp, 0), max(w.t1 - w.ntp, 0), c1 - c0);
 
-    const float l = rows_sum(l_run);
-    __syncthreads();
     float* const so = smem;
     float2* const sml = reinterpret_cast<float2*>(so + 4 * 16 * OLD);
 #pragma unroll
-    for (int h = 0; h < NJ; ++h) {
-        const float v[4] = {oacc[h][0], oacc[h][1], oacc[h][2], oacc[h][3]};
-        store4<float>(so + (wave * 16 + l16) * OLD + h * 16 + grp * 4, v);
+    for (int qb = 0; qb < NQB; ++qb) {
+        const float l = rows_sum(l_run[qb]);
+        __syncthreads();    // every wave is past its last read of the tiles, or of the block before
+#pragma unroll
+        for (int h = 0; h < NJ; ++h) {
+            const float v[4] = {oacc[qb][h][0], oacc[qb][h][1], oacc[qb][h][2], oacc[qb][h][3]};
+            store4<float>(so + (wave * 16 + l16) * OLD + h * 16 + grp * 4, v);
+        }
+        if (grp == 0) sml[wave * 16 + l16] = make_float2(m_run[qb], l);
+        __syncthreads();
+        join_waves<float, HD, OLD>(a, w, so, sml, tid, qb * 16, bad);
     }
-    if (grp == 0) sml[wave * 16 + l16] = make_float2(m_run, l);
-    __syncthreads();
-    join_waves<float, HD, OLD>(a, w, so, sml, tid, 0, bad);
-    __syncthreads();    // the flags are complete, and the results of flagged slots written
-    recompute_bad<float, 16, KT>(a, w, tables, bad, wave);
+    __syncthreads();    // the flags are complete
+    recompute_bad<float, QT, KT>(a, w, tables, bad, wave);
 }
 
 // Join of the key ranges: range s has the weight l_s 2^(m_s - m); rows of no
@@ -937,12 +984,13 @@ void launch_bf16(const SharedAttnDesc& a, hipStream_t s) {
     }
 }
 
+template <int NQB>
 void launch_f32(const SharedAttnDesc& a, hipStream_t s) {
-    const int qtiles = slot_tiles(a, 16);
+    const int qtiles = slot_tiles(a, 16 * NQB);
     const int pairs = qtiles * a.nsplit;
     const dim3 grid((unsigned)(pairs + kXcds - 1) / kXcds * kXcds * a.heads), block(kThreads);
     switch (a.hd) {
-#define MS_HD(n) case n: hipLaunchKernelGGL(shared_f32_kernel<n>, grid, block, 0, s, a, qtiles); break;
+#define MS_HD(n) case n: hipLaunchKernelGGL((shared_f32_kernel<n, NQB>), grid, block, 0, s, a, qtiles); break;
         MS_HD(8) MS_HD(16) MS_HD(24) MS_HD(32) MS_HD(40) MS_HD(48) MS_HD(56) MS_HD(64)
 #undef MS_HD
     }
@@ -962,10 +1010,12 @@ bool ranges_fit(const SharedAttnDesc& a, int tile, int n) {
 //   a + rounds (steps (s0 + s1 hd/64 + (s2 + s3 hd/64) k) + o0 + o1 hd/64)
 // and more than one range r0 + r1 n MB + r2 MB more, MB the size of one range's parts. A tile's own rows are taken
 // as its slots' rows and an eighth of all: the requests' number plays no part, so that a workspace is planned for the call's shapes.
-// Fitted to 4437 measured times (285 shapes: 16 to 128 columns, 1 to 24 K/V heads, groups of 1 to 8, 64 to 11000 tokens, 1 to 5700
-// rows of 1 to 32 requests, every form, 1 to 48 ranges); among powers of two the chosen pair takes 1.02 times the fastest on
-// average, 1.40 times at most. In us at the best count of ranges, 16 / 32 / 128 slots: 8 requests over 4096 tokens of 16 heads of
-// 64, one row each 11 / 13 / 17, 16 rows 21 / 19 / 24, 32 rows 31 / 25 / 30, 128 rows 94 / 54 / 50, 500 rows 390 / 237 / 133.
+// Fitted to 5949 measured times (237 shapes in bf16 and 234 in float32: 16 to 128 columns, 1 to 24 K/V heads, groups of 1 to 8, 64 to
+// 11000 tokens, 1 to 5700 rows of 1 to 32 requests, every form, 1 to 48 ranges); among powers of two the chosen pair takes 1.02
+// times the fastest on average, 1.40 times at most. In us at the best count of ranges, bf16, 16 / 32 / 128 slots: 8 requests over
+// 4096 tokens of 16 heads of 64, one row each 11 / 13 / 17, 16 rows 21 / 19 / 24, 32 rows 31 / 25 / 30, 128 rows 94 / 54 / 50, 500 rows
+// 390 / 237 / 133; float32, 16 / 32 slots: 1 request of 205 rows over 1024 tokens of 4 heads of 64 14.4 / 15.9, 4 of them 31.5 /
+// 30.2, 3 of 137 to 661 rows over 1687 tokens of 26 heads 264 / 210.
 void plan_shared_attention(int dtype, SharedAttnDesc& a) {
     a.tile = 16;
     a.nsplit = 1;
@@ -977,11 +1027,12 @@ void plan_shared_attention(int dtype, SharedAttnDesc& a) {
     static const Form bf16[] = {{16, 128, 2.98, 0.101, 0.237, 0.208, 0.201, 2.16, 0.345, 3.21, 0.85, 1.92},
                                 {32, 128, 3.23, 0.044, 0.528, 0.378, 0.023, 2.96, 0.581, 2.92, 0.533, 2.83},
                                 {128, 64, 5.25, 0.051, 0.356, 0.563, 0.0, 1.99, 1.21, 3.4, 0.248, 2.37}};
-    static const Form f32[] = {{16, 128, 4.8, 0.236, 0.211, 0.039, 1.64, 0.0, 0.99, 3.4, 1.07, 1.0}};
+    static const Form f32[] = {{16, 128, 4.02, 0.0, 0.597, 0.258, 0.972, 1.085, 1.099, 3.08, 0.731, 0.607},
+                               {32, 128, 4.19, 0.0, 0.99, 0.56, 1.378, 1.264, 1.244, 3.18, 1.06, 0.737}};
     const long slots = (long)a.M * a.group;
     const double h = a.hd / 64.0, mb = (double)slots * a.heads * (a.hd + 2) * 4e-6;
     double least = 1e30;
-    for (int i = 0; i < (dtype == kBF16 ? 3 : 1); ++i) {
+    for (int i = 0; i < (dtype == kBF16 ? 3 : 2); ++i) {
         const Form& f = dtype == kBF16 ? bf16[i] : f32[i];
         // few slots: not where a larger tile is full several times over
         if (dtype == kBF16 && f.tile < 128 && slots > 16 * f.tile + 16 * (f.tile - 16)) continue;
@@ -1016,8 +1067,10 @@ hipError_t launch_shared_attention(int dtype, const SharedAttnDesc& a, hipStream
         if (a.tile == 16) launch_bf16<16>(a, s);
         else if (a.tile == 32) launch_bf16<32>(a, s);
         else launch_bf16<128>(a, s);
+    } else if (a.tile == 16) {
+        launch_f32<1>(a, s);
     } else {
-        launch_f32(a, s);
+        launch_f32<2>(a, s);
     }
     return hipGetLastError();
 }

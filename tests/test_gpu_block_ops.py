@@ -173,6 +173,38 @@ def test_nan_scales_stay_in_their_rows_and_columns(M, N, K):
     assert torch.equal(torch.isnan(out), nan) and torch.equal(out[~nan], clean[~nan])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,N,K,shift", [(300, 264, 128, 0), (300, 264, 256, 0), (300, 264, 384, 0), (300, 264, 4096, 0), (270, 200, 4224, 0),
+                                         (4100, 4100, 384, 0), (4097, 4004, 512, 0), (2000, 4100, 640, 0), (2049, 4036, 1024, 0),
+                                         (1030, 2052, 2080, 0), (2000, 4100, 672, 0), (300, 264, 384, 1), (2000, 4100, 640, 2), (33, 68, 2048, 3)])
+def test_product_of_every_tile_size(dtype, M, N, K, shift):
+    """Sizes that take small and large tiles, whole and half steps, K ranges; scales that start at any byte."""
+    g = torch.Generator().manual_seed(M + K)
+    a, w = _operand(g, M, K), _operand(g, N, K, 1.0 / math.sqrt(K))
+    bias, out = _randn(g, (N,), dtype), torch.empty(M + 1, N, dtype=DT[dtype], device=DEV)
+    want, size = mx4.linear(mx4.values(a[0].cpu().numpy(), a[1].cpu().numpy()), mx4.values(w[0].cpu().numpy(), w[1].cpu().numpy()), _np(bias))
+    bound = _product_bound(want, size, K, dtype)
+    store = [torch.full((shift + t.numel() + 8,), 255, dtype=torch.uint8, device=DEV) for t in (a[1], w[1])]
+    sa, sw = (m[shift:shift + t.numel()].view(t.shape) for m, t in zip(store, (a[1], w[1])))
+    sa.copy_(a[1])
+    sw.copy_(w[1])
+    need = MS.ms_mx4_linear_workspace_bytes(a[0], w[0])
+    for size in sorted({0, need // 2, need}):
+        ws = torch.full((size + 16,), 0xff, dtype=torch.uint8, device=DEV) if size else None
+        out.fill_(7.0)
+        MS.ms_mx4_linear(a[0], sa, w[0], sw, bias, out[:M], workspace=ws)
+        _within(_np(out[:M]), want, bound, f"{M}x{N}x{K} workspace {size}")
+        assert bool((out[M] == 7.0).all())
+    MS.ms_mx4_linear(a[0], sa, w[0], sw, bias, out[:M])
+    sa[M - 1, 0] = sw[1, K // 32 - 1] = sw[N - 1, 0] = 255
+    nan = torch.zeros(M, N, dtype=torch.bool, device=DEV)
+    nan[M - 1] = True
+    nan[:, 1] = nan[:, N - 1] = True
+    got = torch.empty(M, N, dtype=DT[dtype], device=DEV)
+    MS.ms_mx4_linear(a[0], sa, w[0], sw, bias, got)
+    assert torch.equal(torch.isnan(got), nan) and torch.equal(got[~nan], out[:M][~nan])
+
+
 def test_scales_of_every_size():
     """Scale bytes from 2 to 250 on both sides, products within float32."""
     g = torch.Generator().manual_seed(9)
@@ -455,6 +487,21 @@ def test_output_over_the_queries(dtype, rows):
         q = s["q"].clone()
         t = dict(s, q=q)
         assert torch.equal(_attend(t, ws, out=q), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [(4,), (20, 9), (30, 70), (70, 90)])
+def test_output_over_the_queries_with_hidden_nan(dtype, rows):
+    """Results that are computed again read queries that the output has not replaced."""
+    g = torch.Generator().manual_seed(sum(rows))
+    s = _batch(g, dtype, rows, 500, 2, 64, 1)
+    s["hidden"][:, 40:44] = True
+    s["kv"][40:44] = math.nan
+    for ws in (None, "need"):
+        want = _attend(s, ws).clone()
+        _check_rows(s, dtype, want, slice(0, sum(rows)))
+        t = dict(s, q=s["q"].clone())
+        assert torch.equal(_attend(t, ws, out=t["q"]), want)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
