@@ -318,7 +318,7 @@ __global__ __launch_bounds__(WM * WN * kWave) void mx4_stream_kernel(Mx4LinearDe
     const int half_step = g.K % kStep ? steps - 1 : -1;     // its second half lies past K
 
     // rows past the last lie past the buffers and read as zeros; a row's 16-byte chunks are permuted by the row
-    uint32_t va[C::PA], vw[C::PW], vs[C::PS];
+    uint32_t va[C::PA], vw[2][C::PW], vs[C::PS];
     const int c8 = (lane % 8) ^ k_chunk(lane / 8), c8b = (lane % 8) ^ k_chunk(lane / 8 + 8);    // of a copy's rows: even, odd copies
 #pragma unroll
     for (int i = 0; i < C::PA; ++i) {
@@ -328,7 +328,9 @@ __global__ __launch_bounds__(WM * WN * kWave) void mx4_stream_kernel(Mx4LinearDe
 #pragma unroll
     for (int i = 0; i < C::PW; ++i) {
         const int q = i * C::NW + wave, r = q * 8 + lane / 8;
-        vw[i] = (uint32_t)(r / C::HALFN * 2 * C::HALFN + r % C::HALFN) * rowb + (q % 2 ? c8b : c8) * 16;
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+            vw[part][i] = (uint32_t)((r / C::HALFN * 2 + part) * C::HALFN + r % C::HALFN) * rowb + (q % 2 ? c8b : c8) * 16;
     }
 #pragma unroll
     for (int i = 0; i < C::PS; ++i) {       // copies past the last repeat earlier ones
@@ -344,7 +346,7 @@ __global__ __launch_bounds__(WM * WN * kWave) void mx4_stream_kernel(Mx4LinearDe
     auto issue_w = [&](int t, int part, int i) {
         const int q = i * C::NW + wave;
         const bool absent = t == half_step && (q % 2 ? past1 : past0);
-        dma_buf16(rw, absent ? kAbsent : vw[i], (uint32_t)t * C::ROWB + (uint32_t)part * C::HALFN * rowb,
+        dma_buf16(rw, absent ? kAbsent : vw[part][i], (uint32_t)t * C::ROWB,
                   lds0 + (t & 1) * C::STAGEB + C::AT_W + part * C::REGW + q * 1024);
     };
     // scales of steps 4 b to 4 b + 3; what lies past a row's end is not used

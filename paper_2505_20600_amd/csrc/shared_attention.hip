@@ -451,7 +451,7 @@ __global__ __launch_bounds__(kThreads, QT == 128 ? wide_per_cu(HD) : few_per_cu(
 #pragma unroll
         for (int h = 0; h < C::NHS; ++h) oacc[qb][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     // scores are as multiplied, weights 2^(cs score + neg): neg is minus cs times the running maximum
-    const float cs = fabsf(a.scale_log2), rescale_at = kRescaleLog2 / cs;
+    const float cs = fabsf(a.scale_log2), rescale_at = fminf(kRescaleLog2 / cs, 3.4e38f);    // finite for the smallest scales too
     float m_run[NQB], neg[NQB];
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {

@@ -42,7 +42,7 @@ def _same_codes(got, want):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("rows,cols", [(1, 32), (3, 64), (5, 1056), (130, 96), (33, 4096), (1, 16384), (1000, 160)])
+@pytest.mark.parametrize("rows,cols", [(1, 32), (3, 64), (5, 1056), (130, 96), (33, 4096), (1, 16384), (1000, 160), (4099, 2080)])
 def test_codes_are_exact_and_read_back(dtype, rows, cols):
     g = torch.Generator().manual_seed(rows + cols)
     x = _randn(g, (rows, cols), dtype) * torch.exp(2 * torch.randn(rows, cols // 32, generator=g)).repeat_interleave(32, 1).to(DEV).to(DT[dtype])
@@ -470,7 +470,7 @@ def test_scores_of_infinity(dtype, rows, ws):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("scale", [-0.3, 2.0, 1e-6])
+@pytest.mark.parametrize("scale", [-0.3, 2.0, 1e-6, 1e-44])
 def test_attention_scales(dtype, scale):
     g = torch.Generator().manual_seed(3)
     _check(_batch(g, dtype, (20, 5), 300, 2, 64, 2), dtype, scale=scale)
