@@ -57,14 +57,14 @@ struct Mx4LinearDesc {
     int waves;                  // of a workgroup of the form for few rows
 };
 
-// Outputs of a workgroup: 16 x 16, or tiles of 64, 128 or 256 rows and columns, of any K or (Stream) a multiple of 128.
-enum { kMx4Rows = 0, kMx4Any64, kMx4Any256, kMx4Stream64, kMx4Stream128, kMx4Stream256 };
+// Outputs of a workgroup: 16 x 16, or tiles of 64, 128 or 256 rows and columns.
+enum { kMx4Rows = 0, kMx4Tile64, kMx4Tile128, kMx4Tile256 };
 
 hipError_t launch_mx4_quantize(int dtype, const void* x, long rows, int cols, long ld, uint8_t* codes, uint8_t* scales,
                                hipStream_t s);
 hipError_t launch_mx4_dequantize(int dtype, const uint8_t* codes, const uint8_t* scales, long rows, int cols, void* x,
                                  long ld, hipStream_t s);
-// Sets the form and the K split from the shape, the scales' alignment and what the caller's buffer for parts holds.
+// Sets the form and the K split from the shape and what the caller's buffer for parts holds.
 void plan_mx4_linear(Mx4LinearDesc& d, size_t part_floats);
 hipError_t launch_mx4_linear(int dtype, const Mx4LinearDesc& d, hipStream_t s);
 

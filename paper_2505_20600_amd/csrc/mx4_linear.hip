@@ -144,6 +144,11 @@ __device__ __forceinline__ void write_tile(const GemmDesc& g, int m0, int n0, in
 // Tiles of BM x BN outputs by WM x WN waves, steps of 256 elements of K in two stages of LDS. Codes land
 // there by direct loads; a step's scales (8 bytes a row) come through registers, a thread to a row, and are laid
 // out so that a lane finds those of its row and columns for two fragments and both halves of the step in one word.
+// 8192 x 4096 x 16384 in tiles of 256 takes 271 us, 4.06 PFLOP/s of the 7.1 to 7.7 that the instruction reaches alone:
+// matrix cores busy 41%, the rest is the stream of operands into a CU (direct loads cost it about four cycles per 128-byte
+// line, 512 of them a step) and its LDS reads, which two stages and one workgroup per CU overlap in part. A ring of three
+// regions with the next step's fragments and scales (through LDS as well) read under the last products took 271 us too, 283
+// against 283 at 8192 x 8192 x 8192, 49 against 53 at 8192 x 4608 x 1152: 1.4% over 16 sizes, not worth a second kernel.
 template <int BM, int BN, int WM, int WN>
 struct Tile {
     static constexpr int NT = WM * WN * kWave;
@@ -268,221 +273,6 @@ __global__ __launch_bounds__(WM * WN * kWave) void mx4_linear_kernel(Mx4LinearDe
     write_tile<T, EPI, MI, NI>(g, m0 + wm, n0 + wn, split, acc, smem, wave, lane);
 }
 
-// Lane (group g of 16, l) holds the four scale bytes of row 16 g + l, one per 32 columns; returns, in byte i, that
-// of row 16 i + l and columns 32 g on: a transpose of 4 x 4 bytes across the lane groups in two exchanges.
-__device__ __forceinline__ uint32_t scale_bytes(uint32_t v, uint32_t pick2, uint32_t pick1) {
-    const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);       // of group g % 2, of group g % 2 + 2
-    const uint32_t e = __builtin_amdgcn_perm(a[1], a[0], pick2);               // their columns 2 (g / 2) and 2 (g / 2) + 1
-    const auto b = __builtin_amdgcn_permlane16_swap(e, e, false, false);       // the same of even and odd groups
-    return __builtin_amdgcn_perm(b[1], b[0], pick1);
-}
-
-// The same where K is a multiple of 128 and the scales are 4-byte aligned: everything lands in LDS by direct loads. Such a
-// load costs a CU about four cycles per 128-byte line that it touches, however little of it, so a row's codes come
-// as 128 bytes (a step) and its scales as 32 (four steps). A stage is three regions: the rows of A, and the first and the
-// second half of every wave's rows of W. Halfway through step t all waves have A's fragments in registers and are done
-// with the first half of W: there, at the only barrier of a step, these regions take step t + 2 and the second half's other
-// stage step t + 1, so that a whole step's copies are under way all the time; the fragments that step t + 1 starts with
-// are read under the last products of step t.
-template <int BM, int BN, int WM, int WN>
-struct Stream {
-    static constexpr int NW = WM * WN;
-    static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
-    static constexpr int ROWB = kRowB, HALFN = BN / WN / 2;         // rows of W of a wave in each of its regions
-    static constexpr int AT_W = BM * ROWB, REGW = BN / 2 * ROWB, STAGEB = AT_W + 2 * REGW;
-    static constexpr int SCALES = 2 * STAGEB, SCALEB = (BM + BN) * 32;  // two blocks of four steps' scales behind the stages
-    static constexpr int OUTB = NW * 16 * (NI * 16 + 4) * 4;
-    static constexpr int END = SCALES + 2 * SCALEB, LDSB = END > OUTB ? END : OUTB;
-    static constexpr int PA = BM / 8 / NW, PW = BN / 16 / NW;       // 1 KB copies of a wave: A, half of W
-    static constexpr int SC = (BM + BN) / 32, PS = (SC + NW - 1) / NW;  // 1 KB copies of scales, those of a wave
-    static_assert(BM / 8 % NW == 0 && BN / 16 % NW == 0 && BM % 64 == 0 && BN % 64 == 0 && NI % 2 == 0 && MI <= 4, "tile");
-};
-
-template <typename T, int EPI, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * kWave) void mx4_stream_kernel(Mx4LinearDesc d) {
-    using C = Stream<BM, BN, WM, WN>;
-    constexpr int MI = C::MI, NI = C::NI, NS = (NI + 3) / 4;
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDSB];
-    const GemmDesc& g = d.g;
-    const uint32_t lds0 = lds_addr(smem);
-    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const int grp = lane / 16, l16 = lane % 16;
-    int m0, n0, split;
-    tile_of<BM, BN>(g, m0, n0, split);
-    const uint32_t rowb = (uint32_t)g.K / 2, blocks = (uint32_t)g.K / kMxBlock;
-    const int rows_a = min(BM, g.M - m0), rows_w = min(BN, g.N - n0);
-    const u32x4_t ra = raw_rsrc(d.a + (long)m0 * rowb, (uint32_t)rows_a * rowb), rw = raw_rsrc(d.w + (long)n0 * rowb, (uint32_t)rows_w * rowb);
-    const u32x4_t qa = raw_rsrc(d.as + (long)m0 * blocks, (uint32_t)rows_a * blocks), qw = raw_rsrc(d.ws + (long)n0 * blocks, (uint32_t)rows_w * blocks);
-    const int steps = (g.K + kStep - 1) / kStep;
-    const int t0 = split * g.kchunk, t1 = min(steps, t0 + g.kchunk);
-    const int half_step = g.K % kStep ? steps - 1 : -1;     // its second half lies past K
-
-    // rows past the last lie past the buffers and read as zeros; a row's 16-byte chunks are permuted by the row
-    uint32_t va[C::PA], vw[2][C::PW], vs[C::PS];
-    const int c8 = (lane % 8) ^ k_chunk(lane / 8), c8b = (lane % 8) ^ k_chunk(lane / 8 + 8);    // of a copy's rows: even, odd copies
-#pragma unroll
-    for (int i = 0; i < C::PA; ++i) {
-        const int q = i * C::NW + wave;
-        va[i] = (uint32_t)(q * 8 + lane / 8) * rowb + (q % 2 ? c8b : c8) * 16;
-    }
-#pragma unroll
-    for (int i = 0; i < C::PW; ++i) {
-        const int q = i * C::NW + wave, r = q * 8 + lane / 8;
-#pragma unroll
-        for (int part = 0; part < 2; ++part)
-            vw[part][i] = (uint32_t)((r / C::HALFN * 2 + part) * C::HALFN + r % C::HALFN) * rowb + (q % 2 ? c8b : c8) * 16;
-    }
-#pragma unroll
-    for (int i = 0; i < C::PS; ++i) {       // copies past the last repeat earlier ones
-        const int c = (i * C::NW + wave) % C::SC;
-        vs[i] = (uint32_t)((c < BM / 32 ? c : c - BM / 32) * 32 + lane / 2) * blocks + lane % 2 * 16;
-    }
-    const bool past0 = c8 >= 4, past1 = c8b >= 4;           // chunks that the half step lacks
-    auto issue_a = [&](int t, int i) {
-        const int q = i * C::NW + wave;
-        const bool absent = t == half_step && (q % 2 ? past1 : past0);
-        dma_buf16(ra, absent ? kAbsent : va[i], (uint32_t)t * C::ROWB, lds0 + (t & 1) * C::STAGEB + q * 1024);
-    };
-    auto issue_w = [&](int t, int part, int i) {
-        const int q = i * C::NW + wave;
-        const bool absent = t == half_step && (q % 2 ? past1 : past0);
-        dma_buf16(rw, absent ? kAbsent : vw[part][i], (uint32_t)t * C::ROWB,
-                  lds0 + (t & 1) * C::STAGEB + C::AT_W + part * C::REGW + q * 1024);
-    };
-    // scales of steps 4 b to 4 b + 3; what lies past a row's end is not used
-    auto issue_scales = [&](int b, int i) {
-        const int c = (i * C::NW + wave) % C::SC;
-        dma_buf16(c < BM / 32 ? qa : qw, vs[i], (uint32_t)b * 32u, lds0 + C::SCALES + (b & 1) * C::SCALEB + c * 1024);
-    };
-    const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
-
-    f32x4_t acc[NI][MI];
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < MI; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    // selectors of the scales' transpose
-    const uint32_t pick2 = grp < 2 ? 0x05040100u : 0x07060302u, pick1 = grp % 2 ? 0x07030501u : 0x06020400u;
-    // scales of up to 64 staged rows from `row` on, both halves of step t as they lie
-    auto read_scales = [&](int t, int row, int rows) {
-        const uint8_t* const p = smem + C::SCALES + (t / 4 & 1) * C::SCALEB + t % 4 * 8;
-        return *reinterpret_cast<const uint2*>(p + (row + lane % (rows < 64 ? rows : 64)) * 32);
-    };
-    const uint32_t at_k[2] = {(uint32_t)((grp ^ k_chunk(l16)) * 16), (uint32_t)(((4 + grp) ^ k_chunk(l16)) * 16)};
-    const uint32_t at_a = (uint32_t)(wm + l16) * C::ROWB;
-    const uint32_t at_w = (uint32_t)(C::AT_W + (wn / 2 + l16) * C::ROWB);
-    // what a step starts with; A's other half is read under its first products
-    struct Start {
-        vec16 a[MI], w[2];
-        uint32_t sa[2], sw[2][NS];
-    };
-    auto read_a = [&](int t, int k, int j) { return ld16(smem + (t & 1) * C::STAGEB + at_a + j * 16 * C::ROWB + at_k[k]); };
-    auto read_w = [&](int t, int i, int k) {
-        return ld16(smem + (t & 1) * C::STAGEB + at_w + (i < NI / 2 ? i * 16 * C::ROWB : C::REGW + (i - NI / 2) * 16 * C::ROWB) + at_k[k]);
-    };
-    // A step is 2 MI NI slots of one product each; what has to be done besides is dealt out to them in a fixed order, so that
-    // it is issued while the matrix cores work. After the barrier (slot MID): the copies, the next step's first
-    // operands, and the transposes of its scales.
-    constexpr int SLOTS = 2 * MI * NI, MID = (NI / 2 - 1) * 2 * MI;
-    constexpr int A0 = C::PW, A1 = A0 + C::PA, A2 = A1 + C::PW, A3 = A2 + C::PS, A4 = A3 + 1 + NS, A5 = A4 + MI, A6 = A5 + 2 * (1 + NS), AUX = A6 + 2;
-    auto step = [&](const Start& c, Start& n, int t) __attribute__((always_inline)) {
-        vec16 w[NI][2], a1[MI];
-        uint2 raw[1 + NS];
-        w[0][0] = c.w[0];
-        w[0][1] = c.w[1];
-        const uint32_t upper = t + 1 == half_step ? 0u : ~0u;       // a row's end may have any bytes behind it
-        auto other = [&](int x) __attribute__((always_inline)) {
-            if (x < A0) {
-                if (t + 1 < t1) issue_w(t + 1, 1, x);
-            } else if (x < A1) {
-                if (t + 2 < t1) issue_a(t + 2, x - A0);
-            } else if (x < A2) {
-                if (t + 2 < t1) issue_w(t + 2, 0, x - A1);
-            } else if (x < A3) {
-                if (t + 2 < t1 && (t + 2) % 4 == 0) issue_scales((t + 2) / 4, x - A2);
-            } else if (x < A4) {
-                raw[x - A3] = x == A3 ? read_scales(t + 1, wm, MI * 16) : read_scales(t + 1, BM + wn + (x - A3 - 1) * 64, NI * 16);
-            } else if (x < A5) {
-                n.a[x - A4] = read_a(t + 1, 0, x - A4);
-            } else if (x < A6) {
-                const int y = (x - A5) / 2, k = (x - A5) % 2;
-                const uint32_t v = scale_bytes(k ? raw[y].y & upper : raw[y].x, pick2, pick1);
-                if (y == 0) n.sa[k] = v;
-                else n.sw[k][y - 1] = v;
-            } else {
-                n.w[x - A6] = read_w(t + 1, 0, x - A6);
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int j = 0; j < MI; ++j) {
-                    const int slot = (i * 2 + k) * MI + j;
-                    if (MID >= MI ? slot < MI : slot == 0) {    // before the barrier
-#pragma unroll
-                        for (int x = 0; x < MI; ++x)
-                            if (MID < MI || x == slot) a1[x] = read_a(t, 1, x);
-                    }
-                    if (slot == MID) {
-                        wait_all();     // what the last step's middle sent for has landed; A and the first half of W are read
-                        barrier_only();
-                    }
-                    if (i + 1 < NI && k == 0 && j < 2) w[i + 1][j] = read_w(t, i + 1, j);
-#pragma unroll
-                    for (int x = 0; x < AUX; ++x)
-                        if (MID + 1 + x * (SLOTS - MID - 1) / AUX == slot) other(x);
-                    __builtin_amdgcn_sched_barrier(0);
-                    acc[i][j] = mfma_mx4_b(w[i][k], k ? a1[j] : c.a[j], acc[i][j], (int)c.sw[k][i / 4], i % 4, (int)c.sa[k], j);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-    };
-    if (t0 < t1) {
-        auto issue_step = [&](int t, bool scales, int parts) {
-#pragma unroll
-            for (int i = 0; i < C::PS; ++i)
-                if (scales) issue_scales(t / 4, i);
-#pragma unroll
-            for (int i = 0; i < C::PA; ++i) issue_a(t, i);
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int i = 0; i < C::PW; ++i)
-                    if (p < parts) issue_w(t, p, i);
-        };
-        issue_step(t0, true, 2);
-        if (t0 + 1 < t1) {
-            issue_step(t0 + 1, (t0 + 1) % 4 == 0, 1);
-            wait_vmcnt<C::PA + C::PW>();
-        } else {
-            wait_all();
-        }
-        barrier_only();
-        Start f0, f1;
-        const uint32_t upper = t0 == half_step ? 0u : ~0u;
-        const uint2 v = read_scales(t0, wm, MI * 16);
-        f0.sa[0] = scale_bytes(v.x, pick2, pick1);
-        f0.sa[1] = scale_bytes(v.y & upper, pick2, pick1);
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const uint2 u = read_scales(t0, BM + wn + i * 64, NI * 16);
-            f0.sw[0][i] = scale_bytes(u.x, pick2, pick1);
-            f0.sw[1][i] = scale_bytes(u.y & upper, pick2, pick1);
-        }
-#pragma unroll
-        for (int j = 0; j < MI; ++j) f0.a[j] = read_a(t0, 0, j);
-        f0.w[0] = read_w(t0, 0, 0);
-        f0.w[1] = read_w(t0, 0, 1);
-        for (int t = t0; t < t1; ++t) {
-            step(f0, f1, t);
-            f0 = f1;
-        }
-    }
-    wait_all();
-    write_tile<T, EPI, MI, NI>(g, m0 + wm, n0 + wn, split, acc, smem, wave, lane);
-}
-
 // Few rows: 16 x 16 outputs per workgroup of up to 16 waves; every wave has 256-element steps of its own (step wave +
 // waves i) and loads its fragments from global memory, so that the weights' rows are on their way at once; the waves'
 // sums meet in LDS. Bound by latency: one row of 3456 x 1152 3.9 us, of 4096 x 16384 13 us (34 MB of weights, 2.7 TB/s).
@@ -554,11 +344,9 @@ hipError_t launch(const Mx4LinearDesc& d, hipStream_t s) {
     auto tiles = [&](int bm, int bn) { return dim3((unsigned)((long)((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn) * g.ksplit)); };
     switch (d.form) {
         case kMx4Rows: hipLaunchKernelGGL((mx4_rows_kernel<T, EPI>), tiles(16, 16), dim3(d.waves * kWave), 0, s, d); break;
-        case kMx4Any64: hipLaunchKernelGGL((mx4_linear_kernel<T, EPI, 64, 64, 2, 2>), tiles(64, 64), dim3(256), 0, s, d); break;
-        case kMx4Any256: hipLaunchKernelGGL((mx4_linear_kernel<T, EPI, 256, 256, 4, 2>), tiles(256, 256), dim3(512), 0, s, d); break;
-        case kMx4Stream64: hipLaunchKernelGGL((mx4_stream_kernel<T, EPI, 64, 64, 2, 2>), tiles(64, 64), dim3(256), 0, s, d); break;
-        case kMx4Stream128: hipLaunchKernelGGL((mx4_stream_kernel<T, EPI, 128, 128, 2, 2>), tiles(128, 128), dim3(256), 0, s, d); break;
-        case kMx4Stream256: hipLaunchKernelGGL((mx4_stream_kernel<T, EPI, 256, 256, 4, 2>), tiles(256, 256), dim3(512), 0, s, d); break;
+        case kMx4Tile64: hipLaunchKernelGGL((mx4_linear_kernel<T, EPI, 64, 64, 2, 2>), tiles(64, 64), dim3(256), 0, s, d); break;
+        case kMx4Tile128: hipLaunchKernelGGL((mx4_linear_kernel<T, EPI, 128, 128, 2, 2>), tiles(128, 128), dim3(256), 0, s, d); break;
+        case kMx4Tile256: hipLaunchKernelGGL((mx4_linear_kernel<T, EPI, 256, 256, 4, 2>), tiles(256, 256), dim3(512), 0, s, d); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
@@ -579,11 +367,11 @@ hipError_t launch(const Mx4LinearDesc& d, hipStream_t s) {
 // Form and K split: the least modelled time. A form with tiles of its side takes, with k workgroups on the fullest of 256
 // CUs (at most as many as fit) and `full` of the CUs busy, in us
 //   a + rounds (steps (s0 + s1 k + s2 full) + o0 + o1 k)
-// for `steps` of 256 columns in its K range, and a K split 2.3 + 1.36e-6 per range and output more. The form for few
-// rows takes its steps in up to 16 waves at once. Fitted to 9600 measured times (17 widths and depths, 128 to 16384, by 20 row counts,
-// 1 to 8192, each form, 1 to 32 ranges); the chosen pair takes 1.017 times the fastest on average, 1.40 times at most. In
-// us, rows / 64 / 128 / 256: 16 x 1152 x 1152 4.0 / 5.7 / 8.3 / 15, 410 x 4608 x 1152 31 / 7.4 / 9.4 / 16, 1024 x 16384 x 4096
-// - / 69 / 51 / 42, 8192 x 4096 x 16384 - / 510 / 328 / 267; 64 x 4096 x 16384 in 1 / 2 / 4 / 8 / 16 ranges 34 / 22 / 16 / 15 / 18.
+// for `steps` of 256 columns in its K range, and a K split 2.2 + 1.37e-6 per range and output more. The form for few
+// rows takes its steps in up to 16 waves at once. Fitted to 6105 measured times (21 widths and depths, 128 to 16384, by 20 row counts,
+// 1 to 8192, each form, 1 to 16 ranges); the chosen pair takes 1.015 times the fastest on average, 1.38 times at most. In
+// us, rows / 64 / 128 / 256: 16 x 1152 x 1152 4.6 / 6.0 / 8.6 / 15, 410 x 4608 x 1152 - / 8.4 / 10.5 / 17, 3000 x 2304 x 768 - / 12.2 /
+// 11.5 / 14.7, 8192 x 4096 x 16384 - / 588 / 350 / 276; 64 x 4096 x 16384 in 1 / 2 / 4 / 8 / 16 ranges 40 / 25 / 17 / 16 / 19.
 void plan_mx4_linear(Mx4LinearDesc& d, size_t part_floats) {
     GemmDesc& g = d.g;
     const int steps = (g.K + kStep - 1) / kStep;
@@ -597,18 +385,16 @@ void plan_mx4_linear(Mx4LinearDesc& d, size_t part_floats) {
         int form, side, most;
         double a, s0, s1, s2, o0, o1;
     };
-    static const Form forms[] = {{kMx4Any64, 64, 4, 3.2, 0.39, 0.16, 0.16, 0.0, 0.45},      {kMx4Any256, 256, 1, 5.1, 0.71, 1.14, 1.03, 1.25, 0.66},
-                                 {kMx4Stream64, 64, 4, 3.8, 0.26, 0.13, 0.08, 0.0, 0.56},   {kMx4Stream128, 128, 2, 4.0, 0.47, 0.22, 0.2, 0.0, 1.71},
-                                 {kMx4Stream256, 256, 1, 2.4, 0.83, 0.63, 0.45, 1.1, 5.1}};
-    const bool stream = g.K % 128 == 0 && ((reinterpret_cast<uintptr_t>(d.as) | reinterpret_cast<uintptr_t>(d.ws)) & 3) == 0;
+    static const Form forms[] = {{kMx4Tile64, 64, 4, 3.67, 0.235, 0.161, 0.149, 0.0, 0.44},
+                                 {kMx4Tile128, 128, 2, 3.95, 0.468, 0.247, 0.267, 0.0, 1.48},
+                                 {kMx4Tile256, 256, 1, 2.9, 0.868, 0.668, 0.484, 4.36, 0.769}};
     const double mn = (double)g.M * g.N;
     double least = 1e30;
     if (g.M <= 256) {
         const double tiles = (double)((g.M + 15) / 16) * ((g.N + 15) / 16);
-        least = 2.2 + 1.25 * ((steps + d.waves - 1) / d.waves) + 2.36e-6 * tiles * g.K + 0.085 * std::ceil(tiles / 256) * d.waves + 0.53e-6 * g.M * g.K;
+        least = 2.35 + 1.06 * ((steps + d.waves - 1) / d.waves) + 2.53e-6 * tiles * g.K + 0.061 * std::ceil(tiles / 256) * d.waves + 0.82e-6 * g.M * g.K;
     }
     for (const Form& f : forms) {
-        if ((f.form >= kMx4Stream64) != stream) continue;
         const long tiles = (long)((g.M + f.side - 1) / f.side) * ((g.N + f.side - 1) / f.side);
         int before = 0;
         for (int want : {1, 2, 3, 4, 6, 8, 12, 16}) {
@@ -619,7 +405,7 @@ void plan_mx4_linear(Mx4LinearDesc& d, size_t part_floats) {
             const double q = std::ceil(tiles * n / 256.0), k = std::min(q, (double)f.most), rounds = std::max(1.0, q / f.most);
             const double full = std::min(1.0, tiles * n / 256.0);
             double us = f.a + rounds * (chunk * (f.s0 + f.s1 * k + f.s2 * full) + f.o0 + f.o1 * k);
-            if (n > 1) us += 2.3 + 1.36e-6 * n * mn;
+            if (n > 1) us += 2.2 + 1.37e-6 * n * mn;
             if (us < least) {
                 least = us;
                 d.form = f.form;

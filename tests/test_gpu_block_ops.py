@@ -176,7 +176,7 @@ def test_nan_scales_stay_in_their_rows_and_columns(M, N, K):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("M,N,K,shift", [(300, 264, 128, 0), (300, 264, 256, 0), (300, 264, 384, 0), (300, 264, 4096, 0), (270, 200, 4224, 0),
                                          (4100, 4100, 384, 0), (4097, 4004, 512, 0), (2000, 4100, 640, 0), (2049, 4036, 1024, 0),
-                                         (1030, 2052, 2080, 0), (2000, 4100, 672, 0), (300, 264, 384, 1), (2000, 4100, 640, 2), (33, 68, 2048, 3)])
+                                         (1030, 2052, 2080, 0), (1900, 2052, 1056, 0), (600, 640, 12800, 0), (2000, 4100, 672, 0), (300, 264, 384, 1), (2000, 4100, 640, 2), (33, 68, 2048, 3)])
 def test_product_of_every_tile_size(dtype, M, N, K, shift):
     """Sizes that take small and large tiles, whole and half steps, K ranges; scales that start at any byte."""
     g = torch.Generator().manual_seed(M + K)
