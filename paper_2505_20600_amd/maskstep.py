@@ -189,7 +189,8 @@ EXPORTED = ("mask_abi_version", "mask_last_error", "mask_workspace_bytes", "mask
             "mask_fit_linear", "mask_batch_cost", "mask_route_request", "mask_plan_copies",
             "mask_probe_mfma", "mask_probe_lds", "mask_probe_operand_stream",
             "ms_kv8_keys", "ms_kv8_quantize", "ms_kv8_dequantize", "ms_kv8_attention_workspace_bytes",
-            "ms_kv8_attention")
+            "ms_kv8_attention", "ms_mx4_quantize", "ms_mx4_dequantize", "ms_mx4_linear_workspace_bytes", "ms_mx4_linear",
+            "ms_qk_norm_rope", "ms_shared_bits", "ms_shared_attention_workspace_bytes", "ms_shared_attention")
 
 MS_EPI_BIAS, MS_EPI_BIAS_RESID, MS_EPI_BIAS_GELU = 0, 1, 2
 
