@@ -57,15 +57,25 @@ struct Tables {
     int32_t own[kSharedMaxBatch + 1];
 };
 
-// Request of packed row r: the last one that starts at or before it (any request where starts do not ascend).
-__device__ __forceinline__ int request_of(const SharedAttnDesc& a, const Tables& t, int r) {
-    int lo = 0, hi = a.batch;               // row[lo] <= r or lo = 0, row[hi] > r or hi = batch
+// Request of packed row r: the last one of [lo, hi) that starts at or before it, lo where none does (any of them where starts do
+// not ascend).
+__device__ __forceinline__ int request_of(const Tables& t, int r, int lo, int hi) {
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (t.row[mid] <= r) lo = mid;
         else hi = mid;
     }
     return lo;
+}
+
+// The same of all requests, a lane to two of them, for a row that the whole wave asks for.
+__device__ __forceinline__ int request_of_all(const SharedAttnDesc& a, const Tables& t, int r) {
+    static_assert(kSharedMaxBatch == 2 * kWave, "requests");
+    if (a.batch == 1) return 0;
+    const int lane = threadIdx.x % kWave;
+    const uint64_t lower = __ballot(lane < a.batch && t.row[lane] <= r);
+    const uint64_t upper = a.batch > kWave ? __ballot(lane + kWave < a.batch && t.row[lane + kWave] <= r) : 0ull;
+    return upper ? 2 * kWave - 1 - __builtin_clzll(upper) : lower ? kWave - 1 - __builtin_clzll(lower) : 0;
 }
 
 // Row index of a query slot's (row, query head) in [M][n_heads].
@@ -89,8 +99,8 @@ __device__ __forceinline__ bool find_work(const SharedAttnDesc& a, int tile, int
     w.kvh = kvh;
     w.split = split;
     if (w.q0 >= w.slots) return false;
-    w.first = uniform(request_of(a, t, w.row0 + w.q0 / a.group));
-    w.last = uniform(request_of(a, t, w.row0 + (min(w.q0 + QT, w.slots) - 1) / a.group));
+    w.first = uniform(request_of_all(a, t, w.row0 + w.q0 / a.group));
+    w.last = max(uniform(request_of_all(a, t, w.row0 + (min(w.q0 + QT, w.slots) - 1) / a.group)), w.first);
     w.f0 = uniform(t.own[w.first]);
     w.f1 = max(uniform(t.own[w.last + 1]), w.f0);
     w.ntp = (a.T + KT - 1) / KT;
@@ -119,7 +129,7 @@ struct Sight {
     int lo, hi;                 // its request's own rows
     __device__ __forceinline__ void init(const SharedAttnDesc& a, const Tables& t, const Work& w, int slot) {
         const int s = min(slot, w.slots - 1);
-        const int b = request_of(a, t, w.row0 + s / a.group);
+        const int b = request_of(t, w.row0 + s / a.group, w.first, w.last + 1);
         at = (uint32_t)b * a.words * 8u;
         lo = t.own[b];
         hi = max(t.own[b + 1], lo);
@@ -313,20 +323,25 @@ struct Tiles {
 // The prefix tiles of 64 tokens that some request of the workgroup sees, 64 tiles at a time: every wave finds the same. A
 // request that hides 30% of the tokens as one region skips as many tiles (453 us without hidden tokens, 397 with, above).
 struct Live {
+    static constexpr int kMost = 8;     // requests
     uint64_t seen;
     int base, to;
     bool some;      // whether tiles are left out at all
     __device__ __forceinline__ void look(const SharedAttnDesc& a, const Work& w, int lane) {
         const int t = base + lane;
+        uint64_t v[kMost];      // all on their way at once
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) v[i] = a.bits[(long)min(w.first + i, w.last) * a.words + min(t, a.words - 1)];
         uint64_t hidden = ~0ull;
-        for (int b = w.first; b <= w.last; ++b) hidden &= a.bits[(long)b * a.words + min(t, a.words - 1)];
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) hidden &= v[i];
         seen = __ballot(t < to && hidden != ~0ull);
     }
     // of tiles [from, to); a few tiles, or those of many requests, are all taken
     __device__ __forceinline__ void init(const SharedAttnDesc& a, const Work& w, int lane, int from, int end) {
         base = from;
         to = end;
-        some = a.bits && end - from >= 8 && w.last >= w.first && w.last - w.first < 8;
+        some = a.bits && end - from >= 8 && w.last - w.first < kMost;
         if (some) look(a, w, lane);
     }
     // the first tile from t on, `to` where there is none
