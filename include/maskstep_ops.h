@@ -205,7 +205,8 @@ ms_status ms_mx4_linear(int32_t dtype, int32_t M, int32_t N, int32_t K, const vo
  *   (y_i, y_j) <- (y_i cos - y_j sin, y_j cos + y_i sin)   (the first `rot` columns)
  * with the pairs (i, j) = (2p, 2p + 1) or (p, p + rot / 2) and cos, sin =
  * table[pos[m]][p]. Q goes to q[m], K and V of packed row m to kv[dst_rows[m]]. Float32
- * within, one rounding; V is copied. Conventions as above; a row of kv must not
+ * within, one rounding; V is copied. The norm holds for heads of any finite size, also where float32
+ * does not hold their squares; a head of zeros is 0, with eps = 0 NaN. Conventions as above; a row of kv must not
  * be named twice in one call, and the outputs must not overlap the inputs.
  * Limits: rows 0..2^26; heads 1..1024 each; head_dim a multiple of 8, <= 128; ld whole 16 bytes. */
 enum { MS_ROPE_PAIRS = 0, MS_ROPE_HALVES = 1 };

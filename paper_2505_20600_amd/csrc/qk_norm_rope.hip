@@ -11,6 +11,12 @@
 // 32768 rows of 16 Q, K and V heads of 72 (bf16) take 95 us, 4.9 TB/s where a copy of as much reaches 5.3; 24 + 8 + 8
 // heads of 128 127 us (5.4 TB/s), of 12 heads of 64 62 us (5.0); float32, 8 heads of 64 78 us (5.2). One row of 24
 // heads of 128 5.1 us, a launch and one chain of loads.
+//
+// Where the mean square with eps lies far out in float32 the head is scaled by the power of two that brings its largest
+// element, or the root of eps, near 1, and eps by its square: exact but for what is 2^-126 of the largest. Far out is infinite,
+// or below 2^-46: squares lose digits further down and the root's instruction takes a subnormal as 0, and a reciprocal root above 2^23
+// would lift the last place of a subnormal product above 2^-126. A head whose root mean square is 1e-7 is there only with
+// an eps as small.
 #include <algorithm>
 
 #include "kernels.h"
@@ -205,7 +211,45 @@ __global__ __launch_bounds__(kThreads, 4) void qk_norm_rope_kernel(QkNormRopeDes
             }
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u) ss[u] = __shfl(ss[u], sub * lph, kWave);
+            // 1 / sqrt(mean + eps) of the head times 2^down, that power of two the one near its largest element
+            auto scaled_inv = [&](const vec16& r, int& down) {
+                float x[VEC], big = sqrtf(d.eps), sum = 0.f;
+                load_vec<T>(reinterpret_cast<const T*>(&r), x);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) big = fmaxf(big, fabsf(x[e]));
+                for (int o = 1; o < lph; o <<= 1) {
+                    const float t = __shfl_down(big, o, kWave);
+                    if (at + o < lph) big = fmaxf(big, t);
+                }
+                big = __shfl(big, sub * lph, kWave);
+                down = -__builtin_amdgcn_frexp_expf(big);       // 0 for 0, infinities and NaN
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float t = ldexpf(x[e], down);
+                    sum = fmaf(t, t, sum);
+                }
+                for (int o = 1; o < lph; o <<= 1) {
+                    const float t = __shfl_down(sum, o, kWave);
+                    if (at + o < lph) sum += t;
+                }
+                sum = __shfl(sum, sub * lph, kWave);
+                return __builtin_amdgcn_rsqf(fmaf(sum, per, ldexpf(d.eps, 2 * down)));
+            };
             auto turned = [&](int u, const float (&fc_)[VEC], const float (&fs_)[VEC], bool norm) {
+                float inv = 1.0f;
+                int down = 0;
+                bool any = false;
+                if (norm) {
+                    const float mean = fmaf(ss[u], per, d.eps);
+                    const bool far = !(mean >= 0x1p-46f && mean < INFINITY);
+                    inv = __builtin_amdgcn_rsqf(mean);
+                    any = __any(far);
+                    if (any) {
+                        const float scaled = scaled_inv(raw[u], down);
+                        if (far) inv = scaled;
+                        else down = 0;
+                    }
+                }
                 float v[VEC], p[VEC], y[VEC];
                 load_vec<T>(reinterpret_cast<const T*>(&raw[u]), v);
                 if constexpr (PAIRING == kPairs) {
@@ -221,7 +265,13 @@ __global__ __launch_bounds__(kThreads, 4) void qk_norm_rope_kernel(QkNormRopeDes
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) p[e] = Elt<T>::to_f32(x[col + e < d.rot ? partner(e) : 0]);
                 }
-                const float inv = norm ? __builtin_amdgcn_rsqf(fmaf(ss[u], per, d.eps)) : 1.0f;
+                if (any) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        v[e] = ldexpf(v[e], down);
+                        p[e] = ldexpf(p[e], down);
+                    }
+                }
                 if (turn && whole_heads) {
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) y[e] = fmaf(p[e], fs_[e], v[e] * fc_[e]) * inv;
