@@ -236,9 +236,10 @@ ms_status ms_qk_norm_rope(const ms_qk_norm_rope_args* a, void* stream);
  * j over the prefix tokens that row m's request b does not hide, then its own rows
  * [fresh_start[b], fresh_start[b + 1]); K/V head h / (n_heads / n_kv_heads). A row
  * without any key gives zeros, and so does one whose scores are all -infinity
- * (scores are float32, and one beyond its range is infinite; one of +infinity makes its
+ * (scores are float32, q[m][h].k_j before the scale too, and one beyond its range is infinite; one of +infinity makes its
  * row NaN). What a row does not see has no effect on it whatever it holds; a NaN in a
- * query or in a key or value that it sees makes it NaN. Rows outside [seg_start[0],
+ * query or in a key or value that it sees makes it NaN. Finite values give a finite result, up
+ * to the type's largest (less float32's rounding), whatever the weights sum to. Rows outside [seg_start[0],
  * seg_start[batch]) are left as they are.
  * Scores, maxima, sums and the parts of key ranges are float32. bf16 rounds twice: the
  * weights w_j relative to the running maximum, the matrix cores' operand (numerator

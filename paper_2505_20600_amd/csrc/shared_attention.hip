@@ -20,7 +20,8 @@
 //
 // A hidden key's weight is 0, and 0 times an infinity or NaN in its V row is NaN: a
 // slot whose result is not finite is computed again over the keys that it sees, one
-// wave at a slot (recompute). Finite inputs never come there.
+// wave at a slot (recompute). So is one whose sums of finite values, the weights above 1 and not yet divided by their own
+// sum, leave float32: the second computation and the join keep weights that sum to at most 1.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -156,7 +157,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t hidden_table(const SharedAttnD
 }
 
 // One slot's result over the keys [t0, t1) that it sees, by a wave: 64 keys at a time, a
-// lane's key's score, then the lanes as columns of the weighted sum.
+// lane's key's score, then the lanes as columns of the weighted mean so far (not a sum: the mean of finite values is finite).
 template <typename T, int KT>
 __device__ __forceinline__ void recompute(const SharedAttnDesc& a, const Work& w, const Tables& t, int slot) {
     const int lane = threadIdx.x % kWave, hd = a.hd, dkv = a.heads * hd;
@@ -188,25 +189,26 @@ __device__ __forceinline__ void recompute(const SharedAttnDesc& a, const Work& w
             const float corr = m == -INFINITY ? 0.f : fast_exp2(m - ref);
             const float p = sees ? fast_exp2(s - ref) : 0.f;
             m = up;
-            l = l * corr + wave_sum(p);
-            o[0] *= corr;
-            o[1] *= corr;
+            const float before = l * corr;
+            l = before + wave_sum(p);
+            const float inv = l == 0.f ? 0.f : 1.0f / l;
+            o[0] *= before * inv;
+            o[1] *= before * inv;
             for (int j = 0; j < kWave; ++j) {
                 if (!((seen >> j) & 1)) continue;
-                const float pj = __shfl(p, j, kWave);
+                const float pj = __shfl(p, j, kWave) * inv;
                 const T* const row = kv + (long)(k + j) * 2 * dkv + dkv;
                 if (lane < hd) o[0] = fmaf(pj, Elt<T>::to_f32(row[lane]), o[0]);
                 if (lane + kWave < hd) o[1] = fmaf(pj, Elt<T>::to_f32(row[lane + kWave]), o[1]);
             }
         }
     }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
     const long part = (long)w.split * a.M * a.heads * a.group + at;
     for (int i = 0; i < 2; ++i) {
         const int c = lane + i * kWave;
         if (c >= hd) continue;
-        if (a.nsplit == 1) static_cast<T*>(a.o)[at * hd + c] = Elt<T>::from_f32(o[i] * inv);
-        else a.part_o[part * hd + c] = o[i] * inv;
+        if (a.nsplit == 1) static_cast<T*>(a.o)[at * hd + c] = Elt<T>::from_f32(o[i]);
+        else a.part_o[part * hd + c] = o[i];
     }
     if (a.nsplit > 1 && lane == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * part) = make_float2(m, l);
 }
@@ -951,8 +953,11 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedAttnDesc a)
     if (lane < a.nsplit) ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (lane * plane + sr));
     float m = wave_max(ml.x);
     if (__any(ml.x != ml.x)) m = __uint_as_float(0x7fc00000u);      // maxima drop NaN
-    const float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m) * ml.y;
-    const float L = wave_sum(f);
+    float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m) * ml.y;
+    float L = wave_sum(f);
+    const int down = -__builtin_amdgcn_frexp_expf(L);       // weights that sum to less than 1; 0 for 0 and NaN
+    f = ldexpf(f, down);
+    L = ldexpf(L, down);
     const float inv = L == 0.f ? 0.f : 1.0f / L;
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
     const float* const po = a.part_o + sr * hd + col * 4;

@@ -1,9 +1,13 @@
-"""Per-head norms with rotation at the far ends of their types, against the float64 oracle."""
+"""Per-head norms with rotation and attention over a shared prefix at the far ends of their types, against the float64
+oracle."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_block_ops import DT, _qk_case, _qk_check
+from oracle import shared
+from tests.test_gpu_block_ops import DEV, DT, _attend, _attend_bound, _batch, _np, _qk_case, _qk_check, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +41,28 @@ def test_norms_with_eps_of_the_size_of_the_mean_square(dtype, eps, M):
     g = torch.Generator().manual_seed(M)
     s = _qk_case(g, dtype, M, 6, 2, 64, 64, 0, 60, M + 5)
     _qk_check(s, dtype, 6, 2, 64, True, float(np.float32(eps)))
+
+
+# ------------------------------------------------------------------ attention
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [(3,), (20, 9), (60, 140), (800, 7)], ids=lambda r: f"{sum(r)}")
+@pytest.mark.parametrize("values", ["one", "both signs", "few"])
+@pytest.mark.parametrize("ws", [None, "need"])
+def test_values_near_the_largest_of_the_type(dtype, rows, values, ws):
+    """Results are means of the values, so they are finite where the values are, whatever the weights sum to."""
+    g = torch.Generator().manual_seed(sum(rows))
+    s = _batch(g, dtype, rows, 700, 2, 64, 1, hide=0.2)
+    big = 3e38
+    for kv in (s["kv"], s["fresh"]):
+        v = kv[:, 1]
+        if values == "one":
+            v.fill_(big)
+        elif values == "both signs":
+            v.copy_(torch.where(torch.rand(v.shape, generator=g) < 0.5, big, -big).to(DT[dtype]).to(DEV))
+        else:
+            v[::97] = big
+    hd = s["q"].shape[2]
+    want, spread, size, reach = shared.attention(_np(s["q"]), _np(s["kv"]), s["hidden"].numpy(), s["seg"], _np(s["fresh"]), s["own"], 1 / math.sqrt(hd))
+    keys = len(s["kv"]) + len(s["fresh"])
+    _within(_np(_attend(s, ws)), want, _attend_bound(want, spread, size, reach, keys, hd, dtype), f"{values} {ws}")
