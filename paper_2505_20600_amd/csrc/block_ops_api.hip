@@ -37,9 +37,8 @@ ms_status check_product(int32_t M, int32_t N, int32_t K) {
     if (M < 0 || M > kMaxRows) return set_error(MS_ESHAPE, "M %d outside 0..2^26", M);
     if (N < 4 || N % 4 || N > (1 << 20)) return set_error(MS_ESHAPE, "N %d must be a multiple of 4, 4..2^20", N);
     if (K < 32 || K % 32 || K > (1 << 20)) return set_error(MS_ESHAPE, "K %d must be a multiple of 32, 32..2^20", K);
-    // outputs and their 64 x 64 tiles are counted in 32 bits
-    if (((int64_t)M + 15) / 16 * (((int64_t)N + 15) / 16) >= (1ll << 23))
-        return set_error(MS_ESHAPE, "M x N above 2^31");
+    // then fewer than 2^21 tiles of 64 rows and columns or more, and at most 2^29 threads of the pass over a K split
+    if ((int64_t)M * N > (1ll << 31)) return set_error(MS_ESHAPE, "M x N, %lld, above 2^31", (long long)M * N);
     return MS_OK;
 }
 
