@@ -190,6 +190,10 @@ ms_status ms_mx4_dequantize(int32_t dtype, const void* codes, const void* scales
  * error set on invalid sizes, else the error is cleared). */
 size_t ms_mx4_linear_workspace_bytes(int32_t M, int32_t N, int32_t K);
 
+/* What ms_mx4_linear launches for these sizes with ws_bytes of workspace (for parity tests and tuning): a workgroup's
+ * outputs are tile x tile (16, 64, 128 or 256), K is split into `ranges`. */
+ms_status ms_mx4_linear_plan(int32_t M, int32_t N, int32_t K, size_t ws_bytes, int32_t* tile, int32_t* ranges);
+
 /* out[M][N] = epilogue(A W^T + bias[N] (+ resid[M][N])), A [M][K] and W [N][K] codes and scales, float32 sums, one
  * rounding to `dtype` (that of bias, resid and out). A NaN scale makes its row (of A) or column (of W) NaN. With less
  * workspace than the above (or none) K is split into fewer ranges; the order of summation then differs. */
@@ -272,6 +276,10 @@ ms_status ms_shared_bits(const void* mask, int32_t batch, int32_t tokens, uint64
 /* Bytes of workspace with which ms_shared_attention may split the keys as it sees fit (0 when it would not; 0 with the error set on
  * invalid arguments, else the error is cleared). The tables are not read. */
 size_t ms_shared_attention_workspace_bytes(int32_t dtype, const ms_shared_attn* a);
+
+/* What ms_shared_attention launches for such arguments with ws_bytes of workspace (for parity tests and tuning): `tile` query
+ * slots (a row and a query head of one K/V head) per workgroup (16, 32, or in bf16 128), the keys in `ranges`. The tables are not read. */
+ms_status ms_shared_attention_plan(int32_t dtype, const ms_shared_attn* a, size_t ws_bytes, int32_t* tile, int32_t* ranges);
 
 /* With less workspace than that (or none) it splits into fewer ranges; the order of summation
  * then differs, and with it the last bits. */

@@ -98,6 +98,12 @@ ms_status check_attn(int32_t dtype, const ms_shared_attn* a, ms::SharedAttnDesc*
 // Float32 words of partial results per key range.
 size_t range_floats(const ms::SharedAttnDesc& d) { return (size_t)d.M * d.heads * d.group * (d.hd + 2); }
 
+// The form and the key ranges of a call with rows, its parts within ws_bytes.
+void plan_attn(int32_t dtype, ms::SharedAttnDesc& d, size_t ws_bytes) {
+    ms::plan_shared_attention(dtype, d);
+    d.nsplit = std::max(1, std::min(d.nsplit, (int)std::min<size_t>(ws_bytes / (range_floats(d) * sizeof(float)), 1024)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -165,6 +171,20 @@ ms_status ms_mx4_linear(int32_t dtype, int32_t M, int32_t N, int32_t K, const vo
     return ms::clear_error();
 }
 
+ms_status ms_mx4_linear_plan(int32_t M, int32_t N, int32_t K, size_t ws_bytes, int32_t* tile, int32_t* ranges) {
+    if (!tile || !ranges) return set_error(MS_EINVAL, "tile or ranges is NULL");
+    ms_status st = check_product(M, N, K);
+    if (st != MS_OK) return st;
+    ms::Mx4LinearDesc d{};
+    d.g.M = M;
+    d.g.N = N;
+    d.g.K = K;
+    ms::plan_mx4_linear(d, ws_bytes / sizeof(float));
+    *tile = d.form == ms::kMx4Rows ? 16 : d.form == ms::kMx4Tile64 ? 64 : d.form == ms::kMx4Tile128 ? 128 : 256;
+    *ranges = d.g.ksplit;
+    return ms::clear_error();
+}
+
 ms_status ms_qk_norm_rope(const ms_qk_norm_rope_args* a, void* stream) {
     if (!a) return set_error(MS_EINVAL, "arguments are NULL");
     if (!known_dtype(a->dtype)) return set_error(MS_EDTYPE, "unknown dtype %d", a->dtype);
@@ -216,15 +236,24 @@ size_t ms_shared_attention_workspace_bytes(int32_t dtype, const ms_shared_attn* 
     return d.nsplit > 1 ? d.nsplit * range_floats(d) * sizeof(float) : 0;
 }
 
+ms_status ms_shared_attention_plan(int32_t dtype, const ms_shared_attn* a, size_t ws_bytes, int32_t* tile, int32_t* ranges) {
+    if (!tile || !ranges) return set_error(MS_EINVAL, "tile or ranges is NULL");
+    ms::SharedAttnDesc d;
+    ms_status st = check_attn(dtype, a, &d);
+    if (st != MS_OK) return st;
+    if (d.M > 0) plan_attn(dtype, d, ws_bytes);
+    *tile = d.tile;
+    *ranges = d.nsplit;
+    return ms::clear_error();
+}
+
 ms_status ms_shared_attention(int32_t dtype, const ms_shared_attn* a, void* d_ws, size_t ws_bytes, void* stream) {
     ms::SharedAttnDesc d;
     ms_status st = check_attn(dtype, a, &d);
     if (st != MS_OK) return st;
     if (!aligned(d_ws, 16)) return set_error(MS_EALIGN, "workspace not 16-byte aligned");
     if (d.M == 0) return ms::clear_error();
-    const size_t one = range_floats(d) * sizeof(float);
-    ms::plan_shared_attention(dtype, d);
-    d.nsplit = std::max(1, std::min(d.nsplit, d_ws ? (int)std::min<size_t>(ws_bytes / one, 1024) : 1));
+    plan_attn(dtype, d, d_ws ? ws_bytes : 0);
     if (d.nsplit > 1) {
         d.part_o = static_cast<float*>(d_ws);
         d.part_ml = d.part_o + (size_t)d.nsplit * d.M * d.heads * d.group * d.hd;

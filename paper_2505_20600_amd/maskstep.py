@@ -146,9 +146,11 @@ def load() -> C.CDLL:
             "ms_mx4_dequantize": (i32, [i32, vp, vp, C.c_int64, i32, vp, C.c_int64, vp]),
             "ms_mx4_linear_workspace_bytes": (sz, [i32, i32, i32]),
             "ms_mx4_linear": (i32, [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]),
+            "ms_mx4_linear_plan": (i32, [i32, i32, i32, sz, C.POINTER(i32), C.POINTER(i32)]),
             "ms_qk_norm_rope": (i32, [C.POINTER(QkNormRopeArgs), vp]),
             "ms_shared_bits": (i32, [vp, i32, i32, vp, vp]),
             "ms_shared_attention_workspace_bytes": (sz, [i32, C.POINTER(SharedAttn)]),
+            "ms_shared_attention_plan": (i32, [i32, C.POINTER(SharedAttn), sz, C.POINTER(i32), C.POINTER(i32)]),
             "ms_shared_attention": (i32, [i32, C.POINTER(SharedAttn), vp, sz, vp]),
             "ms_kv8_keys": (i32, [vp, i32, i32, vp, i32, vp, vp]),
             "ms_kv8_quantize": (i32, [C.POINTER(Kv8Cache), vp, C.c_int64, C.c_int64, vp, vp]),
@@ -189,8 +191,9 @@ EXPORTED = ("mask_abi_version", "mask_last_error", "mask_workspace_bytes", "mask
             "mask_fit_linear", "mask_batch_cost", "mask_route_request", "mask_plan_copies",
             "mask_probe_mfma", "mask_probe_lds", "mask_probe_operand_stream",
             "ms_kv8_keys", "ms_kv8_quantize", "ms_kv8_dequantize", "ms_kv8_attention_workspace_bytes",
-            "ms_kv8_attention", "ms_mx4_quantize", "ms_mx4_dequantize", "ms_mx4_linear_workspace_bytes", "ms_mx4_linear",
-            "ms_qk_norm_rope", "ms_shared_bits", "ms_shared_attention_workspace_bytes", "ms_shared_attention")
+            "ms_kv8_attention", "ms_mx4_quantize", "ms_mx4_dequantize", "ms_mx4_linear_workspace_bytes", "ms_mx4_linear_plan", "ms_mx4_linear",
+            "ms_qk_norm_rope", "ms_shared_bits", "ms_shared_attention_workspace_bytes", "ms_shared_attention_plan",
+            "ms_shared_attention")
 
 MS_EPI_BIAS, MS_EPI_BIAS_RESID, MS_EPI_BIAS_GELU = 0, 1, 2
 
@@ -479,6 +482,13 @@ def ms_mx4_linear_workspace_bytes(a_codes, w_codes) -> int:
     return n
 
 
+def ms_mx4_linear_plan(a_codes, w_codes, workspace_bytes=0):
+    """(rows and columns of a workgroup's outputs, ranges of K) that ms_mx4_linear takes for codes of these shapes."""
+    tile, ranges = C.c_int32(), C.c_int32()
+    _check(load().ms_mx4_linear_plan(a_codes.shape[0], w_codes.shape[0], 2 * w_codes.shape[1], workspace_bytes, C.byref(tile), C.byref(ranges)))
+    return tile.value, ranges.value
+
+
 def _workspace(workspace, dev):
     if workspace is None:
         return 0, 0
@@ -540,16 +550,29 @@ def ms_shared_bits(mask, bits, *, stream=None):
     _kv8_run(load().ms_shared_bits, mask, stream, mask.data_ptr(), B, T, bp)
 
 
+def _shared_shapes(q, kv, fresh):
+    """Arguments of these shapes; their addresses are checked but not read."""
+    some = _KV8_NO_ENTRIES
+    n_own = 0 if fresh is None else fresh.shape[0]
+    return SharedAttn(some, some, q.shape[0], q.shape[1], kv.shape[2], q.shape[2], some, kv.shape[0], 1, None, some,
+                      some if n_own else None, n_own, some, 0.0)
+
+
 def ms_shared_attention_workspace_bytes(q, kv, *, fresh=None) -> int:
     """Bytes of workspace with which ms_shared_attention may split the keys as it sees fit, for tensors of these shapes."""
-    some = _KV8_NO_ENTRIES   # addresses are checked but not read
-    n_own = 0 if fresh is None else fresh.shape[0]
-    a = SharedAttn(some, some, q.shape[0], q.shape[1], kv.shape[2], q.shape[2], some, kv.shape[0], 1, None, some,
-                   some if n_own else None, n_own, some, 0.0)
+    a = _shared_shapes(q, kv, fresh)
     n = load().ms_shared_attention_workspace_bytes(_KV8_DTYPES.get(q.dtype, -1), C.byref(a))
     if n == 0 and load().mask_last_error():
         raise _bad(load().mask_last_error().decode())
     return n
+
+
+def ms_shared_attention_plan(q, kv, *, fresh=None, workspace_bytes=0):
+    """(query slots of a workgroup, ranges of the keys) that ms_shared_attention takes for tensors of these shapes."""
+    tile, ranges = C.c_int32(), C.c_int32()
+    _check(load().ms_shared_attention_plan(_KV8_DTYPES.get(q.dtype, -1), C.byref(_shared_shapes(q, kv, fresh)), workspace_bytes,
+                                           C.byref(tile), C.byref(ranges)))
+    return tile.value, ranges.value
 
 
 def ms_shared_attention(q, kv, out, *, seg_start=None, bits=None, fresh=None, fresh_start=None, scale=None, workspace=None,
