@@ -233,12 +233,14 @@ ms_status ms_qk_norm_rope(const ms_qk_norm_rope_args* a, void* stream);
 
 /* ------------------------------------------------------------------------
  * Attention of a batch over one shared prefix: the requests edit one template (or
- * follow one prompt), whose K/V rows are read and multiplied once for all of
+ * follow one prompt, a row at a time), whose K/V rows are read and multiplied once for all of
  * them; each request hides prefix tokens of its own (those it recomputes) and brings K/V
  * rows of its own, one softmax over both:
  *   out[m][h] = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q[m][h].k_j),
  * j over the prefix tokens that row m's request b does not hide, then its own rows
- * [fresh_start[b], fresh_start[b + 1]); K/V head h / (n_heads / n_kv_heads). A row
+ * [fresh_start[b], fresh_start[b + 1]); K/V head h / (n_heads / n_kv_heads). There is no order
+ * among own rows: a row sees all of its request's, so that several rows of a causal continuation
+ * in one call would see later ones. A row
  * without any key gives zeros, and so does one whose scores are all -infinity
  * (scores are float32, q[m][h].k_j before the scale too, and one beyond its range is infinite; one of +infinity makes its
  * row NaN). What a row does not see has no effect on it whatever it holds; a NaN in a

@@ -3,8 +3,9 @@
 // Both are bound by the wide side's bytes. A lane has eight consecutive elements,
 // 16 bytes of bf16 or 32 of float32, and one word of codes, so that a wave reads or
 // writes 1 KB (2 KB) and 256 bytes in a row; the four lanes of a block of 32 share its
-// largest magnitude through two exchanges. At 16384 rows of 4096, bf16: codes in 26 us
-// (6.5 TB/s), read back in 26 us (6.5 TB/s); float32 48 us (6.4 TB/s) and 62 us (4.9 TB/s).
+// largest magnitude through two exchanges. At 16384 rows of 4096, bf16: codes in 27 us and read back in 26 us where
+// the last-level cache holds the rows (6.3 and 6.5 TB/s, a copy there 7.0), 32 and 34 us over buffers that no cache holds (5.3 and
+// 5.0, a copy 5.3); float32 there 53 us (5.8) and 62 us (4.9).
 #include <algorithm>
 
 #include "mx4.h"
@@ -112,8 +113,8 @@ hipError_t launch_mx4_quantize(int dtype, const void* x, long rows, int cols, lo
     if (rows == 0) return hipSuccess;
     const int per = cols / 8;
     const long n = rows * per;
-    // bf16 pieces are one load: four at once where there are enough to fill the CUs with them. 16384 rows of 4096 take 26 us
-    // instead of 30, 2048 rows of 1152 would take 3.9 instead of 3.6; in float32 four at once gain nothing (48 us both ways).
+    // bf16 pieces are one load: four at once where there are enough to fill the CUs with them. 16384 rows of 4096, in the cache,
+    // take 26 us instead of 30, 2048 rows of 1152 would take 3.9 instead of 3.6; in float32 four at once gain nothing (48 us both ways).
     if (dtype != kBF16) quantize<float, 1>(x, n, per, ld, codes, scales, s);
     else if (n < 1 << 20) quantize<bf16_t, 1>(x, n, per, ld, codes, scales, s);
     else quantize<bf16_t, 4>(x, n, per, ld, codes, scales, s);

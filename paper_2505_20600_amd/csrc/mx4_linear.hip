@@ -161,7 +161,8 @@ __device__ __forceinline__ void write_tile(const GemmDesc& g, int m0, int n0, in
 // Tiles of BM x BN outputs by WM x WN waves, steps of 256 elements of K in two stages of LDS. Codes land
 // there by direct loads; a step's scales (8 bytes a row) come through registers, a thread to a row, and are laid
 // out so that a lane finds those of its row and columns for two fragments and both halves of the step in one word.
-// 8192 x 4096 x 16384 in tiles of 256 takes 271 us, 4.06 PFLOP/s of the 7.1 to 7.7 that the instruction reaches alone:
+// 8192 x 4096 x 16384 in tiles of 256 takes 269 to 280 us by the card where such calls follow each other (290 to 300 among other
+// work, up to 340 after an idle card), 3.9 to 4.1 PFLOP/s of the 7.1 to 7.7 that the instruction reaches alone:
 // matrix cores busy 41%, the rest is the stream of operands into a CU (direct loads cost it about four cycles per 128-byte
 // line, 512 of them a step) and its LDS reads, which two stages and one workgroup per CU overlap in part. A ring of three
 // regions with the next step's fragments and scales (through LDS as well) read under the last products took 271 us too, 283
@@ -292,7 +293,8 @@ __global__ __launch_bounds__(WM * WN * kWave) void mx4_linear_kernel(Mx4LinearDe
 
 // Few rows: 16 x 16 outputs per workgroup of up to 16 waves; every wave has 256-element steps of its own (step wave +
 // waves i) and loads its fragments from global memory, so that the weights' rows are on their way at once; the waves'
-// sums meet in LDS. Bound by latency: one row of 3456 x 1152 3.9 us, of 4096 x 16384 13 us (34 MB of weights, 2.7 TB/s).
+// sums meet in LDS. Bound by latency, and with large weights by its loads, a lane's scale one byte of a line of its own: one row of
+// 3456 x 1152 3.0 us, of 4096 x 16384 12.3 us (36 MB of weights, 2.9 TB/s), 3.5 and 12.9 us with weights that no cache holds.
 template <typename T, int EPI>
 __global__ __launch_bounds__(1024) void mx4_rows_kernel(Mx4LinearDesc d) {
     constexpr int OLD = 20;
@@ -386,8 +388,9 @@ hipError_t launch(const Mx4LinearDesc& d, hipStream_t s) {
 //   a + rounds (steps (s0 + s1 k + s2 full) + o0 + o1 k)
 // for `steps` of 256 columns in its K range, and a K split 2.2 + 1.37e-6 per range and output more. The form for few
 // rows takes its steps in up to 16 waves at once. Fitted to 6105 measured times (21 widths and depths, 128 to 16384, by 20 row counts,
-// 1 to 8192, each form, 1 to 16 ranges); the chosen pair takes 1.015 times the fastest on average, 1.38 times at most. In
-// us, rows / 64 / 128 / 256: 16 x 1152 x 1152 4.6 / 6.0 / 8.6 / 15, 410 x 4608 x 1152 - / 8.4 / 10.5 / 17, 3000 x 2304 x 768 - / 12.2 /
+// 1 to 8192, each form, 1 to 16 ranges); the chosen pair takes 1.015 times the fastest on average, 1.38 times at most (one row of
+// 4096 x 16384, with a workspace, 14.9 us in 16 ranges of tiles of 64; the form for few rows has 12.3). In
+// us, as graphs of one card, rows / 64 / 128 / 256: 16 x 1152 x 1152 4.6 / 6.0 / 8.6 / 15, 410 x 4608 x 1152 - / 8.4 / 10.5 / 17, 3000 x 2304 x 768 - / 12.2 /
 // 11.5 / 14.7, 8192 x 4096 x 16384 - / 588 / 350 / 276; 64 x 4096 x 16384 in 1 / 2 / 4 / 8 / 16 ranges 40 / 25 / 17 / 16 / 19.
 void plan_mx4_linear(Mx4LinearDesc& d, size_t part_floats) {
     GemmDesc& g = d.g;

@@ -8,15 +8,16 @@
 // as many heads side by side as a wave holds, and walk over the row's heads: their
 // columns stay the same, so the products of gains and (cos, sin) are formed once per row and
 // live in registers. Sums of squares, norms and rotations are float32; the result is rounded once.
-// 32768 rows of 16 Q, K and V heads of 72 (bf16) take 95 us, 4.9 TB/s where a copy of as much reaches 5.3; 24 + 8 + 8
-// heads of 128 127 us (5.4 TB/s), of 12 heads of 64 62 us (5.0); float32, 8 heads of 64 78 us (5.2). One row of 24
-// heads of 128 5.1 us, a launch and one chain of loads.
+// 32768 rows of 16 Q, K and V heads of 72 (bf16) take 98 us, 4.7 TB/s where a copy of as much reaches 5.3; 24 + 8 + 8
+// heads of 128 133 us (5.2 TB/s), of 12 heads of 64 65 us (4.8); float32, 8 heads of 64 81 us (5.1). One row of 24
+// heads of 128 4.5 us, a launch and one chain of loads.
 //
 // Where the mean square with eps lies far out in float32 the head is scaled by the power of two that brings its largest
 // element, or the root of eps, near 1, and eps by its square: exact but for what is 2^-126 of the largest. Far out is infinite,
 // or below 2^-46: squares lose digits further down and the root's instruction takes a subnormal as 0, and a reciprocal root above 2^23
 // would lift the last place of a subnormal product above 2^-126. A head whose root mean square is 1e-7 is there only with
-// an eps as small.
+// an eps as small. Looking for such heads costs 1 to 4% (95, 132, 62 and 81 us above without it); scaling them at the wave's end,
+// out of the passes' way, took 101, 134, 69 and 81, one branch for four passes 100, 133, 66 and 81.
 #include <algorithm>
 
 #include "kernels.h"
